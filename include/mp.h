@@ -36,6 +36,10 @@
  *     learns of it from mp_state_read (status) or mp_gemm_device_status, and resumes with
  *     mp_gemm_device_status (which clears the device-wide word) followed by mp_state_write
  *     with status = 0.
+ *   - Token ids live in device memory, so only a kernel can see that one is out of range.  It
+ *     reads nothing through such an id, marks the row's outputs (see the calls) and records
+ *     MP_ERR_INVALID_ARG in state->status when the call was given a state, which freezes the
+ *     training state as above.
  */
 #ifndef MP_H_
 #define MP_H_
@@ -96,7 +100,8 @@ typedef struct {
   int32_t growth_interval, dynamic;
   int32_t good_steps;  /* clean steps since S last changed                                  */
   int32_t found_inf;   /* flag accumulated by the current step so far                       */
-  int32_t status;      /* MP_OK or the first device-side error (MP_ERR_TIMEOUT), see above  */
+  int32_t status;      /* MP_OK or the first device-side error (MP_ERR_TIMEOUT, or
+                          MP_ERR_INVALID_ARG for a token id out of range), see above        */
   int32_t overflow_tolerance;
   int32_t strikes;     /* overflows since S last changed (dynamic scale with tolerance 1:
                           always 0; static scale: S never changes, so every overflow counts) */
@@ -267,6 +272,128 @@ int mp_lstm_cell_fwd(const void* G16, int64_t ldg, const void* c_prev16, void* c
 int mp_lstm_cell_bwd(const void* G16, int64_t ldg, const void* c_prev16, const void* c_new16,
                      const void* dh16, const void* dc_in16, void* dG16, int64_t lddg, void* dc_prev16,
                      int64_t M, int64_t H, void* stream);
+
+/* ---- operators of a token model ---------------------------------------------------------
+ * What stands around the products when the stack is a language model: the embedding that turns
+ * tokens into its input, the norms, gate and residual sum that join its blocks, the loss whose
+ * gradient enters its top layer, and an AdamW update.  (The paper's models have an embedding and
+ * train with Adam; it gives no arithmetic for these.)  Matrices are FP16 with row pitches that
+ * are multiples of 8 and may have any width: what lies between the width and the pitch is not
+ * written, and its values do not matter.  Sums, norms and softmax statistics are FP32; each
+ * stored value is rounded once.  No call uses floating-point atomics: the same inputs give the
+ * same bits.  Gradients arrive and leave multiplied by the loss scale; a call that is given a
+ * state sets state->found_inf when a parameter gradient or logit gradient that it stores is inf
+ * or NaN. */
+
+/* Y[i,:] = rn16( scale * W[ids[i],:] ), and +0 where ids[i] == pad_id (pad_id < 0: no padding id).
+ * ids: n integers of id_bytes (4 or 8) bytes each, aligned to id_bytes; W16 [V,D] ldw >= D, Y16
+ * [n,D] ldy >= D.  A row whose id is neither the padding id nor in 0 .. V-1 becomes NaN, and
+ * state->status (state may be NULL) becomes MP_ERR_INVALID_ARG.  n = 0 is legal. */
+int mp_embedding_fwd(const void* ids, int id_bytes, const void* W16, int64_t ldw, void* Y16, int64_t ldy,
+                     int64_t n, int64_t V, int64_t D, int64_t pad_id, float scale, mp_state* state,
+                     void* stream);
+
+/* Gradient of the lookup: dW[v,:] = rn16( scale * sum_{i: ids[i] = v} dY[i,:] ) for every v of
+ * 0 .. V-1; rows of the padding id and of ids that do not occur become +0.  The tokens are sorted
+ * by id, in ascending i for each id, and the sums follow that order in FP32 (a long run of one id
+ * as the sums of its pieces, in order).  An id out of range adds to nothing and sets state->status as above.
+ * workspace: at least mp_embedding_bwd_workspace_bytes(n,V,D) bytes of device scratch, 16-byte
+ * aligned.  n and V below 2^31 - 1. */
+int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t lddy, void* dW16, int64_t ldw,
+                     int64_t n, int64_t V, int64_t D, int64_t pad_id, float scale, mp_state* state,
+                     void* workspace, size_t workspace_bytes, void* stream);
+size_t mp_embedding_bwd_workspace_bytes(int64_t n, int64_t V, int64_t D);
+
+/* Norms before and after a block, with the block's gate and the residual scale, for rows of D
+ * elements (1 .. MP_NORM_MAX_D).  With y the block's output:
+ *   h = norm(y) * g_post,   x_out = res_scale * x + gate * h,   n = norm(x_out) * g_pre
+ * norm(v) = v / sqrt(mean(v^2) + eps) for MP_NORM_RMS, (v - mean(v)) / sqrt(var(v) + eps) for
+ * MP_NORM_LAYER.  n, the next block's input, is formed from the FP32 x_out before its rounding.
+ * x, x_out: the residual stream, FP16 (x_bytes 2, pitch a multiple of 8) or FP32 (x_bytes 4, pitch
+ * a multiple of 4).  gate16: NULL (1), one vector of D for all rows (ldgate 0), or a matrix [M,D]
+ * (ldgate >= D).  stats (may be NULL): M records of four FP32 values, mean and 1/sqrt of y's norm
+ * and of x_out's (means 0 for MP_NORM_RMS), for the backward call.
+ * g_post16 NULL: the norm before the first block alone, n = norm(x) * g_pre; y16, x_out and gate16
+ * must be NULL, and the first two values of a record are 0.  M = 0 is legal.
+ * x_out may be x itself, n16 may be y16 itself (same pitch). */
+typedef enum { MP_NORM_RMS = 0, MP_NORM_LAYER = 1 } mp_norm_kind;
+#define MP_NORM_MAX_D 16384
+int mp_block_norm_fwd(int kind, float eps, float res_scale, const void* x, int x_bytes, int64_t ldx,
+                      const void* y16, int64_t ldy, const void* g_post16, const void* gate16, int64_t ldgate,
+                      void* x_out, int64_t ldxo, const void* g_pre16, void* n16, int64_t ldn, float* stats,
+                      int64_t M, int64_t D, void* stream);
+
+/* Backward of the call above, from the stored x_out, y and stats.  dn16: gradient at n; dx_out:
+ * gradient that reaches x_out from above (of x's type; NULL = none).  With xhat, yhat the normed rows:
+ *   gx = dx_out + d norm(x_out)/d x_out applied to dn * g_pre,   dx = res_scale * gx,
+ *   dy = d norm(y)/d y applied to gx * gate * g_post,
+ *   dg_pre = sum_rows dn * xhat,   dg_post = sum_rows gx * gate * yhat,
+ *   dgate = gx * h, summed over the rows for a gate vector, [M,D] (lddgate >= D) for a gate matrix.
+ * With g_post16 NULL: dx = gx, and y16, dy16, gate16, dg_post16, dgate16 must be NULL; dgate16 is
+ * NULL exactly when gate16 is.  dx may be dx_out itself, dy16 may be dn16 or y16 itself, a gate
+ * matrix's dgate16 may be gate16 itself (same pitch).  The gradients of the gains and of a gate
+ * vector are FP32 sums over the rows in a fixed order.  workspace: at least
+ * mp_block_norm_bwd_workspace_bytes(M,D) bytes, 16-byte aligned. */
+int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn, const void* dx_out,
+                      int64_t lddxo, const void* x_out, int x_bytes, int64_t ldxo, const void* y16, int64_t ldy,
+                      const void* g_post16, const void* gate16, int64_t ldgate, const void* g_pre16,
+                      const float* stats, void* dx, int64_t lddx, void* dy16, int64_t lddy, void* dg_post16,
+                      void* dgate16, int64_t lddgate, void* dg_pre16, int64_t M, int64_t D, mp_state* state,
+                      void* workspace, size_t workspace_bytes, void* stream);
+size_t mp_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
+
+/* Clipped policy loss with a KL term, forward and backward in one call.  For row i with logits z,
+ * target t and weight w:
+ *   lp = z_t - log sum_j exp(z_j),   r = exp(lp - old_logp),   d = ref_logp - lp
+ *   l  = -min( r A, clip(r, 1 - clip_lo, 1 + clip_hi) A ) + kl_coef (exp(d) - d - 1)
+ *   dz_j = rn16( grad_scale * S * w * dl/dlp * ([j = t] - exp(z_j) / sum exp(z)) )
+ * S: the loss scale of `state` (1 without a state).  Where r A equals its clipped value the gradient is
+ * that of r A.  logp[i] = lp, token_loss[i] = w l, loss[0] = sum_i token_loss[i] (fixed order; may be
+ * NULL).  A row of weight 0 is masked: nothing of it is read, its outputs are 0.  ref_logp NULL: no
+ * KL term.  A target outside 0 .. V-1 in a row that is not masked gives NaN for the row's outputs
+ * and sets state->status.  logits16 [N,V] ldl >= V, dlogits16 [N,V] lddl >= V; dlogits16 may be
+ * logits16 itself (same pitch), or NULL for the forward pass alone.  targets: N integers of id_bytes
+ * (4 or 8) bytes.  N = 0 is legal (loss 0). */
+typedef struct {
+  float clip_lo, clip_hi; /* 0 <= clip_lo, 0 <= clip_hi */
+  float kl_coef;
+  float grad_scale;
+} mp_policy_config;
+int mp_policy_loss(const void* logits16, int64_t ldl, const void* targets, int id_bytes, const float* old_logp,
+                   const float* ref_logp, const float* advantage, const float* weight, int64_t N, int64_t V,
+                   const mp_policy_config* cfg, void* dlogits16, int64_t lddl, float* logp, float* token_loss,
+                   float* loss, mp_state* state, void* stream);
+
+/* logp[i] = z_t - log sum_j exp(z_j): what the loss takes as old_logp and ref_logp.  weight: rows
+ * of weight 0 give 0 and are not read (NULL: every row counts).  Other arguments as above; without
+ * a state an id out of range shows as NaN alone. */
+int mp_token_logp(const void* logits16, int64_t ldl, const void* targets, int id_bytes, const float* weight,
+                  int64_t N, int64_t V, float* logp, mp_state* state, void* stream);
+
+/* AdamW (weight decay apart from the gradient) over the tensors of a plan, on the FP32 master, with
+ * the flag, S and t of `state` as in mp_master_update.  Per element, with g = float(g16) / S,
+ * c1 = 1 - beta1^t, c2 = 1 - beta2^t:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,   r = sqrt(v)
+ *   w = w - (lr weight_decay decay[i]) w,   w = w - (lr / c1) ( m / (r / sqrt(c2) + eps) ),   w16 = rn16(w)
+ * decay[i]: factor of tensor i (0 for the gains and biases that should not decay).
+ * state_bits 32: m[i], v[i] are FP32 buffers of count[i].  state_bits 8: m[i], v[i] are bytes that
+ * hold E4M3 numbers, of m and of r, each to be multiplied by the FP32 scale of its block of
+ * MP_ADAMW_BLOCK elements (m_scale[i], v_scale[i]: ceil(count[i] / MP_ADAMW_BLOCK) values); the
+ * block's scale is its largest magnitude / 448 (0 when that is below 2^-100: the block is stored as
+ * zeros).  r is kept instead of v because its range is half as many binades; an r above 0 is stored
+ * as at least the smallest number above 0, since a step by m / (0 + eps) would be far too long.
+ * All-zero buffers and scales are the initial state.  Errors as mp_update_plan_create and mp_master_update. */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* 1 - beta is formed in double before it is rounded */
+} mp_adamw_config;
+#define MP_ADAMW_BLOCK 256
+typedef struct mp_adamw_plan mp_adamw_plan;
+int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const* m, void* const* v,
+                         void* const* w16, const int64_t* count, const float* decay, int state_bits,
+                         float* const* m_scale, float* const* v_scale, mp_adamw_plan** out);
+int mp_adamw_plan_destroy(mp_adamw_plan* plan); /* NULL is accepted */
+int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config* opt, int check_mode,
+                    void* stream);
 
 /* ---- auxiliaries --------------------------------------------------------------------- */
 

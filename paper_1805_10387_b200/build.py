@@ -8,8 +8,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libmp_b200.so")
-SOURCES = ["update.cu", "gemm.cu", "lstm.cu"]
-HEADERS = ["common.h", "ptx.cuh", os.path.join(_ROOT, "include", "mp.h")]
+SOURCES = ["update.cu", "gemm.cu", "lstm.cu", "embedding.cu", "norm.cu", "loss.cu", "adamw.cu"]
+HEADERS = ["common.h", "ptx.cuh", "rows.cuh", os.path.join(_ROOT, "include", "mp.h")]
 
 
 def _stale() -> bool:
@@ -26,7 +26,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared",
+           "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared", "--threads", "0",
            "-I", os.path.join(_ROOT, "include"), "-I", CSRC]
     if verbose:
         cmd += ["-Xptxas", "-v"]

@@ -21,6 +21,9 @@ MP_OPT_ADAM, MP_OPT_MOMENTUM = 0, 1
 MP_OP_FWD, MP_OP_DGRAD, MP_OP_WGRAD = 0, 1, 2
 MP_LOG_CAPACITY = 4096
 MP_ACT_NONE, MP_ACT_RELU, MP_ACT_CLIPPED_RELU = 0, 1, 2
+MP_NORM_RMS, MP_NORM_LAYER = 0, 1
+MP_NORM_MAX_D = 16384
+MP_ADAMW_BLOCK = 256
 
 
 class MpError(RuntimeError):
@@ -48,13 +51,22 @@ class StateHost(C.Structure):
                 ("step", C.c_int64), ("skipped", C.c_int64)]
 
 
+class PolicyConfig(C.Structure):
+    _fields_ = [("clip_lo", C.c_float), ("clip_hi", C.c_float), ("kl_coef", C.c_float), ("grad_scale", C.c_float)]
+
+
+class AdamWConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double)]
+
+
 class LogRecord(C.Structure):
     _fields_ = [("step", C.c_int64), ("t", C.c_int64), ("scale_before", C.c_float),
                 ("scale_after", C.c_float), ("found_inf", C.c_int32), ("good_steps", C.c_int32)]
 
 
 # name -> (restype, argtypes): the declarations of include/mp.h
-_p, _i64, _i32, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_size_t
+_p, _i64, _i32, _sz, _f32 = C.c_void_p, C.c_int64, C.c_int, C.c_size_t, C.c_float
 SIGNATURES = {
     "mp_linear_fwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
     "mp_linear_bwd_dgrad": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _sz, _p]),
@@ -93,6 +105,22 @@ SIGNATURES = {
     "mp_update_plan_destroy": (_i32, [_p]),
     "mp_selftest_wait_timeout": (_i32, [_p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _i64, _p, _p]),
     "mp_gemm_device_status": (_i32, [C.POINTER(_i32)]),
+    "mp_embedding_fwd": (_i32, [_p, _i32, _p, _i64, _p, _i64, _i64, _i64, _i64, _i64, _f32, _p, _p]),
+    "mp_embedding_bwd": (_i32, [_p, _i32, _p, _i64, _p, _i64, _i64, _i64, _i64, _i64, _f32, _p, _p, _sz, _p]),
+    "mp_embedding_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "mp_block_norm_fwd": (_i32, [_i32, _f32, _f32, _p, _i32, _i64, _p, _i64, _p, _p, _i64, _p, _i64, _p, _p, _i64, _p,
+                                 _i64, _i64, _p]),
+    "mp_block_norm_bwd": (_i32, [_i32, _f32, _p, _i64, _p, _i64, _p, _i32, _i64, _p, _i64, _p, _p, _i64, _p, _p, _p,
+                                 _i64, _p, _i64, _p, _p, _i64, _p, _i64, _i64, _p, _p, _sz, _p]),
+    "mp_block_norm_bwd_workspace_bytes": (_sz, [_i64, _i64]),
+    "mp_policy_loss": (_i32, [_p, _i64, _p, _i32, _p, _p, _p, _p, _i64, _i64, C.POINTER(PolicyConfig), _p, _i64, _p, _p,
+                              _p, _p, _p]),
+    "mp_token_logp": (_i32, [_p, _i64, _p, _i32, _p, _i64, _i64, _p, _p, _p]),
+    "mp_adamw_plan_create": (_i32, [_i32, C.POINTER(_p), C.POINTER(_p), C.POINTER(_p), C.POINTER(_p), C.POINTER(_p),
+                                    C.POINTER(_i64), C.POINTER(_f32), _i32, C.POINTER(_p), C.POINTER(_p),
+                                    C.POINTER(_p)]),
+    "mp_adamw_plan_destroy": (_i32, [_p]),
+    "mp_adamw_update": (_i32, [_p, _p, C.POINTER(AdamWConfig), _i32, _p]),
     "mp_last_error": (C.c_char_p, []),
     "mp_kernel_launch_count": (_i64, []),
 }
@@ -337,6 +365,162 @@ def mp_check_finite(g16, state):
     _check(lib().mp_check_finite(_dev(g16, torch.float16), g16.numel(), state.handle, _stream()))
 
 
+# ---- operators of a token model ----
+
+def _ids(t):
+    """(pointer, bytes per id) of a contiguous vector of int32 or int64 ids."""
+    if not t.is_cuda or t.dtype not in (torch.int64, torch.int32) or t.dim() != 1 or not t.is_contiguous():
+        raise TypeError(f"expected a contiguous CUDA vector of int32 or int64, got {t.device} {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), t.element_size()
+
+
+def _vec(t, n, dtype):
+    """Pointer of a contiguous vector of n elements (None stays None)."""
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous vector of {n}, got {tuple(t.shape)}")
+    return _dev(t, dtype)
+
+
+def _rows(t, shape, dtypes):
+    """(pointer, pitch) of a row-major matrix of the given shape."""
+    if t.dim() != 2 or tuple(t.shape) != shape or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"expected a {shape} matrix with unit column stride, got {tuple(t.shape)}, {t.stride()}")
+    if not t.is_cuda or t.dtype not in dtypes:
+        raise TypeError(f"expected a CUDA tensor of {dtypes}, got {t.device} {t.dtype}")
+    if t.shape[0] > 1:
+        return t.data_ptr(), t.stride(0)
+    a = 16 // t.element_size()                       # the pitch of a single row does not matter
+    return t.data_ptr(), (t.shape[1] + a - 1) // a * a
+
+
+_F16, _X = (torch.float16,), (torch.float16, torch.float32)
+
+
+def _handle(state):
+    return state.handle if state is not None else None
+
+
+def mp_embedding_fwd(ids, W16, Y16, pad_id=-1, scale=1.0, state=None):
+    """Y16[i] = scale * W16[ids[i]]; zeros for pad_id (negative: none)."""
+    n, (V, D) = ids.shape[0], W16.shape
+    p, nb = _ids(ids)
+    (w, ldw), (y, ldy) = _rows(W16, (V, D), _F16), _rows(Y16, (n, D), _F16)
+    _check(lib().mp_embedding_fwd(p, nb, w, ldw, y, ldy, n, V, D, pad_id, scale, _handle(state), _stream()))
+
+
+def mp_embedding_bwd_workspace_bytes(n: int, V: int, D: int) -> int:
+    return int(lib().mp_embedding_bwd_workspace_bytes(n, V, D))
+
+
+def mp_embedding_bwd(ids, dY16, dW16, pad_id=-1, scale=1.0, state=None, workspace=None):
+    """dW16[v] = scale * sum of dY16[i] over the tokens i with ids[i] == v, for every row v."""
+    n, (V, D) = ids.shape[0], dW16.shape
+    p, nb = _ids(ids)
+    (dy, lddy), (dw, ldw) = _rows(dY16, (n, D), _F16), _rows(dW16, (V, D), _F16)
+    ws, size = _ws(workspace)
+    _check(lib().mp_embedding_bwd(p, nb, dy, lddy, dw, ldw, n, V, D, pad_id, scale, _handle(state), ws, size, _stream()))
+
+
+def _gate(gate16, M, D):
+    """(pointer, pitch) of a gate: none, a vector of D (pitch 0) or a matrix [M, D]."""
+    if gate16 is None:
+        return None, 0
+    return (_vec(gate16, D, torch.float16), 0) if gate16.dim() == 1 else _rows(gate16, (M, D), _F16)
+
+
+def _same(a, b, what):
+    if a.dtype != b.dtype:
+        raise TypeError(f"{what} must have one type, got {a.dtype} and {b.dtype}")
+
+
+def mp_block_norm_fwd(x, g_pre16, n16, stats=None, y16=None, g_post16=None, gate16=None, x_out=None, kind=MP_NORM_RMS,
+                      eps=1e-6, res_scale=1.0):
+    """x_out = res_scale * x + gate * norm(y) * g_post;  n = norm(x_out) * g_pre.  Without a block
+    (g_post16 None): n = norm(x) * g_pre.  x and x_out: FP16 or FP32."""
+    M, D = x.shape
+    (px, ldx), (pn, ldn) = _rows(x, (M, D), _X), _rows(n16, (M, D), _F16)
+    py, ldy, pxo, ldxo = None, 0, None, 0
+    if y16 is not None:
+        py, ldy = _rows(y16, (M, D), _F16)
+    if x_out is not None:
+        pxo, ldxo = _rows(x_out, (M, D), _X)
+        _same(x, x_out, "x and x_out")
+    pg, ldg = _gate(gate16, M, D)
+    if stats is not None and (tuple(stats.shape) != (M, 4) or not stats.is_contiguous()):
+        raise ValueError(f"expected contiguous stats [{M}, 4]")
+    _check(lib().mp_block_norm_fwd(kind, eps, res_scale, px, x.element_size(), ldx, py, ldy,
+                                   _vec(g_post16, D, torch.float16), pg, ldg, pxo, ldxo,
+                                   _vec(g_pre16, D, torch.float16), pn, ldn,
+                                   None if stats is None else _dev(stats, torch.float32), M, D, _stream()))
+
+
+def mp_block_norm_bwd_workspace_bytes(M: int, D: int) -> int:
+    return int(lib().mp_block_norm_bwd_workspace_bytes(M, D))
+
+
+def mp_block_norm_bwd(dn16, x_out, g_pre16, stats, dx, dg_pre16, dx_out=None, y16=None, g_post16=None, gate16=None,
+                      dy16=None, dg_post16=None, dgate16=None, kind=MP_NORM_RMS, res_scale=1.0, state=None,
+                      workspace=None):
+    """Backward of mp_block_norm_fwd; dx_out: the gradient that reaches x_out from above (None: none)."""
+    M, D = x_out.shape
+    (pdn, lddn), (px, ldx), (pdx, lddx) = _rows(dn16, (M, D), _F16), _rows(x_out, (M, D), _X), _rows(dx, (M, D), _X)
+    _same(x_out, dx, "x_out and dx")
+    pu, ldu, py, ldy, pdy, lddy = None, 0, None, 0, None, 0
+    if dx_out is not None:
+        pu, ldu = _rows(dx_out, (M, D), _X)
+        _same(x_out, dx_out, "x_out and dx_out")
+    if y16 is not None:
+        py, ldy = _rows(y16, (M, D), _F16)
+    if dy16 is not None:
+        pdy, lddy = _rows(dy16, (M, D), _F16)
+    pg, ldg = _gate(gate16, M, D)
+    pdg, lddg = _gate(dgate16, M, D)
+    if gate16 is not None and dgate16 is not None and gate16.dim() != dgate16.dim():
+        raise ValueError("dgate16 must have the form of gate16")
+    if tuple(stats.shape) != (M, 4) or not stats.is_contiguous():
+        raise ValueError(f"expected contiguous stats [{M}, 4]")
+    ws, size = _ws(workspace)
+    _check(lib().mp_block_norm_bwd(kind, res_scale, pdn, lddn, pu, ldu, px, x_out.element_size(), ldx, py, ldy,
+                                   _vec(g_post16, D, torch.float16), pg, ldg, _vec(g_pre16, D, torch.float16),
+                                   _dev(stats, torch.float32), pdx, lddx, pdy, lddy, _vec(dg_post16, D, torch.float16),
+                                   pdg, lddg, _vec(dg_pre16, D, torch.float16), M, D, _handle(state), ws, size,
+                                   _stream()))
+
+
+def mp_policy_loss(logits16, targets, old_logp, advantage, weight, logp, token_loss, loss=None, dlogits16=None,
+                   ref_logp=None, clip_lo=0.2, clip_hi=0.2, kl_coef=0.0, grad_scale=1.0, state=None):
+    """Clipped policy loss with a KL term: logp, token_loss [N] and loss [1] (FP32), and the gradient at the
+    logits times grad_scale and the loss scale of `state` (dlogits16 None: forward only)."""
+    N, V = logits16.shape
+    z, ldl = _rows(logits16, (N, V), _F16)
+    if targets.shape[0] != N:
+        raise ValueError(f"expected {N} targets, got {targets.shape[0]}")
+    t, nb = _ids(targets)
+    dz, lddl = (None, 0) if dlogits16 is None else _rows(dlogits16, (N, V), _F16)
+    cfg = PolicyConfig(clip_lo, clip_hi, kl_coef, grad_scale)
+    f = torch.float32
+    _check(lib().mp_policy_loss(z, ldl, t, nb, _vec(old_logp, N, f), _vec(ref_logp, N, f), _vec(advantage, N, f),
+                                _vec(weight, N, f), N, V, C.byref(cfg), dz, lddl, _vec(logp, N, f),
+                                _vec(token_loss, N, f), _vec(loss, 1, f), _handle(state), _stream()))
+
+
+def mp_token_logp(logits16, targets, logp, weight=None, state=None):
+    """logp[i] = log softmax(logits16[i])[targets[i]]; 0 where weight is 0."""
+    N, V = logits16.shape
+    z, ldl = _rows(logits16, (N, V), _F16)
+    if targets.shape[0] != N:
+        raise ValueError(f"expected {N} targets, got {targets.shape[0]}")
+    t, nb = _ids(targets)
+    _check(lib().mp_token_logp(z, ldl, t, nb, _vec(weight, N, torch.float32), N, V, _vec(logp, N, torch.float32),
+                               _handle(state), _stream()))
+
+
+def mp_adamw_update(plan, state, opt: AdamWConfig, check_mode: int = 0):
+    _check(lib().mp_adamw_update(plan.handle, state.handle, C.byref(opt), check_mode, _stream()))
+
+
 def mp_state_export_flag(state, word):
     """word[0] (int32 CUDA tensor) = the state's overflow flag, on the stream."""
     _check(lib().mp_state_export_flag(state.handle, _dev(word, torch.int32), _stream()))
@@ -421,6 +605,48 @@ class UpdatePlan:
     def close(self):
         if self.handle is not None and _lib is not None:
             _lib.mp_update_plan_destroy(self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamWPlan:
+    """Owner of an mp_adamw_plan handle.  m and v are FP32 tensors, or 8-bit ones (torch.float8_e4m3fn) with the
+    FP32 scales m_scale and v_scale, one value for each MP_ADAMW_BLOCK elements of a tensor.  decay: a factor
+    of the weight decay for each tensor (None: 1)."""
+
+    def __init__(self, g16, w32, m, v, w16, m_scale=None, v_scale=None, decay=None):
+        n = len(g16)
+        bits = 32 if m_scale is None and v_scale is None else 8
+        self._keep = (g16, w32, m, v, w16, m_scale, v_scale)
+        sizes = [t.numel() for t in g16]
+
+        def arr(ts, dtype, want):
+            if ts is None:
+                return None
+            if [t.numel() for t in ts] != want or not all(t.is_contiguous() for t in ts):
+                raise ValueError("the tensors of a plan must be contiguous and of matching sizes")
+            return (C.c_void_p * n)(*[_dev(t, dtype) if t.numel() else None for t in ts])
+        st = torch.float32 if bits == 32 else torch.float8_e4m3fn
+        blocks = [-(-k // MP_ADAMW_BLOCK) for k in sizes]
+        if decay is not None and len(decay) != n:
+            raise ValueError(f"expected {n} decay factors, got {len(decay)}")
+        h = C.c_void_p()
+        _check(lib().mp_adamw_plan_create(
+            n, arr(g16, torch.float16, sizes), arr(w32, torch.float32, sizes), arr(m, st, sizes), arr(v, st, sizes),
+            arr(w16, torch.float16, sizes), (C.c_int64 * n)(*sizes),
+            None if decay is None else (C.c_float * n)(*decay), bits, arr(m_scale, torch.float32, blocks),
+            arr(v_scale, torch.float32, blocks), C.byref(h)))
+        self.handle = h
+        self.total = sum(sizes)
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and _lib is not None:
+            _lib.mp_adamw_plan_destroy(self.handle)
         self.handle = None
 
     def __del__(self):
