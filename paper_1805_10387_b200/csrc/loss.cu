@@ -2,17 +2,19 @@
 
 #include <math.h>
 
+#include <map>
+#include <mutex>
+
+#include "ptx.cuh"
 #include "rows.cuh"
 
 namespace {
-
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 
 struct LossArgs {
   const uint16_t* z;
   int64_t ldl;
   const void* targets;
+  int id_bytes;
   const float *old_logp, *ref_logp, *advantage, *weight;
   int64_t N, V;
   float lo, hi, kl, grad_scale;
@@ -37,64 +39,391 @@ __device__ __forceinline__ void token_terms(const LossArgs& a, int64_t i, float 
   }
 }
 
-// One block per row, three passes over it.
-template <class ID, bool LOSS>
-__global__ void __launch_bounds__(kThreads) mp_policy_loss_kernel(const LossArgs a) {
-  __shared__ float red[kWarps];
+__device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t i) {
+  return a.id_bytes == 8 ? rows::load_id<int64_t>(a.targets, i) : rows::load_id<int32_t>(a.targets, i);
+}
+
+// ---- softmax statistics in powers of two ----
+//
+// exp(z) = 2^(z log2 e).  A partial sum over some of a row's logits is kept as s * 2^k with an INTEGER k near
+// the largest z log2 e of its part: z log2 e - k is then one fused operation with one rounding, and
+// partial sums are brought to a common k by exact powers of two.
+struct Sum2 {
+  float k, s;
+};
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kNegInf2 = 0xFC00FC00u;       // two FP16 -inf: what stands for words past the vocabulary
+
+__device__ __forceinline__ float ex2(float x) {   // 2 units in the last place; 0 below the normal range
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float k_of(float m) {   // a row part of -inf alone has s = 0 whatever its k
+  return m == -INFINITY ? 0.0f : rintf(m * kLog2e);
+}
+// Products and sums are rounded one by one, so that both sides of an exchange get the same bits.
+__device__ __forceinline__ Sum2 join(Sum2 x, Sum2 y) {
+  // a part without anything in it (s = 0) has no say in k
+  const float k = x.s == 0.0f ? y.k : y.s == 0.0f ? x.k : fmaxf(x.k, y.k);
+  const float a = x.s == 0.0f ? 0.0f : __fmul_rn(x.s, ex2(x.k - k)), b = y.s == 0.0f ? 0.0f : __fmul_rn(y.s, ex2(y.k - k));
+  return Sum2{k, __fadd_rn(a, b)};
+}
+template <int LANES>
+__device__ __forceinline__ Sum2 join_lanes(Sum2 v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1)
+    v = join(v, Sum2{__shfl_xor_sync(0xFFFFFFFFu, v.k, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)});
+  return v;
+}
+
+// Sum over the live words of C vectors of a thread.
+template <int C>
+__device__ __forceinline__ Sum2 thread_sum(const uint4 (&z)[C]) {
+  __half2 m2 = __half2half2(__ushort_as_half(0xFC00));
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m2 = __hmax2(m2, *reinterpret_cast<const __half2*>(&w[j]));
+  }
+  const float2 m = __half22float2(m2);
+  Sum2 v{k_of(fmaxf(m.x, m.y)), 0.0f};            // a NaN is lost here, and found again by the sum
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+      v.s += ex2(fmaf(f.x, kLog2e, -v.k)) + ex2(fmaf(f.y, kLog2e, -v.k));
+    }
+  }
+  return v;
+}
+
+// What a row's threads know once its sum is known: the row's outputs and the factors of its gradient.
+struct RowGrad {
+  float hot, cold;                                // dz_j = cold 2^(z_j log2 e - k), and hot more at the target
+};
+__device__ __forceinline__ RowGrad finish_row(const LossArgs& a, int64_t i, Sum2 v, int64_t t, float zt, float w, float S,
+                                              bool writer) {
+  const bool bad = t < 0 || t >= a.V;
+  const float lp = bad ? NAN : (fmaf(zt, kLog2e, -v.k) - log2f(v.s)) * kLn2;
+  float loss = 0.0f, dlp = 0.0f;
+  if (a.token_loss != nullptr) token_terms(a, i, lp, loss, dlp);
+  if (writer) {
+    if (bad) rows::record_bad_id(a.st);
+    a.logp[i] = lp;
+    if (a.token_loss != nullptr) a.token_loss[i] = w * loss;
+  }
+  const float c = a.grad_scale * S * w * dlp;
+  return RowGrad{c, -c / v.s};
+}
+// The gradient of eight words from column col on, and whether one of them is inf or NaN.
+__device__ __forceinline__ bool grad8(uint16_t* dz, const uint4& z, int nv, int64_t to_target, float k, RowGrad g) {
+  const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+    f[2 * j] = g.cold * ex2(fmaf(x.x, kLog2e, -k));
+    f[2 * j + 1] = g.cold * ex2(fmaf(x.y, kLog2e, -k));
+  }
+  if (to_target >= 0 && to_target < 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] += j == (int)to_target ? g.hot : 0.0f;
+  }
+  if (nv >= 8) {
+    const uint4 q = rows::pack8(f);
+    __stcs(reinterpret_cast<uint4*>(dz), q);
+    auto both = [](uint32_t v) { return __vcmpeq2(v & 0x7C007C00u, 0x7C007C00u); };
+    return (both(q.x) | both(q.y) | both(q.z) | both(q.w)) != 0;
+  }
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < nv) {
+      dz[j] = rows::f2h(f[j]);
+      bad |= rows::nonfinite16(dz[j]);
+    }
+  return bad;
+}
+__device__ __forceinline__ void zero8(uint16_t* dz, int nv) {
+  const float f[8] = {};
+  rows::store8(dz, f, nv);
+}
+// The first nv of eight words; -inf for the others.
+__device__ __forceinline__ uint4 live8(uint4 q, int nv) {
+  if (nv >= 8) return q;
+  uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = nv >= 2 * j + 2 ? w[j] : nv == 2 * j + 1 ? (w[j] & 0xFFFFu) | 0xFC000000u : kNegInf2;
+  return q;
+}
+
+// ---- rows of up to 8192 words: a group of TPR threads per row, the row in registers ----
+constexpr int kGroupThreads = 256;
+template <int TPR, int C>
+__global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(const LossArgs a) {
+  constexpr int G = kGroupThreads / TPR, W = TPR / 32;
+  __shared__ Sum2 s_part[G][W > 1 ? W : 1];
+  const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int64_t i = (int64_t)blockIdx.x * G + group;
+  const bool inside = i < a.N;
+  const float w = !inside ? 0.0f : a.weight ? a.weight[i] : 1.0f;
+  const bool live = w != 0.0f;
+  if (TPR >= 32 && !inside) return;
+  int nv[C];
+  uint4 z[C];
+  int64_t target = -1;
+  float zt = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int left = (int)a.V - (c * TPR + t) * 8;
+    nv[c] = !inside || left < 0 ? 0 : left < 8 ? left : 8;
+    z[c] = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+    if (live && nv[c] > 0)
+      z[c] = live8(__ldcs(reinterpret_cast<const uint4*>(a.z + i * a.ldl + (c * TPR + t) * 8)), nv[c]);
+  }
+  if (live) {
+    target = target_of(a, i);
+    if (target >= 0 && target < a.V) zt = rows::h2f(a.z[i * a.ldl + target]);
+  }
   const float S = a.st ? a.st->h.scale : 1.0f;
+  Sum2 v = join_lanes<(TPR < 32 ? TPR : 32)>(thread_sum<C>(z));
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 31) == 0) s_part[group][t >> 5] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
+    v = s_part[group][0];
+#pragma unroll
+    for (int x = 1; x < W; ++x) v = join(v, s_part[group][x]);
+  } else {
+    __syncwarp();                                  // every lane has read zt before dz may take its place
+  }
+  bool bad = false;
+  if (live) {
+    const RowGrad g = finish_row(a, i, v, target, zt, w, S, t == 0);
+    if (a.dz != nullptr)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = (c * TPR + t) * 8;
+        if (nv[c] > 0) bad |= grad8(a.dz + i * a.lddl + col, z[c], nv[c], target - col, v.k, g);
+      }
+  } else if (inside) {
+    if (t == 0) {
+      a.logp[i] = 0.0f;
+      if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
+    }
+    if (a.dz != nullptr)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (nv[c] > 0) zero8(a.dz + i * a.lddl + (c * TPR + t) * 8, nv[c]);
+  }
+  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
+}
+
+// ---- rows of up to 262144 words: CL blocks of a cluster per row, the row in their registers ----
+//
+// Persistent clusters.  While a row is worked on, each thread's asynchronous copies bring its own
+// vectors of the cluster's next row into its own slots of shared memory, so the loads never
+// stop; the blocks of a cluster exchange their partial sums through each other's shared memory, one
+// cluster barrier a row.
+constexpr int kRowThreads = 512;
+template <int C, int CL>
+__global__ void __launch_bounds__(kRowThreads, 2) mp_policy_loss_row_kernel(const LossArgs a) {
+  extern __shared__ uint4 slots[];                // [C][threads]
+  __shared__ Sum2 s_part[2][kRowThreads / 32];
+  __shared__ Sum2 s_block[2][CL];
+  const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0;
+  const int64_t step = gridDim.x / CL, first = blockIdx.x / CL;
+  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
+  const float S = a.st ? a.st->h.scale : 1.0f;
+  auto col_of = [&](int c) { return (int64_t)((c * CL + rank) * kRowThreads + (int)threadIdx.x) * 8; };
+  auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
+  auto fetch = [&](int64_t i, float w) {          // w: the weight of row i; a masked row is not read
+    if (w != 0.0f)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (col_of(c) < a.V)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + c * kRowThreads * 16),
+                       "l"(a.z + i * a.ldl + col_of(c)) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
+  float w = weight_of(first), w_next = weight_of(first + step);
+  fetch(first, w);
+  int parity = 0;
+  bool bad = false;
+  for (int64_t i = first; i < a.N; i += step) {
+    const float w_after = weight_of(i + 2 * step);
+    if (w != 0.0f) {
+      const int64_t target = target_of(a, i);
+      const float zt = target >= 0 && target < a.V ? rows::h2f(a.z[i * a.ldl + target]) : 0.0f;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      uint4 z[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int64_t left = a.V - col_of(c);
+        z[c] = left > 0 ? live8(slots[c * kRowThreads + threadIdx.x], left < 8 ? (int)left : 8)
+                        : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+      }
+      Sum2 v = thread_sum<C>(z);
+      fetch(i + step, w_next);                    // the slots have been read
+      v = join_lanes<32>(v);
+      if ((threadIdx.x & 31) == 0) s_part[parity][threadIdx.x >> 5] = v;
+      __syncthreads();
+      v = join_lanes<kRowThreads / 32>(s_part[parity][threadIdx.x & (kRowThreads / 32 - 1)]);
+      if constexpr (CL > 1) {
+        if (threadIdx.x < CL) {                   // thread r hands this block's sum to block r
+          const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_block[parity][rank]), threadIdx.x);
+          asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.k), "f"(v.s) : "memory");
+        }
+        ptx::cluster_sync();
+        v = s_block[parity][0];
+#pragma unroll
+        for (int r = 1; r < CL; ++r) v = join(v, s_block[parity][r]);
+      }
+      parity ^= 1;                                // the other half is free: its readers passed this barrier
+      const RowGrad g = finish_row(a, i, v, target, zt, w, S, threadIdx.x == 0 && rank == 0);
+      if (a.dz != nullptr)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int64_t col = col_of(c), left = a.V - col;
+          if (left > 0) bad |= grad8(a.dz + i * a.lddl + col, z[c], left < 8 ? (int)left : 8, target - col, v.k, g);
+        }
+    } else {
+      fetch(i + step, w_next);
+      if (threadIdx.x == 0 && rank == 0) {
+        a.logp[i] = 0.0f;
+        if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
+      }
+      if (a.dz != nullptr)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int64_t col = col_of(c), left = a.V - col;
+          if (left > 0) zero8(a.dz + i * a.lddl + col, left < 8 ? (int)left : 8);
+        }
+    }
+    w = w_next;
+    w_next = w_after;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
+}
+
+// ---- longer rows: one block per row, two passes over it, the second mostly from L2 ----
+__global__ void __launch_bounds__(kRowThreads) mp_policy_loss_long_kernel(const LossArgs a) {
+  __shared__ Sum2 s_part[kRowThreads / 32];
+  const float S = a.st ? a.st->h.scale : 1.0f;
+  bool bad = false;
   for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
     const uint16_t* z = a.z + i * a.ldl;
     uint16_t* dz = a.dz ? a.dz + i * a.lddl : nullptr;
     const float w = a.weight ? a.weight[i] : 1.0f;
     if (w == 0.0f) {
-      if (dz) for (int64_t j = threadIdx.x; j < a.V; j += kThreads) dz[j] = 0;
+      if (dz)
+        for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8)
+          zero8(dz + col, a.V - col < 8 ? (int)(a.V - col) : 8);
       if (threadIdx.x == 0) {
         a.logp[i] = 0.0f;
-        if (LOSS) a.token_loss[i] = 0.0f;
+        if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
       }
       continue;
     }
-    float m = -INFINITY;
-    for (int64_t j = threadIdx.x; j < a.V; j += kThreads) m = fmaxf(m, rows::h2f(z[j]));
-    m = rows::block_max<kWarps>(m, red);
-    if (isinf(m)) m = 0.0f;
-    float s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.V; j += kThreads) s += expf(rows::h2f(z[j]) - m);
-    s = rows::block_sum<kWarps>(s, red);
-    const int64_t t = rows::load_id<ID>(a.targets, i);
-    const bool bad = t < 0 || t >= a.V;
-    const float lp = bad ? NAN : (rows::h2f(z[t]) - m) - logf(s);
-    float loss = 0.0f, dlp = 0.0f;
-    if (LOSS) token_terms(a, i, lp, loss, dlp);
-    if (threadIdx.x == 0) {
-      if (bad) rows::record_bad_id(a.st);
-      a.logp[i] = lp;
-      if (LOSS) a.token_loss[i] = w * loss;
+    const int64_t target = target_of(a, i);
+    const float zt = target >= 0 && target < a.V ? rows::h2f(z[target]) : 0.0f;
+    Sum2 v{0.0f, 0.0f};
+    for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8) {
+      const uint4 q[1] = {live8(*reinterpret_cast<const uint4*>(z + col), a.V - col < 8 ? (int)(a.V - col) : 8)};
+      v = join(v, thread_sum<1>(q));
     }
-    if (dz) {
-      const float c = a.grad_scale * S * w * dlp, inv = 1.0f / s;
-      __syncthreads();                               // z[t] is read before dz may overwrite it
-      bool nonfinite = false;
-      for (int64_t j = threadIdx.x; j < a.V; j += kThreads) {
-        const uint16_t h = rows::f2h(c * ((j == t ? 1.0f : 0.0f) - expf(rows::h2f(z[j]) - m) * inv));
-        dz[j] = h;
-        nonfinite |= rows::nonfinite16(h);
+    v = join_lanes<32>(v);
+    __syncthreads();                               // the part sums of the row before have been read
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = join_lanes<kRowThreads / 32>(s_part[threadIdx.x & (kRowThreads / 32 - 1)]);
+    const RowGrad g = finish_row(a, i, v, target, zt, w, S, threadIdx.x == 0);
+    if (dz)
+      for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8) {
+        const int nv = a.V - col < 8 ? (int)(a.V - col) : 8;
+        bad |= grad8(dz + col, live8(*reinterpret_cast<const uint4*>(z + col), nv), nv, target - col, v.k, g);
       }
-      if (nonfinite && a.st) atomicOr(&a.st->h.found_inf, 1);
-    }
   }
+  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 
 // loss[0] = sum of the token losses, by one block in a fixed order.
-__global__ void __launch_bounds__(kThreads) mp_loss_sum_kernel(const float* token_loss, int64_t N, float* loss) {
-  __shared__ float red[kWarps];
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads) mp_loss_sum_kernel(const float* token_loss, int64_t N, float* loss) {
+  __shared__ float red[kSumThreads / 32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the token losses are complete and visible
   float s = 0.0f;
-  for (int64_t i = threadIdx.x; i < N; i += kThreads) s += token_loss[i];
-  s = rows::block_sum<kWarps>(s, red);
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < N; i += kSumThreads) s += token_loss[i];
+  s = rows::block_sum<kSumThreads / 32>(s, red);
   if (threadIdx.x == 0) loss[0] = s;
 }
 
-int launch(const char* name, const LossArgs& a, int id_bytes, float* loss, bool with_loss, void* stream) {
+template <int TPR, int C>
+void group_launch(const LossArgs& a, cudaStream_t st) {
+  constexpr int G = kGroupThreads / TPR;
+  mp_policy_loss_group_kernel<TPR, C><<<(unsigned)((a.N + G - 1) / G), kGroupThreads, 0, st>>>(a);
+}
+
+// Persistent grid of whole clusters, as many as are resident at once (asked once per device and kernel).
+template <int C, int CL>
+int row_launch(const LossArgs& a, cudaStream_t st) {
+  static std::mutex mu;
+  static std::map<int, int> resident;             // clusters of this kernel per device
+  const size_t smem = (size_t)C * kRowThreads * 16;
+  auto kernel = mp_policy_loss_row_kernel<C, CL>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kRowThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = CL;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int dev = 0, clusters = 0;
+  MP_CUDA_TRY(cudaGetDevice(&dev));
+  {
+    std::lock_guard<std::mutex> lock(mu);
+    int& have = resident[dev];
+    if (have == 0) {
+      MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      cfg.gridDim = dim3(CL * 148 * 2, 1, 1);
+      MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&have, kernel, &cfg));
+      if (have < 1) have = 1;
+    }
+    clusters = have;
+  }
+  if (a.N < clusters) clusters = (int)a.N;
+  cfg.gridDim = dim3((unsigned)(clusters * CL), 1, 1);
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+  return MP_OK;
+}
+
+int dispatch(const LossArgs& a, cudaStream_t st) {
+  if (a.V <= 32) group_launch<4, 1>(a, st);
+  else if (a.V <= 128) group_launch<8, 2>(a, st);
+  else if (a.V <= 512) group_launch<32, 2>(a, st);
+  else if (a.V <= 2048) group_launch<32, 8>(a, st);
+  else if (a.V <= 8192) group_launch<128, 8>(a, st);
+  else if (a.V <= 16384) return row_launch<4, 1>(a, st);
+  else if (a.V <= 32768) return row_launch<8, 1>(a, st);
+  else if (a.V <= 65536) return row_launch<8, 2>(a, st);
+  else if (a.V <= 131072) return row_launch<8, 4>(a, st);
+  else if (a.V <= 262144) return row_launch<8, 8>(a, st);
+  else mp_policy_loss_long_kernel<<<(unsigned)(a.N < 296 ? a.N : 296), kRowThreads, 0, st>>>(a);
+  return MP_OK;
+}
+
+int launch(const char* name, const LossArgs& a, float* loss, bool with_loss, void* stream) {
+  const int id_bytes = a.id_bytes;
   if (a.N < 0 || a.V <= 0 || a.ldl < a.V || (a.dz && a.lddl < a.V) || (id_bytes != 4 && id_bytes != 8))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: bad size, pitch or id width", name);
   if (a.N > 0 && (!a.z || !a.targets || !a.logp ||
@@ -109,21 +438,22 @@ int launch(const char* name, const LossArgs& a, int id_bytes, float* loss, bool 
   if (int rc = mp::check_device()) return rc;
   cudaStream_t st = (cudaStream_t)stream;
   if (a.N > 0) {
-    const int grid = (int)(a.N < 148 * 8 ? a.N : 148 * 8);
-    if (with_loss) {
-      if (id_bytes == 8) mp_policy_loss_kernel<int64_t, true><<<grid, kThreads, 0, st>>>(a);
-      else mp_policy_loss_kernel<int32_t, true><<<grid, kThreads, 0, st>>>(a);
-    } else {
-      if (id_bytes == 8) mp_policy_loss_kernel<int64_t, false><<<grid, kThreads, 0, st>>>(a);
-      else mp_policy_loss_kernel<int32_t, false><<<grid, kThreads, 0, st>>>(a);
-    }
+    if (int rc = dispatch(a, st)) return rc;
     mp::count_launch();
     MP_CUDA_TRY(cudaGetLastError());
   }
   if (loss) {
-    mp_loss_sum_kernel<<<1, kThreads, 0, st>>>(a.token_loss, a.N, loss);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1, 1, 1);
+    cfg.blockDim = dim3(kSumThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;            // resident early, waits on the device for the token losses
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_loss_sum_kernel, (const float*)a.token_loss, a.N, loss));
     mp::count_launch();
-    MP_CUDA_TRY(cudaGetLastError());
   }
   return MP_OK;
 }
@@ -139,17 +469,17 @@ int mp_policy_loss(const void* logits16, int64_t ldl, const void* targets, int i
   if (!cfg) return mp::set_error(MP_ERR_INVALID_ARG, "mp_policy_loss: null configuration");
   if (!(cfg->clip_lo >= 0.0f) || !(cfg->clip_hi >= 0.0f) || !isfinite(cfg->kl_coef) || !isfinite(cfg->grad_scale))
     return mp::set_error(MP_ERR_INVALID_ARG, "mp_policy_loss: bad configuration");
-  const LossArgs a{(const uint16_t*)logits16, ldl, targets, old_logp, ref_logp, advantage, weight, N, V,
+  const LossArgs a{(const uint16_t*)logits16, ldl, targets, id_bytes, old_logp, ref_logp, advantage, weight, N, V,
                    cfg->clip_lo, cfg->clip_hi, cfg->kl_coef, cfg->grad_scale, (uint16_t*)dlogits16, lddl, logp,
                    token_loss, state ? state->dev : nullptr};
-  return launch("mp_policy_loss", a, id_bytes, loss, true, stream);
+  return launch("mp_policy_loss", a, loss, true, stream);
 }
 
 int mp_token_logp(const void* logits16, int64_t ldl, const void* targets, int id_bytes, const float* weight,
                   int64_t N, int64_t V, float* logp, mp_state* state, void* stream) {
-  const LossArgs a{(const uint16_t*)logits16, ldl, targets, nullptr, nullptr, nullptr, weight, N, V,
+  const LossArgs a{(const uint16_t*)logits16, ldl, targets, id_bytes, nullptr, nullptr, nullptr, weight, N, V,
                    0.0f, 0.0f, 0.0f, 1.0f, nullptr, 0, logp, nullptr, state ? state->dev : nullptr};
-  return launch("mp_token_logp", a, id_bytes, nullptr, false, stream);
+  return launch("mp_token_logp", a, nullptr, false, stream);
 }
 
 }  // extern "C"
