@@ -49,9 +49,11 @@ __device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t i) {
 // the largest z log2 e of its part: z log2 e - k is then one fused operation with one rounding, and
 // partial sums are brought to a common k by exact powers of two.
 struct Sum2 {
-  float k, s;
+  int k;
+  float s;
 };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kNothing = -(1 << 20);             // k of a part of -inf alone: below every k that FP16 gives
 constexpr uint32_t kNegInf2 = 0xFC00FC00u;       // two FP16 -inf: what stands for words past the vocabulary
 
 __device__ __forceinline__ float ex2(float x) {   // 2 units in the last place; 0 below the normal range
@@ -59,25 +61,24 @@ __device__ __forceinline__ float ex2(float x) {   // 2 units in the last place; 
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float k_of(float m) {   // a row part of -inf alone has s = 0 whatever its k
-  return m == -INFINITY ? 0.0f : rintf(m * kLog2e);
-}
-// Products and sums are rounded one by one, so that both sides of an exchange get the same bits.
-__device__ __forceinline__ Sum2 join(Sum2 x, Sum2 y) {
-  // a part without anything in it (s = 0) has no say in k
-  const float k = x.s == 0.0f ? y.k : y.s == 0.0f ? x.k : fmaxf(x.k, y.k);
-  const float a = x.s == 0.0f ? 0.0f : __fmul_rn(x.s, ex2(x.k - k)), b = y.s == 0.0f ? 0.0f : __fmul_rn(y.s, ex2(y.k - k));
-  return Sum2{k, __fadd_rn(a, b)};
-}
+// Joins the sums of LANES neighbouring lanes; every lane gets the same bits.
 template <int LANES>
 __device__ __forceinline__ Sum2 join_lanes(Sum2 v) {
+  int k;
+  if constexpr (LANES == 32) {
+    k = __reduce_max_sync(0xFFFFFFFFu, v.k);
+  } else {
+    k = v.k;
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1)
-    v = join(v, Sum2{__shfl_xor_sync(0xFFFFFFFFu, v.k, o), __shfl_xor_sync(0xFFFFFFFFu, v.s, o)});
-  return v;
+    for (int o = LANES / 2; o > 0; o >>= 1) k = max(k, __shfl_xor_sync(0xFFFFFFFFu, k, o));
+  }
+  float s = v.s * ex2((float)(v.k - k));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  return Sum2{k, s};
 }
 
-// Sum over the live words of C vectors of a thread.
+// Sum over the words of C vectors of a thread.
 template <int C>
 __device__ __forceinline__ Sum2 thread_sum(const uint4 (&z)[C]) {
   __half2 m2 = __half2half2(__ushort_as_half(0xFC00));
@@ -88,27 +89,36 @@ __device__ __forceinline__ Sum2 thread_sum(const uint4 (&z)[C]) {
     for (int j = 0; j < 4; ++j) m2 = __hmax2(m2, *reinterpret_cast<const __half2*>(&w[j]));
   }
   const float2 m = __half22float2(m2);
-  Sum2 v{k_of(fmaxf(m.x, m.y)), 0.0f};            // a NaN is lost here, and found again by the sum
+  const float top = fmaxf(m.x, m.y);              // a NaN is lost here, and found again by the sum
+  const float k = top == -INFINITY ? (float)kNothing : rintf(top * kLog2e);
+  float s = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-      v.s += ex2(fmaf(f.x, kLog2e, -v.k)) + ex2(fmaf(f.y, kLog2e, -v.k));
+      s += ex2(fmaf(f.x, kLog2e, -k));
+      s += ex2(fmaf(f.y, kLog2e, -k));
     }
   }
-  return v;
+  // a logit of +inf leaves no distribution: inf - inf above made the sum a NaN
+  return Sum2{top == INFINITY ? 0 : (int)k, s};
 }
 
-// What a row's threads know once its sum is known: the row's outputs and the factors of its gradient.
+// What a row's threads need to form its gradient: dz_j = cold 2^(z_j log2 e - k), and `hot` more at the
+// target.  Every |dz_j| is at most |hot| (a probability is at most 1), so unless `check` is set nothing that
+// is stored can be inf or NaN and nobody looks.
 struct RowGrad {
-  float hot, cold;                                // dz_j = cold 2^(z_j log2 e - k), and hot more at the target
+  float k, hot, cold, at_target;
+  int check;
 };
+// Finishes a row's sums: its outputs (by `writer`) and the factors of its gradient.
 __device__ __forceinline__ RowGrad finish_row(const LossArgs& a, int64_t i, Sum2 v, int64_t t, float zt, float w, float S,
                                               bool writer) {
   const bool bad = t < 0 || t >= a.V;
-  const float lp = bad ? NAN : (fmaf(zt, kLog2e, -v.k) - log2f(v.s)) * kLn2;
+  const float k = (float)v.k, up = fmaf(zt, kLog2e, -k);
+  const float lp = bad ? NAN : (up - log2f(v.s)) * kLn2;
   float loss = 0.0f, dlp = 0.0f;
   if (a.token_loss != nullptr) token_terms(a, i, lp, loss, dlp);
   if (writer) {
@@ -116,41 +126,52 @@ __device__ __forceinline__ RowGrad finish_row(const LossArgs& a, int64_t i, Sum2
     a.logp[i] = lp;
     if (a.token_loss != nullptr) a.token_loss[i] = w * loss;
   }
-  const float c = a.grad_scale * S * w * dlp;
-  return RowGrad{c, -c / v.s};
+  const float c = a.grad_scale * S * w * dlp, cold = -c / v.s;
+  return RowGrad{k, c, cold, fmaf(cold, ex2(up), c), !(fabsf(c) < 65000.0f) || !(fabsf(cold) <= 3.0e38f)};
 }
-// The gradient of eight words from column col on, and whether one of them is inf or NaN.
-__device__ __forceinline__ bool grad8(uint16_t* dz, const uint4& z, int nv, int64_t to_target, float k, RowGrad g) {
+__device__ __forceinline__ uint4 grad8(const uint4& z, const RowGrad& g) {
   const uint32_t w[4] = {z.x, z.y, z.z, z.w};
   float f[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-    f[2 * j] = g.cold * ex2(fmaf(x.x, kLog2e, -k));
-    f[2 * j + 1] = g.cold * ex2(fmaf(x.y, kLog2e, -k));
+    f[2 * j] = g.cold * ex2(fmaf(x.x, kLog2e, -g.k));
+    f[2 * j + 1] = g.cold * ex2(fmaf(x.y, kLog2e, -g.k));
   }
-  if (to_target >= 0 && to_target < 8) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] += j == (int)to_target ? g.hot : 0.0f;
-  }
+  return rows::pack8(f);
+}
+__device__ __forceinline__ void store_words(uint16_t* dz, const uint4& q, int nv) {   // the first nv of eight words
   if (nv >= 8) {
-    const uint4 q = rows::pack8(f);
     __stcs(reinterpret_cast<uint4*>(dz), q);
-    auto both = [](uint32_t v) { return __vcmpeq2(v & 0x7C007C00u, 0x7C007C00u); };
-    return (both(q.x) | both(q.y) | both(q.z) | both(q.w)) != 0;
+    return;
   }
-  bool bad = false;
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
   for (int j = 0; j < 8; ++j)
-    if (j < nv) {
-      dz[j] = rows::f2h(f[j]);
-      bad |= rows::nonfinite16(dz[j]);
-    }
+    if (j < nv) dz[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+}
+__device__ __forceinline__ bool nonfinite8(const uint4& q, int nv) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bad |= j < nv && rows::nonfinite16((uint16_t)(w[j / 2] >> (16 * (j & 1))));
   return bad;
 }
-__device__ __forceinline__ void zero8(uint16_t* dz, int nv) {
-  const float f[8] = {};
-  rows::store8(dz, f, nv);
+// The gradient of the nv live words of a vector, `dz` its place.
+__device__ __forceinline__ bool put_grad(uint16_t* dz, const uint4& z, int nv, const RowGrad& g) {
+  const uint4 q = grad8(z, g);
+  store_words(dz, q, nv);
+  return g.check ? nonfinite8(q, nv) : false;
+}
+// Then the target's word, by the thread that has just stored the vector with it.
+__device__ __forceinline__ bool put_target(uint16_t* dz, const RowGrad& g) {
+  const uint16_t h = rows::f2h(g.at_target);
+  *dz = h;
+  return rows::nonfinite16(h);
+}
+__device__ __forceinline__ void masked_outputs(const LossArgs& a, int64_t i) {
+  a.logp[i] = 0.0f;
+  if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
 }
 // The first nv of eight words; -inf for the others.
 __device__ __forceinline__ uint4 live8(uint4 q, int nv) {
@@ -161,6 +182,7 @@ __device__ __forceinline__ uint4 live8(uint4 q, int nv) {
     w[j] = nv >= 2 * j + 2 ? w[j] : nv == 2 * j + 1 ? (w[j] & 0xFFFFu) | 0xFC000000u : kNegInf2;
   return q;
 }
+__device__ __forceinline__ uint4 no_words() { return make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2); }
 
 // ---- rows of up to 8192 words: a group of TPR threads per row, the row in registers ----
 constexpr int kGroupThreads = 256;
@@ -171,9 +193,9 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const int64_t i = (int64_t)blockIdx.x * G + group;
   const bool inside = i < a.N;
+  if (TPR >= 32 && !inside) return;
   const float w = !inside ? 0.0f : a.weight ? a.weight[i] : 1.0f;
   const bool live = w != 0.0f;
-  if (TPR >= 32 && !inside) return;
   int nv[C];
   uint4 z[C];
   int64_t target = -1;
@@ -182,7 +204,7 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   for (int c = 0; c < C; ++c) {
     const int left = (int)a.V - (c * TPR + t) * 8;
     nv[c] = !inside || left < 0 ? 0 : left < 8 ? left : 8;
-    z[c] = make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+    z[c] = no_words();
     if (live && nv[c] > 0)
       z[c] = live8(__ldcs(reinterpret_cast<const uint4*>(a.z + i * a.ldl + (c * TPR + t) * 8)), nv[c]);
   }
@@ -195,116 +217,148 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   if constexpr (W > 1) {
     if ((threadIdx.x & 31) == 0) s_part[group][t >> 5] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
-    v = s_part[group][0];
-#pragma unroll
-    for (int x = 1; x < W; ++x) v = join(v, s_part[group][x]);
+    v = join_lanes<W>(s_part[group][threadIdx.x & (W - 1)]);
   } else {
     __syncwarp();                                  // every lane has read zt before dz may take its place
   }
   bool bad = false;
   if (live) {
     const RowGrad g = finish_row(a, i, v, target, zt, w, S, t == 0);
-    if (a.dz != nullptr)
+    if (a.dz != nullptr) {
+      uint16_t* dz = a.dz + i * a.lddl;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int col = (c * TPR + t) * 8;
-        if (nv[c] > 0) bad |= grad8(a.dz + i * a.lddl + col, z[c], nv[c], target - col, v.k, g);
+        if (nv[c] > 0) bad |= put_grad(dz + col, z[c], nv[c], g);
       }
-  } else if (inside) {
-    if (t == 0) {
-      a.logp[i] = 0.0f;
-      if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
+      if (target >= 0 && target < a.V && (int)(target / 8) % TPR == t) bad |= put_target(dz + target, g);
     }
+  } else if (inside) {
+    if (t == 0) masked_outputs(a, i);
     if (a.dz != nullptr)
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (nv[c] > 0) zero8(a.dz + i * a.lddl + (c * TPR + t) * 8, nv[c]);
+        if (nv[c] > 0) store_words(a.dz + i * a.lddl + (c * TPR + t) * 8, make_uint4(0, 0, 0, 0), nv[c]);
   }
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 
-// ---- rows of up to 262144 words: CL blocks of a cluster per row, the row in their registers ----
+// ---- rows of up to 262144 words: CL blocks of a cluster per row, the row in their shared memory ----
 //
-// Persistent clusters.  While a row is worked on, each thread's asynchronous copies bring its own
-// vectors of the cluster's next row into its own slots of shared memory, so the loads never
-// stop; the blocks of a cluster exchange their partial sums through each other's shared memory, one
-// cluster barrier a row.
-constexpr int kRowThreads = 512;
+// Persistent clusters.  512 workers of a block hold up to 32768 words of a row, each thread its own vectors, which
+// its own asynchronous copies bring into its own slots; three stages of slots, so that while row i is
+// summed and row i - 1 gets its gradient, row i + 1 is on its way.  One more warp joins the partial
+// sums of row i and works out the token's loss and the factors of the gradient while the workers
+// are busy with the gradient of row i - 1; one block barrier a row is all that they share.  The
+// blocks of a cluster hand their sums to each other's shared memory; the workers arrive at the
+// cluster's barrier before a row's gradient and wait for it after.
+// (Before: workers that held the row in registers and waited for its factors, two blocks an SM:
+// 258 us for 8192 x 32768.)
+constexpr int kWorkers = 512, kWorkerWarps = kWorkers / 32, kRowThreads = kWorkers + 32, kStages = 3;
 template <int C, int CL>
-__global__ void __launch_bounds__(kRowThreads, 2) mp_policy_loss_row_kernel(const LossArgs a) {
-  extern __shared__ uint4 slots[];                // [C][threads]
-  __shared__ Sum2 s_part[2][kRowThreads / 32];
+__global__ void __launch_bounds__(kRowThreads, C > 4 ? 1 : 2) mp_policy_loss_row_kernel(const LossArgs a) {
+  extern __shared__ uint4 slots[];                // [stage][C][workers]
+  __shared__ Sum2 s_part[2][kWorkerWarps];
   __shared__ Sum2 s_block[2][CL];
-  const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0;
+  __shared__ RowGrad s_grad[2];
+  const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0, lane = threadIdx.x & 31;
   const int64_t step = gridDim.x / CL, first = blockIdx.x / CL;
-  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
-  const float S = a.st ? a.st->h.scale : 1.0f;
-  auto col_of = [&](int c) { return (int64_t)((c * CL + rank) * kRowThreads + (int)threadIdx.x) * 8; };
+  const int V = (int)a.V;
   auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
-  auto fetch = [&](int64_t i, float w) {          // w: the weight of row i; a masked row is not read
-    if (w != 0.0f)
+  auto arrive = [] { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); };
+  auto wait = [] { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+  if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
+  if (threadIdx.x >= kWorkers) {
+    const float S = a.st ? a.st->h.scale : 1.0f;
+    int half = 0;
+    for (int64_t i = first; i - step < a.N; i += step, half ^= 1) {
+      const float w = weight_of(i);
+      int64_t target = 0;
+      float zt = 0.0f;
+      if (w != 0.0f) {
+        target = target_of(a, i);
+        if (target >= 0 && target < V) zt = rows::h2f(a.z[i * a.ldl + target]);
+      }
+      __syncthreads();                            // the workers' sums of row i are there
+      Sum2 v{kNothing, 0.0f};
+      if (w != 0.0f) v = join_lanes<kWorkerWarps>(s_part[half][lane & (kWorkerWarps - 1)]);
+      if constexpr (CL > 1) {
+        if (lane < CL) {                          // lane r hands this block's sum to block r
+          const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_block[half][rank]), lane);
+          asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(v.k), "r"(__float_as_int(v.s)) : "memory");
+        }
+        __syncwarp();
+        arrive();
+        wait();
+        v = join_lanes<CL>(s_block[half][lane & (CL - 1)]);
+      }
+      if (w != 0.0f) {
+        const RowGrad g = finish_row(a, i, v, target, zt, w, S, lane == 0 && rank == 0);
+        if (lane == 0) s_grad[half] = g;
+      } else if (i < a.N && lane == 0 && rank == 0) {
+        masked_outputs(a, i);
+      }
+    }
+    return;
+  }
+  const int mine = rank * kWorkers + (int)threadIdx.x;    // vector c of this thread: mine + c CL workers
+  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
+  auto left_of = [&](int c) { return V - (mine + c * (CL * kWorkers)) * 8; };     // words from the vector's first on
+  auto fetch = [&](int64_t i, float w, int stage) {       // w: the weight of row i; a masked row is not read
+    if (w != 0.0f) {
+      const uint16_t* z = a.z + i * a.ldl + mine * 8;
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (col_of(c) < a.V)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + c * kRowThreads * 16),
-                       "l"(a.z + i * a.ldl + col_of(c)) : "memory");
+        if (left_of(c) > 0)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + (stage * C + c) * kWorkers * 16),
+                       "l"(z + c * (CL * kWorkers * 8)) : "memory");
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
-  float w = weight_of(first), w_next = weight_of(first + step);
-  fetch(first, w);
-  int parity = 0;
+  float w_before = 0.0f, w = weight_of(first), w_next = weight_of(first + step);
+  fetch(first, w, 0);
+  int stage = 0, half = 0;
   bool bad = false;
-  for (int64_t i = first; i < a.N; i += step) {
+  for (int64_t i = first; i - step < a.N; i += step, half ^= 1) {
     const float w_after = weight_of(i + 2 * step);
+    const int next = stage == kStages - 1 ? 0 : stage + 1, before = stage == 0 ? kStages - 1 : stage - 1;
+    fetch(i + step, w_next, next);                // that stage held row i - 2, whose gradient is stored
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
     if (w != 0.0f) {
-      const int64_t target = target_of(a, i);
-      const float zt = target >= 0 && target < a.V ? rows::h2f(a.z[i * a.ldl + target]) : 0.0f;
-      asm volatile("cp.async.wait_all;" ::: "memory");
       uint4 z[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int64_t left = a.V - col_of(c);
-        z[c] = left > 0 ? live8(slots[c * kRowThreads + threadIdx.x], left < 8 ? (int)left : 8)
-                        : make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2);
+        const int left = left_of(c);
+        z[c] = left > 0 ? slots[(stage * C + c) * kWorkers + threadIdx.x] : no_words();
+        if (left > 0 && left < 8) z[c] = live8(z[c], left);
       }
-      Sum2 v = thread_sum<C>(z);
-      fetch(i + step, w_next);                    // the slots have been read
-      v = join_lanes<32>(v);
-      if ((threadIdx.x & 31) == 0) s_part[parity][threadIdx.x >> 5] = v;
-      __syncthreads();
-      v = join_lanes<kRowThreads / 32>(s_part[parity][threadIdx.x & (kRowThreads / 32 - 1)]);
-      if constexpr (CL > 1) {
-        if (threadIdx.x < CL) {                   // thread r hands this block's sum to block r
-          const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_block[parity][rank]), threadIdx.x);
-          asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.k), "f"(v.s) : "memory");
-        }
-        ptx::cluster_sync();
-        v = s_block[parity][0];
-#pragma unroll
-        for (int r = 1; r < CL; ++r) v = join(v, s_block[parity][r]);
-      }
-      parity ^= 1;                                // the other half is free: its readers passed this barrier
-      const RowGrad g = finish_row(a, i, v, target, zt, w, S, threadIdx.x == 0 && rank == 0);
-      if (a.dz != nullptr)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int64_t col = col_of(c), left = a.V - col;
-          if (left > 0) bad |= grad8(a.dz + i * a.lddl + col, z[c], left < 8 ? (int)left : 8, target - col, v.k, g);
-        }
-    } else {
-      fetch(i + step, w_next);
-      if (threadIdx.x == 0 && rank == 0) {
-        a.logp[i] = 0.0f;
-        if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
-      }
-      if (a.dz != nullptr)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int64_t col = col_of(c), left = a.V - col;
-          if (left > 0) zero8(a.dz + i * a.lddl + col, left < 8 ? (int)left : 8);
-        }
+      const Sum2 v = join_lanes<32>(thread_sum<C>(z));
+      if (lane == 0) s_part[half][threadIdx.x >> 5] = v;
     }
+    __syncthreads();
+    if constexpr (CL > 1) arrive();
+    const int64_t b = i - step;                   // the row before gets its gradient
+    if (b >= first && a.dz != nullptr) {
+      uint16_t* dz = a.dz + b * a.lddl + mine * 8;
+      if (w_before != 0.0f) {
+        const RowGrad g = s_grad[half ^ 1];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int left = left_of(c);
+          if (left > 0) bad |= put_grad(dz + c * (CL * kWorkers * 8), slots[(before * C + c) * kWorkers + threadIdx.x], left, g);
+        }
+        const int64_t target = target_of(a, b);
+        if (target >= 0 && target < V && (int)(target >> 3) % (CL * kWorkers) == mine)
+          bad |= put_target(a.dz + b * a.lddl + target, g);
+      } else {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (left_of(c) > 0) store_words(dz + c * (CL * kWorkers * 8), make_uint4(0, 0, 0, 0), left_of(c));
+      }
+    }
+    if constexpr (CL > 1) wait();
+    stage = next;
+    w_before = w;
     w = w_next;
     w_next = w_after;
   }
@@ -313,42 +367,46 @@ __global__ void __launch_bounds__(kRowThreads, 2) mp_policy_loss_row_kernel(cons
 }
 
 // ---- longer rows: one block per row, two passes over it, the second mostly from L2 ----
-__global__ void __launch_bounds__(kRowThreads) mp_policy_loss_long_kernel(const LossArgs a) {
-  __shared__ Sum2 s_part[kRowThreads / 32];
+constexpr int kLongThreads = 512, kLongWarps = kLongThreads / 32;
+__global__ void __launch_bounds__(kLongThreads) mp_policy_loss_long_kernel(const LossArgs a) {
+  __shared__ Sum2 s_part[kLongWarps];
   const float S = a.st ? a.st->h.scale : 1.0f;
   bool bad = false;
   for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
     const uint16_t* z = a.z + i * a.ldl;
     uint16_t* dz = a.dz ? a.dz + i * a.lddl : nullptr;
     const float w = a.weight ? a.weight[i] : 1.0f;
+    auto left_of = [&](int64_t col) { return a.V - col < 8 ? (int)(a.V - col) : 8; };
     if (w == 0.0f) {
       if (dz)
-        for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8)
-          zero8(dz + col, a.V - col < 8 ? (int)(a.V - col) : 8);
-      if (threadIdx.x == 0) {
-        a.logp[i] = 0.0f;
-        if (a.token_loss != nullptr) a.token_loss[i] = 0.0f;
-      }
+        for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8)
+          store_words(dz + col, make_uint4(0, 0, 0, 0), left_of(col));
+      if (threadIdx.x == 0) masked_outputs(a, i);
       continue;
     }
     const int64_t target = target_of(a, i);
-    const float zt = target >= 0 && target < a.V ? rows::h2f(z[target]) : 0.0f;
-    Sum2 v{0.0f, 0.0f};
-    for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8) {
-      const uint4 q[1] = {live8(*reinterpret_cast<const uint4*>(z + col), a.V - col < 8 ? (int)(a.V - col) : 8)};
-      v = join(v, thread_sum<1>(q));
+    const bool good = target >= 0 && target < a.V;
+    const float zt = good ? rows::h2f(z[target]) : 0.0f;
+    Sum2 v{kNothing, 0.0f};
+    for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8) {
+      const uint4 q[1] = {live8(*reinterpret_cast<const uint4*>(z + col), left_of(col))};
+      const Sum2 x = thread_sum<1>(q);
+      const int k = max(v.k, x.k);
+      v = Sum2{k, v.s * ex2((float)(v.k - k)) + x.s * ex2((float)(x.k - k))};
     }
     v = join_lanes<32>(v);
     __syncthreads();                               // the part sums of the row before have been read
     if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = join_lanes<kRowThreads / 32>(s_part[threadIdx.x & (kRowThreads / 32 - 1)]);
+    v = join_lanes<kLongWarps>(s_part[threadIdx.x & (kLongWarps - 1)]);
     const RowGrad g = finish_row(a, i, v, target, zt, w, S, threadIdx.x == 0);
-    if (dz)
-      for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kRowThreads * 8) {
-        const int nv = a.V - col < 8 ? (int)(a.V - col) : 8;
-        bad |= grad8(dz + col, live8(*reinterpret_cast<const uint4*>(z + col), nv), nv, target - col, v.k, g);
+    if (dz) {
+      for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8) {
+        const int nv = left_of(col);
+        bad |= put_grad(dz + col, live8(*reinterpret_cast<const uint4*>(z + col), nv), nv, g);
       }
+      if (good && (int)((target >> 3) % kLongThreads) == (int)threadIdx.x) bad |= put_target(dz + target, g);
+    }
   }
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
@@ -376,7 +434,7 @@ template <int C, int CL>
 int row_launch(const LossArgs& a, cudaStream_t st) {
   static std::mutex mu;
   static std::map<int, int> resident;             // clusters of this kernel per device
-  const size_t smem = (size_t)C * kRowThreads * 16;
+  const size_t smem = (size_t)kStages * C * kWorkers * 16;
   auto kernel = mp_policy_loss_row_kernel<C, CL>;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kRowThreads, 1, 1);
@@ -418,7 +476,7 @@ int dispatch(const LossArgs& a, cudaStream_t st) {
   else if (a.V <= 65536) return row_launch<8, 2>(a, st);
   else if (a.V <= 131072) return row_launch<8, 4>(a, st);
   else if (a.V <= 262144) return row_launch<8, 8>(a, st);
-  else mp_policy_loss_long_kernel<<<(unsigned)(a.N < 296 ? a.N : 296), kRowThreads, 0, st>>>(a);
+  else mp_policy_loss_long_kernel<<<(unsigned)(a.N < 296 ? a.N : 296), kLongThreads, 0, st>>>(a);
   return MP_OK;
 }
 
