@@ -353,7 +353,8 @@ size_t mp_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
  * KL term.  A target outside 0 .. V-1 in a row that is not masked gives NaN for the row's outputs
  * and sets state->status.  logits16 [N,V] ldl >= V, dlogits16 [N,V] lddl >= V; dlogits16 may be
  * logits16 itself (same pitch), or NULL for the forward pass alone.  targets: N integers of id_bytes
- * (4 or 8) bytes.  N = 0 is legal (loss 0). */
+ * (4 or 8) bytes.  N = 0 is legal (loss 0).  V is at most MP_POLICY_MAX_V. */
+#define MP_POLICY_MAX_V 524288
 typedef struct {
   float clip_lo, clip_hi; /* 0 <= clip_lo, 0 <= clip_hi */
   float kl_coef;

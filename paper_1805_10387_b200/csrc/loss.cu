@@ -4,6 +4,7 @@
 
 #include <map>
 #include <mutex>
+#include <utility>
 
 #include "ptx.cuh"
 #include "rows.cuh"
@@ -25,22 +26,43 @@ struct LossArgs {
 };
 
 // Loss of one token and its derivative by the token's log-probability.
-__device__ __forceinline__ void token_terms(const LossArgs& a, int64_t i, float lp, float& loss, float& dlp) {
-  const float A = a.advantage[i];
-  const float r = expf(lp - a.old_logp[i]);
+struct Token {
+  float w, zt, old_logp, ref_logp, advantage;     // zt: the target's logit
+  int target;                                     // -1: out of range
+};
+__device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t i) {
+  return a.id_bytes == 8 ? rows::load_id<int64_t>(a.targets, i) : rows::load_id<int32_t>(a.targets, i);
+}
+// What row i has besides its logits; of a masked row (weight 0) and past the last one nothing is read.
+__device__ __forceinline__ Token load_token(const LossArgs& a, int64_t i) {
+  Token t{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, -1};
+  if (i >= a.N) return t;
+  t.w = a.weight ? a.weight[i] : 1.0f;
+  if (t.w == 0.0f) return t;
+  const int64_t id = target_of(a, i);
+  if (a.token_loss != nullptr) {
+    t.old_logp = a.old_logp[i];
+    t.advantage = a.advantage[i];
+    if (a.ref_logp) t.ref_logp = a.ref_logp[i];
+  }
+  if (id >= 0 && id < a.V) {
+    t.target = (int)id;
+    t.zt = rows::h2f(a.z[i * a.ldl + id]);
+  }
+  return t;
+}
+__device__ __forceinline__ void token_terms(const LossArgs& a, const Token& t, float lp, float& loss, float& dlp) {
+  const float A = t.advantage;
+  const float r = expf(lp - t.old_logp);
   const float plain = r * A, clipped = fminf(fmaxf(r, 1.0f - a.lo), 1.0f + a.hi) * A;
   loss = plain <= clipped ? -plain : -clipped;
   dlp = plain <= clipped ? -plain : 0.0f;
   if (plain != plain) loss = dlp = plain;          // a NaN shows in the loss and the gradient
   if (a.ref_logp) {
-    const float d = a.ref_logp[i] - lp, e = expm1f(d);
+    const float d = t.ref_logp - lp, e = expm1f(d);
     loss += a.kl * (e - d);
     dlp -= a.kl * e;
   }
-}
-
-__device__ __forceinline__ int64_t target_of(const LossArgs& a, int64_t i) {
-  return a.id_bytes == 8 ? rows::load_id<int64_t>(a.targets, i) : rows::load_id<int32_t>(a.targets, i);
 }
 
 // ---- softmax statistics in powers of two ----
@@ -78,32 +100,65 @@ __device__ __forceinline__ Sum2 join_lanes(Sum2 v) {
   return Sum2{k, s};
 }
 
+// A thread's largest word, vector by vector, and the k that goes with it.
+__device__ __forceinline__ __half2 max8(__half2 m2, const uint4& z) {
+  const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m2 = __hmax2(m2, *reinterpret_cast<const __half2*>(&w[j]));
+  return m2;
+}
+struct Top {
+  float k;
+  bool infinite;
+};
+__device__ __forceinline__ Top top_of(__half2 m2) {
+  const float2 m = __half22float2(m2);
+  const float top = fmaxf(m.x, m.y);              // a NaN is lost here, and found again by the sum
+  return Top{top == -INFINITY ? (float)kNothing : rintf(top * kLog2e), top == INFINITY};
+}
+__device__ __forceinline__ float sum8(const uint4& z, float k) {
+  const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
+    s[0] += ex2(fmaf(f.x, kLog2e, -k));
+    s[1] += ex2(fmaf(f.y, kLog2e, -k));
+  }
+  return s[0] + s[1];
+}
+// A logit of +inf leaves no distribution: inf - inf made the sum a NaN.
+__device__ __forceinline__ Sum2 sum_of(Top t, float s) { return Sum2{t.infinite ? 0 : (int)t.k, s}; }
+// The sum over a thread's words in one pass: k follows the first vector's largest word and is raised only
+// when a word passes it by 2^64, so almost no vector pays for a change.
+struct Running {
+  float k = 0.0f, s = 0.0f;
+  bool begun = false, infinite = false;
+  __device__ __forceinline__ void add(const uint4& z) {
+    const float2 m = __half22float2(max8(__half2half2(__ushort_as_half(0xFC00)), z));
+    const float top = fmaxf(m.x, m.y);
+    if (!begun || fmaf(top, kLog2e, -k) > 64.0f) {
+      const float up = top == -INFINITY ? (float)kNothing : rintf(top * kLog2e);
+      s = begun ? s * ex2(k - up) : 0.0f;
+      k = up;
+      begun = true;
+      infinite |= top == INFINITY;
+    }
+    s += sum8(z, k);
+  }
+  __device__ __forceinline__ Sum2 sum() const { return begun ? Sum2{infinite ? 0 : (int)k, s} : Sum2{kNothing, 0.0f}; }
+};
 // Sum over the words of C vectors of a thread.
 template <int C>
 __device__ __forceinline__ Sum2 thread_sum(const uint4 (&z)[C]) {
   __half2 m2 = __half2half2(__ushort_as_half(0xFC00));
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m2 = __hmax2(m2, *reinterpret_cast<const __half2*>(&w[j]));
-  }
-  const float2 m = __half22float2(m2);
-  const float top = fmaxf(m.x, m.y);              // a NaN is lost here, and found again by the sum
-  const float k = top == -INFINITY ? (float)kNothing : rintf(top * kLog2e);
+  for (int c = 0; c < C; ++c) m2 = max8(m2, z[c]);
+  const Top t = top_of(m2);
   float s = 0.0f;
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-      s += ex2(fmaf(f.x, kLog2e, -k));
-      s += ex2(fmaf(f.y, kLog2e, -k));
-    }
-  }
-  // a logit of +inf leaves no distribution: inf - inf above made the sum a NaN
-  return Sum2{top == INFINITY ? 0 : (int)k, s};
+  for (int c = 0; c < C; ++c) s += sum8(z[c], t.k);
+  return sum_of(t, s);
 }
 
 // What a row's threads need to form its gradient: dz_j = cold 2^(z_j log2 e - k), and `hot` more at the
@@ -111,23 +166,21 @@ __device__ __forceinline__ Sum2 thread_sum(const uint4 (&z)[C]) {
 // is stored can be inf or NaN and nobody looks.
 struct RowGrad {
   float k, hot, cold, at_target;
-  int check;
+  int target, check;
 };
 // Finishes a row's sums: its outputs (by `writer`) and the factors of its gradient.
-__device__ __forceinline__ RowGrad finish_row(const LossArgs& a, int64_t i, Sum2 v, int64_t t, float zt, float w, float S,
-                                              bool writer) {
-  const bool bad = t < 0 || t >= a.V;
-  const float k = (float)v.k, up = fmaf(zt, kLog2e, -k);
-  const float lp = bad ? NAN : (up - log2f(v.s)) * kLn2;
+__device__ __forceinline__ RowGrad finish_row(const LossArgs& a, int64_t i, Sum2 v, const Token& t, float S, bool writer) {
+  const float k = (float)v.k, up = fmaf(t.zt, kLog2e, -k);
+  const float lp = t.target < 0 ? NAN : (up - log2f(v.s)) * kLn2;
   float loss = 0.0f, dlp = 0.0f;
-  if (a.token_loss != nullptr) token_terms(a, i, lp, loss, dlp);
+  if (a.token_loss != nullptr) token_terms(a, t, lp, loss, dlp);
   if (writer) {
-    if (bad) rows::record_bad_id(a.st);
+    if (t.target < 0) rows::record_bad_id(a.st);
     a.logp[i] = lp;
-    if (a.token_loss != nullptr) a.token_loss[i] = w * loss;
+    if (a.token_loss != nullptr) a.token_loss[i] = t.w * loss;
   }
-  const float c = a.grad_scale * S * w * dlp, cold = -c / v.s;
-  return RowGrad{k, c, cold, fmaf(cold, ex2(up), c), !(fabsf(c) < 65000.0f) || !(fabsf(cold) <= 3.0e38f)};
+  const float c = a.grad_scale * S * t.w * dlp, cold = -c / v.s;
+  return RowGrad{k, c, cold, fmaf(cold, ex2(up), c), t.target, !(fabsf(c) < 65000.0f) || !(fabsf(cold) <= 3.0e38f)};
 }
 __device__ __forceinline__ uint4 grad8(const uint4& z, const RowGrad& g) {
   const uint32_t w[4] = {z.x, z.y, z.z, z.w};
@@ -194,12 +247,10 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   const int64_t i = (int64_t)blockIdx.x * G + group;
   const bool inside = i < a.N;
   if (TPR >= 32 && !inside) return;
-  const float w = !inside ? 0.0f : a.weight ? a.weight[i] : 1.0f;
-  const bool live = w != 0.0f;
+  const Token tok = load_token(a, i);
+  const bool live = tok.w != 0.0f;
   int nv[C];
   uint4 z[C];
-  int64_t target = -1;
-  float zt = 0.0f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int left = (int)a.V - (c * TPR + t) * 8;
@@ -208,10 +259,6 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
     if (live && nv[c] > 0)
       z[c] = live8(__ldcs(reinterpret_cast<const uint4*>(a.z + i * a.ldl + (c * TPR + t) * 8)), nv[c]);
   }
-  if (live) {
-    target = target_of(a, i);
-    if (target >= 0 && target < a.V) zt = rows::h2f(a.z[i * a.ldl + target]);
-  }
   const float S = a.st ? a.st->h.scale : 1.0f;
   Sum2 v = join_lanes<(TPR < 32 ? TPR : 32)>(thread_sum<C>(z));
   if constexpr (W > 1) {
@@ -219,11 +266,11 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
     asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
     v = join_lanes<W>(s_part[group][threadIdx.x & (W - 1)]);
   } else {
-    __syncwarp();                                  // every lane has read zt before dz may take its place
+    __syncwarp();                                  // every lane has read its token's logit before dz may take its place
   }
   bool bad = false;
   if (live) {
-    const RowGrad g = finish_row(a, i, v, target, zt, w, S, t == 0);
+    const RowGrad g = finish_row(a, i, v, tok, S, t == 0);
     if (a.dz != nullptr) {
       uint16_t* dz = a.dz + i * a.lddl;
 #pragma unroll
@@ -231,7 +278,7 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
         const int col = (c * TPR + t) * 8;
         if (nv[c] > 0) bad |= put_grad(dz + col, z[c], nv[c], g);
       }
-      if (target >= 0 && target < a.V && (int)(target / 8) % TPR == t) bad |= put_target(dz + target, g);
+      if (g.target >= 0 && (g.target / 8) % TPR == t) bad |= put_target(dz + g.target, g);
     }
   } else if (inside) {
     if (t == 0) masked_outputs(a, i);
@@ -243,170 +290,125 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 
-// ---- rows of up to 262144 words: CL blocks of a cluster per row, the row in their shared memory ----
+// ---- rows of more than 8192 words: CL blocks of a cluster per row, the row in their shared memory ----
 //
-// Persistent clusters.  512 workers of a block hold up to 32768 words of a row, each thread its own vectors, which
-// its own asynchronous copies bring into its own slots; three stages of slots, so that while row i is
-// summed and row i - 1 gets its gradient, row i + 1 is on its way.  One more warp joins the partial
-// sums of row i and works out the token's loss and the factors of the gradient while the workers
-// are busy with the gradient of row i - 1; one block barrier a row is all that they share.  The
-// blocks of a cluster hand their sums to each other's shared memory; the workers arrive at the
-// cluster's barrier before a row's gradient and wait for it after.
-// (Before: workers that held the row in registers and waited for its factors, two blocks an SM:
-// 258 us for 8192 x 32768.)
-constexpr int kWorkers = 512, kWorkerWarps = kWorkers / 32, kRowThreads = kWorkers + 32, kStages = 3;
-template <int C, int CL>
-__global__ void __launch_bounds__(kRowThreads, C > 4 ? 1 : 2) mp_policy_loss_row_kernel(const LossArgs a) {
-  extern __shared__ uint4 slots[];                // [stage][C][workers]
-  __shared__ Sum2 s_part[2][kWorkerWarps];
+// Persistent clusters, several blocks an SM: while one block sums a row or writes its gradient, the
+// others' rows are on their way.  A block holds its part of a row, each thread its own vectors, which its own
+// asynchronous copies bring into its own slots of shared memory; a slot is filled again with the
+// next row's vector as soon as its gradient is formed.  One warp joins the partial sums and works out
+// the token's loss and the factors of the gradient for all.  The blocks of a cluster hand their sums
+// to each other's shared memory.
+// Small blocks: with 128 threads and at most 32 KiB of a row (up to six blocks an SM) the blocks drift
+// apart and the loads of some cover the arithmetic of others.  8192 x 32768 with 128 threads and 32 KiB
+// 189 us, 64 KiB 195, 16 KiB 223; 256 threads and 64 KiB 206; 512 threads 209; one block of 1024 threads
+// with rows fetched two ahead 221.
+constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
+constexpr int kPartWords = 16 * kRowThreads * 8;  // words of a row that a block takes if a cluster of 8 can
+template <int CL>
+__global__ void __launch_bounds__(kRowThreads, 6) mp_policy_loss_row_kernel(const LossArgs a) {
+  extern __shared__ uint4 slots[];                // [vectors]
+  __shared__ Sum2 s_part[2][kRowWarps];
   __shared__ Sum2 s_block[2][CL];
   __shared__ RowGrad s_grad[2];
   const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0, lane = threadIdx.x & 31;
   const int64_t step = gridDim.x / CL, first = blockIdx.x / CL;
-  const int V = (int)a.V;
+  const int V = (int)a.V, mine = rank * kRowThreads + (int)threadIdx.x;    // vector c of this thread: mine + c CL threads
+  // this thread's whole vectors, and the words of one more that ends the row (most threads have none)
+  const int rest = V / 8 - mine, whole = rest <= 0 ? 0 : (rest + CL * kRowThreads - 1) / (CL * kRowThreads);
+  const int tail = rest >= 0 && rest % (CL * kRowThreads) == 0 ? V % 8 : 0;
+  constexpr int kHop = CL * kRowThreads * 8;      // words from one vector of a thread to its next
+  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
+  const uint4* z = slots + threadIdx.x;
+  const float S = a.st ? a.st->h.scale : 1.0f;
   auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
-  auto arrive = [] { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); };
-  auto wait = [] { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); };
+  auto copy = [&](const uint16_t* from, int c) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + c * kRowThreads * 16), "l"(from + c * kHop) : "memory");
+  };
+  auto fetch = [&](int64_t i) {
+    const uint16_t* from = a.z + i * a.ldl + mine * 8;
+    for (int c = 0; c < whole + (tail > 0); ++c) copy(from, c);
+  };
   if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
-  if (threadIdx.x >= kWorkers) {
-    const float S = a.st ? a.st->h.scale : 1.0f;
-    int half = 0;
-    for (int64_t i = first; i - step < a.N; i += step, half ^= 1) {
-      const float w = weight_of(i);
-      int64_t target = 0;
-      float zt = 0.0f;
-      if (w != 0.0f) {
-        target = target_of(a, i);
-        if (target >= 0 && target < V) zt = rows::h2f(a.z[i * a.ldl + target]);
+  float w = weight_of(first);
+  if (w != 0.0f) fetch(first);                    // a masked row is not read
+  Token ahead{};                                  // first warp, lane l: what the l-th row from the last load on has
+  int half = 0, turn = 0;
+  bool bad = false;
+  for (int64_t i = first; i < a.N; i += step, turn = (turn + 1) & 31) {
+    // the loads of a token depend on one another (weight, target, its logit): 32 rows at a time
+    if (threadIdx.x < 32 && turn == 0) ahead = load_token(a, i + lane * step);
+    const float w_next = weight_of(i + step);
+    const bool more = w_next != 0.0f;
+    const uint16_t* from = a.z + (i + step) * a.ldl + mine * 8;
+    uint16_t* dz = a.dz ? a.dz + i * a.lddl + mine * 8 : nullptr;
+    if (w == 0.0f) {
+      if (threadIdx.x == 0 && rank == 0) masked_outputs(a, i);
+      if (dz != nullptr) {
+        for (int c = 0; c < whole; ++c) __stcs(reinterpret_cast<uint4*>(dz + c * kHop), make_uint4(0, 0, 0, 0));
+        if (tail > 0) store_words(dz + whole * kHop, make_uint4(0, 0, 0, 0), tail);
       }
-      __syncthreads();                            // the workers' sums of row i are there
-      Sum2 v{kNothing, 0.0f};
-      if (w != 0.0f) v = join_lanes<kWorkerWarps>(s_part[half][lane & (kWorkerWarps - 1)]);
-      if constexpr (CL > 1) {
+      if (more) fetch(i + step);
+      w = w_next;
+      continue;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    Running r;
+#pragma unroll 4
+    for (int c = 0; c < whole; ++c) r.add(z[c * kRowThreads]);
+    uint4 last = no_words();
+    if (tail > 0) {
+      last = live8(z[whole * kRowThreads], tail);
+      r.add(last);
+    }
+    Sum2 v = join_lanes<32>(r.sum());
+    if (lane == 0) s_part[half][threadIdx.x >> 5] = v;
+    __syncthreads();
+    if constexpr (CL > 1) {
+      if (threadIdx.x < 32) {
+        v = join_lanes<kRowWarps>(s_part[half][lane & (kRowWarps - 1)]);
         if (lane < CL) {                          // lane r hands this block's sum to block r
           const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_block[half][rank]), lane);
           asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(v.k), "r"(__float_as_int(v.s)) : "memory");
         }
         __syncwarp();
-        arrive();
-        wait();
-        v = join_lanes<CL>(s_block[half][lane & (CL - 1)]);
       }
-      if (w != 0.0f) {
-        const RowGrad g = finish_row(a, i, v, target, zt, w, S, lane == 0 && rank == 0);
-        if (lane == 0) s_grad[half] = g;
-      } else if (i < a.N && lane == 0 && rank == 0) {
-        masked_outputs(a, i);
-      }
+      ptx::cluster_sync();
     }
-    return;
-  }
-  const int mine = rank * kWorkers + (int)threadIdx.x;    // vector c of this thread: mine + c CL workers
-  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
-  auto left_of = [&](int c) { return V - (mine + c * (CL * kWorkers)) * 8; };     // words from the vector's first on
-  auto fetch = [&](int64_t i, float w, int stage) {       // w: the weight of row i; a masked row is not read
-    if (w != 0.0f) {
-      const uint16_t* z = a.z + i * a.ldl + mine * 8;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (left_of(c) > 0)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + (stage * C + c) * kWorkers * 16),
-                       "l"(z + c * (CL * kWorkers * 8)) : "memory");
+    if (threadIdx.x < 32) {
+      if constexpr (CL > 1) v = join_lanes<CL>(s_block[half][lane & (CL - 1)]);
+      else v = join_lanes<kRowWarps>(s_part[half][lane & (kRowWarps - 1)]);
+      auto of = [&](float x) { return __shfl_sync(0xFFFFFFFFu, x, turn); };
+      const Token t{w, of(ahead.zt), of(ahead.old_logp), of(ahead.ref_logp), of(ahead.advantage),
+                    __shfl_sync(0xFFFFFFFFu, ahead.target, turn)};
+      const RowGrad g = finish_row(a, i, v, t, S, lane == 0 && rank == 0);
+      if (lane == 0) s_grad[half] = g;
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  float w_before = 0.0f, w = weight_of(first), w_next = weight_of(first + step);
-  fetch(first, w, 0);
-  int stage = 0, half = 0;
-  bool bad = false;
-  for (int64_t i = first; i - step < a.N; i += step, half ^= 1) {
-    const float w_after = weight_of(i + 2 * step);
-    const int next = stage == kStages - 1 ? 0 : stage + 1, before = stage == 0 ? kStages - 1 : stage - 1;
-    fetch(i + step, w_next, next);                // that stage held row i - 2, whose gradient is stored
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    if (w != 0.0f) {
-      uint4 z[C];
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int left = left_of(c);
-        z[c] = left > 0 ? slots[(stage * C + c) * kWorkers + threadIdx.x] : no_words();
-        if (left > 0 && left < 8) z[c] = live8(z[c], left);
-      }
-      const Sum2 v = join_lanes<32>(thread_sum<C>(z));
-      if (lane == 0) s_part[half][threadIdx.x >> 5] = v;
-    }
-    __syncthreads();
-    if constexpr (CL > 1) arrive();
-    const int64_t b = i - step;                   // the row before gets its gradient
-    if (b >= first && a.dz != nullptr) {
-      uint16_t* dz = a.dz + b * a.lddl + mine * 8;
-      if (w_before != 0.0f) {
-        const RowGrad g = s_grad[half ^ 1];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int left = left_of(c);
-          if (left > 0) bad |= put_grad(dz + c * (CL * kWorkers * 8), slots[(before * C + c) * kWorkers + threadIdx.x], left, g);
+    if (dz != nullptr) {
+      __syncthreads();
+      const RowGrad g = s_grad[half];
+      if (!g.check) {
+#pragma unroll 4
+        for (int c = 0; c < whole; ++c) {
+          const uint4 q = grad8(z[c * kRowThreads], g);
+          if (more) copy(from, c);                // the slot has been read
+          __stcs(reinterpret_cast<uint4*>(dz + c * kHop), q);
         }
-        const int64_t target = target_of(a, b);
-        if (target >= 0 && target < V && (int)(target >> 3) % (CL * kWorkers) == mine)
-          bad |= put_target(a.dz + b * a.lddl + target, g);
       } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (left_of(c) > 0) store_words(dz + c * (CL * kWorkers * 8), make_uint4(0, 0, 0, 0), left_of(c));
+        for (int c = 0; c < whole; ++c) {
+          bad |= put_grad(dz + c * kHop, z[c * kRowThreads], 8, g);
+          if (more) copy(from, c);
+        }
       }
+      if (tail > 0) {
+        bad |= put_grad(dz + whole * kHop, last, tail, g);
+        if (more) copy(from, whole);
+      }
+      if (g.target >= 0 && (g.target >> 3) % (CL * kRowThreads) == mine) bad |= put_target(a.dz + i * a.lddl + g.target, g);
+    } else if (more) {
+      fetch(i + step);
     }
-    if constexpr (CL > 1) wait();
-    stage = next;
-    w_before = w;
+    half ^= 1;                                    // a thread that gets back to this half has passed the next row's barrier
     w = w_next;
-    w_next = w_after;
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
-}
-
-// ---- longer rows: one block per row, two passes over it, the second mostly from L2 ----
-constexpr int kLongThreads = 512, kLongWarps = kLongThreads / 32;
-__global__ void __launch_bounds__(kLongThreads) mp_policy_loss_long_kernel(const LossArgs a) {
-  __shared__ Sum2 s_part[kLongWarps];
-  const float S = a.st ? a.st->h.scale : 1.0f;
-  bool bad = false;
-  for (int64_t i = blockIdx.x; i < a.N; i += gridDim.x) {
-    const uint16_t* z = a.z + i * a.ldl;
-    uint16_t* dz = a.dz ? a.dz + i * a.lddl : nullptr;
-    const float w = a.weight ? a.weight[i] : 1.0f;
-    auto left_of = [&](int64_t col) { return a.V - col < 8 ? (int)(a.V - col) : 8; };
-    if (w == 0.0f) {
-      if (dz)
-        for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8)
-          store_words(dz + col, make_uint4(0, 0, 0, 0), left_of(col));
-      if (threadIdx.x == 0) masked_outputs(a, i);
-      continue;
-    }
-    const int64_t target = target_of(a, i);
-    const bool good = target >= 0 && target < a.V;
-    const float zt = good ? rows::h2f(z[target]) : 0.0f;
-    Sum2 v{kNothing, 0.0f};
-    for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8) {
-      const uint4 q[1] = {live8(*reinterpret_cast<const uint4*>(z + col), left_of(col))};
-      const Sum2 x = thread_sum<1>(q);
-      const int k = max(v.k, x.k);
-      v = Sum2{k, v.s * ex2((float)(v.k - k)) + x.s * ex2((float)(x.k - k))};
-    }
-    v = join_lanes<32>(v);
-    __syncthreads();                               // the part sums of the row before have been read
-    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = join_lanes<kLongWarps>(s_part[threadIdx.x & (kLongWarps - 1)]);
-    const RowGrad g = finish_row(a, i, v, target, zt, w, S, threadIdx.x == 0);
-    if (dz) {
-      for (int64_t col = (int64_t)threadIdx.x * 8; col < a.V; col += kLongThreads * 8) {
-        const int nv = left_of(col);
-        bad |= put_grad(dz + col, live8(*reinterpret_cast<const uint4*>(z + col), nv), nv, g);
-      }
-      if (good && (int)((target >> 3) % kLongThreads) == (int)threadIdx.x) bad |= put_target(dz + target, g);
-    }
   }
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
@@ -429,13 +431,15 @@ void group_launch(const LossArgs& a, cudaStream_t st) {
   mp_policy_loss_group_kernel<TPR, C><<<(unsigned)((a.N + G - 1) / G), kGroupThreads, 0, st>>>(a);
 }
 
-// Persistent grid of whole clusters, as many as are resident at once (asked once per device and kernel).
-template <int C, int CL>
+// Persistent grid of whole clusters, as many as are resident at once (asked once per device, kernel and
+// size of a block's part of a row).
+template <int CL>
 int row_launch(const LossArgs& a, cudaStream_t st) {
   static std::mutex mu;
-  static std::map<int, int> resident;             // clusters of this kernel per device
-  const size_t smem = (size_t)kStages * C * kWorkers * 16;
-  auto kernel = mp_policy_loss_row_kernel<C, CL>;
+  static std::map<std::pair<int, int>, int> resident;
+  const int64_t vecs = (a.V + 7) / 8, layers = (vecs + CL * kRowThreads - 1) / (CL * kRowThreads);
+  const int smem = (int)layers * kRowThreads * 16;
+  auto kernel = mp_policy_loss_row_kernel<CL>;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kRowThreads, 1, 1);
   cfg.dynamicSmemBytes = smem;
@@ -450,10 +454,11 @@ int row_launch(const LossArgs& a, cudaStream_t st) {
   MP_CUDA_TRY(cudaGetDevice(&dev));
   {
     std::lock_guard<std::mutex> lock(mu);
-    int& have = resident[dev];
+    int& have = resident[{dev, smem}];
     if (have == 0) {
-      MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-      cfg.gridDim = dim3(CL * 148 * 2, 1, 1);
+      MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       MP_POLICY_MAX_V / 8 * 2));
+      cfg.gridDim = dim3(CL * 148 * 16, 1, 1);
       MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&have, kernel, &cfg));
       if (have < 1) have = 1;
     }
@@ -471,12 +476,10 @@ int dispatch(const LossArgs& a, cudaStream_t st) {
   else if (a.V <= 512) group_launch<32, 2>(a, st);
   else if (a.V <= 2048) group_launch<32, 8>(a, st);
   else if (a.V <= 8192) group_launch<128, 8>(a, st);
-  else if (a.V <= 16384) return row_launch<4, 1>(a, st);
-  else if (a.V <= 32768) return row_launch<8, 1>(a, st);
-  else if (a.V <= 65536) return row_launch<8, 2>(a, st);
-  else if (a.V <= 131072) return row_launch<8, 4>(a, st);
-  else if (a.V <= 262144) return row_launch<8, 8>(a, st);
-  else mp_policy_loss_long_kernel<<<(unsigned)(a.N < 296 ? a.N : 296), kLongThreads, 0, st>>>(a);
+  else if (a.V <= kPartWords) return row_launch<1>(a, st);
+  else if (a.V <= 2 * kPartWords) return row_launch<2>(a, st);
+  else if (a.V <= 4 * kPartWords) return row_launch<4>(a, st);
+  else return row_launch<8>(a, st);
   return MP_OK;
 }
 
@@ -484,6 +487,7 @@ int launch(const char* name, const LossArgs& a, float* loss, bool with_loss, voi
   const int id_bytes = a.id_bytes;
   if (a.N < 0 || a.V <= 0 || a.ldl < a.V || (a.dz && a.lddl < a.V) || (id_bytes != 4 && id_bytes != 8))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: bad size, pitch or id width", name);
+  if (a.V > MP_POLICY_MAX_V) return mp::set_error(MP_ERR_TOO_LARGE, "%s: V beyond %d", name, MP_POLICY_MAX_V);
   if (a.N > 0 && (!a.z || !a.targets || !a.logp ||
                   (with_loss && (!a.old_logp || !a.advantage || !a.weight || !a.token_loss))))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: null pointer", name);

@@ -115,6 +115,8 @@ def test_policy_loss_refusals(p16):
     for name in ("z", "t", "old", "adv", "w", "lp", "tl"):
         assert _loss(L, p16, **{name: None}) == INV
     assert _loss(L, p16, N=-1) == INV and _loss(L, p16, V=0) == INV and _loss(L, p16, idb=3) == INV
+    big = 524288 + 8
+    assert _loss(L, p16, V=big, ldl=big, lddl=big) == LARGE
     assert _loss(L, p16, ldl=4) == INV and _loss(L, p16, lddl=4) == INV
     assert _loss(L, p16, ldl=12) == ALIGN and _loss(L, p16, lddl=12) == ALIGN
     assert _loss(L, p16, z=p16 + 2) == ALIGN and _loss(L, p16, t=p16 + 4) == ALIGN and _loss(L, p16, adv=p16 + 2) == ALIGN
