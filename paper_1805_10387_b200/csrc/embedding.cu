@@ -1,73 +1,396 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 
 #include <climits>
+#include <map>
+#include <mutex>
 
+#include "ptx.cuh"
 #include "rows.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr uint16_t kNan16 = 0x7FFFu;
+// ---------------------------------------------------------------- lookup
+//
+// A warp's worth of work is 32 vectors of 8 elements in a row or in neighbouring rows: n D 16-byte loads
+// and stores with nothing but a multiplication between them.
+constexpr int kFwdThreads = 256;
+constexpr uint32_t kNan2 = 0x7FFF7FFFu;
 
-template <class ID>
-__global__ void __launch_bounds__(kThreads)
-mp_embedding_fwd_kernel(const void* ids, const uint16_t* W, int64_t ldw, uint16_t* Y, int64_t ldy, int64_t n,
-                        int64_t V, int64_t D, int64_t pad_id, float scale, mp_dev_state* st) {
-  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const int64_t id = rows::load_id<ID>(ids, i);
-    const bool pad = pad_id >= 0 && id == pad_id, bad = !pad && (id < 0 || id >= V);
-    if (bad && threadIdx.x == 0) rows::record_bad_id(st);
-    for (int64_t c = threadIdx.x; c < D; c += kThreads)
-      Y[i * ldy + c] = pad ? (uint16_t)0 : bad ? kNan16 : rows::f2h(scale * rows::h2f(W[id * ldw + c]));
+__device__ __forceinline__ int64_t id_at(const void* ids, int id_bytes, int64_t i) {
+  return id_bytes == 8 ? rows::load_id<int64_t>(ids, i) : rows::load_id<int32_t>(ids, i);
+}
+__device__ __forceinline__ void store_vec(uint16_t* p, const uint4& q, int nv) {   // the first nv of eight elements
+  if (nv >= 8) {
+    *reinterpret_cast<uint4*>(p) = q;
+    return;
   }
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (j < nv) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
 }
 
-// One block per table row: the block looks through all ids, 256 at a time, and lists the tokens
-// of its row in ascending order; then every thread adds its columns over the list.
-template <class ID>
-__global__ void __launch_bounds__(kThreads)
-mp_embedding_bwd_kernel(const void* ids, const uint16_t* dY, int64_t lddy, uint16_t* dW, int64_t ldw, int64_t n,
-                        int64_t V, int64_t D, int64_t pad_id, float scale, mp_dev_state* st, float* acc_all) {
-  __shared__ int64_t s_list[kThreads];
-  __shared__ int s_count[kThreads / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  float* acc = acc_all + (int64_t)blockIdx.x * D;
-  for (int64_t v = blockIdx.x; v < V; v += gridDim.x) {
-    for (int64_t c = threadIdx.x; c < D; c += kThreads) acc[c] = 0.0f;
-    for (int64_t i0 = 0; i0 < n; i0 += kThreads) {
-      const int64_t i = i0 + threadIdx.x;
-      const int64_t id = i < n ? rows::load_id<ID>(ids, i) : -1;
-      if (v == 0 && i < n && (id < 0 || id >= V) && !(pad_id >= 0 && id == pad_id)) rows::record_bad_id(st);
-      const bool mine = i < n && id == v && !(pad_id >= 0 && id == pad_id);
-      const unsigned mask = __ballot_sync(0xFFFFFFFFu, mine);
-      if (lane == 0) s_count[warp] = __popc(mask);
-      __syncthreads();
-      int before = 0, total = 0;
-      for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) before += s_count[w];
-        total += s_count[w];
+__global__ void __launch_bounds__(kFwdThreads)
+mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_t ldw, uint16_t* Y, int64_t ldy,
+                        int64_t n, int64_t V, int D, int64_t pad_id, float scale, mp_dev_state* st) {
+  const int vecs = (D + 7) / 8;
+  const int64_t total = n * vecs;
+  for (int64_t x = (int64_t)blockIdx.x * kFwdThreads + threadIdx.x; x < total; x += (int64_t)gridDim.x * kFwdThreads) {
+    const int64_t i = total <= UINT_MAX ? (uint32_t)x / (uint32_t)vecs : x / vecs;
+    const int col = (int)(x - i * vecs) * 8, nv = D - col < 8 ? D - col : 8;
+    const int64_t id = id_at(ids, id_bytes, i);
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (!(pad_id >= 0 && id == pad_id)) {
+      if (id >= 0 && id < V) {
+        rows::Raw8<uint16_t> r;
+        r.load_cached(W + id * ldw + col, nv);
+        float f[8];
+        r.floats(f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] *= scale;
+        q = rows::pack8(f);
+      } else {
+        q = make_uint4(kNan2, kNan2, kNan2, kNan2);
+        if (col == 0) rows::record_bad_id(st);
       }
-      if (mine) s_list[before + __popc(mask & ((1u << lane) - 1))] = i;
-      __syncthreads();
-      if (total)
-        for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-          float a = acc[c];
-          for (int k = 0; k < total; ++k) a += rows::h2f(dY[s_list[k] * lddy + c]);
-          acc[c] = a;
-        }
-      __syncthreads();
     }
-    bool bad = false;
-    for (int64_t c = threadIdx.x; c < D; c += kThreads) {
-      const uint16_t h = rows::f2h(scale * acc[c]);
-      dW[v * ldw + c] = h;
-      bad |= rows::nonfinite16(h);
-    }
-    if (bad && st != nullptr) atomicOr(&st->h.found_inf, 1);
+    store_vec(Y + i * ldy + col, q, nv);
   }
 }
 
-constexpr int64_t kMaxBlocks = 148 * 8;
+// ---------------------------------------------------------------- gradient
+//
+// 1. One cluster of 8 blocks sorts the tokens by id while the rest of the GPU writes zeros over dW, which
+//    takes longer (most rows of a large table get no token of a batch).  The sort is a stable radix
+//    sort of at most 10 bits a pass; each of the 256 warps owns a run of tokens, counts its digits, and
+//    after a scan over digits, blocks and warps places its tokens in order.
+// 2. The sorted tokens are cut into tiles; a group of threads, one for each 8 columns, adds the rows of
+//    dY over its tile and stores a row of dW whenever the id changes.  A run of one id that reaches
+//    into the next tile is finished by the tile in which it begins; a run over three tiles or more leaves
+//    one FP32 partial row in each tile.
+// 3. The partial rows of such runs are added in order.
+// dY is read once and dW written once (rows with tokens twice): HBM bounds it.  No floating-point
+// atomics: the order of every sum follows from the ids alone.
+constexpr int kSortCluster = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kMostBits = 10;
+constexpr int kTileRound = 128;                  // the sorted lists are filled up to a multiple of this
+
+struct SortArgs {
+  const void* ids;
+  int id_bytes;
+  int n, n_round;                                // n_round: n rounded up to kTileRound
+  int V;
+  int64_t pad_id;
+  int* key[2];                                   // ping-pong: pass p writes [p & 1]
+  int* pos[2];
+  int passes, bits;
+  uint16_t* dW;
+  int64_t ldw;
+  int D;
+  mp_dev_state* st;
+};
+
+__device__ __forceinline__ int sort_key(const SortArgs& a, int i) {   // tokens that count for nothing go last
+  const int64_t id = id_at(a.ids, a.id_bytes, i);
+  if (a.pad_id >= 0 && id == a.pad_id) return a.V;
+  if (id >= 0 && id < a.V) return (int)id;
+  rows::record_bad_id(a.st);
+  return a.V;
+}
+
+__device__ void fill_zeros(const SortArgs& a, int64_t worker, int64_t workers) {
+  const int vecs = (a.D + 7) / 8;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  if (a.ldw == a.D && a.D % 8 == 0) {
+    uint4* p = reinterpret_cast<uint4*>(a.dW);
+    const int64_t total = (int64_t)a.V * vecs;
+    for (int64_t x = worker; x < total; x += workers) __stcs(p + x, zero);
+    return;
+  }
+  const int64_t total = (int64_t)a.V * vecs;
+  for (int64_t x = worker; x < total; x += workers) {
+    const int64_t v = total <= UINT_MAX ? (uint32_t)x / (uint32_t)vecs : x / vecs;
+    const int col = (int)(x - v * vecs) * 8;
+    store_vec(a.dW + v * a.ldw + col, zero, a.D - col < 8 ? a.D - col : 8);
+  }
+}
+
+__global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads, 1)
+mp_embedding_sort_kernel(const SortArgs a) {
+  ptx::launch_dependents();                      // the sum kernel's blocks take the places of those that are done
+  if (blockIdx.x >= kSortCluster) {              // the other clusters
+    fill_zeros(a, (int64_t)(blockIdx.x - kSortCluster) * kSortThreads + threadIdx.x,
+               (int64_t)(gridDim.x - kSortCluster) * kSortThreads);
+    return;
+  }
+  extern __shared__ int hist[];                  // [warp][digit]
+  __shared__ int s_total[1 << kMostBits];        // of this block, by digit; the other blocks read it
+  __shared__ int s_warp[kSortWarps];
+  const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, digits = 1 << a.bits;
+  int* mine = hist + warp * digits;
+  // runs of whole 32s, in order over blocks and warps
+  const int64_t run = (((int64_t)a.n + kSortCluster * kSortThreads - 1) / (kSortCluster * kSortThreads)) * 32;
+  const int64_t begin = (rank * kSortWarps + warp) * run;
+  const int64_t end = begin + run < a.n ? begin + run : a.n;
+  for (int pass = 0; pass < a.passes; ++pass) {
+    const int shift = pass * a.bits;
+    const int* key_in = a.key[(pass & 1) ^ 1];
+    const int* pos_in = a.pos[(pass & 1) ^ 1];
+    int* key_out = a.key[pass & 1];
+    int* pos_out = a.pos[pass & 1];
+    auto key_at = [&](int64_t i) { return pass == 0 ? sort_key(a, (int)i) : __ldcg(key_in + i); };
+    for (int j = threadIdx.x; j < kSortWarps * digits; j += kSortThreads) hist[j] = 0;
+    __syncthreads();
+    // count
+    for (int64_t i0 = begin; i0 < end; i0 += 128) {
+      int d[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t i = i0 + u * 32 + lane;
+        d[u] = i < end ? (key_at(i) >> shift) & (digits - 1) : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (d[u] >= 0) atomicAdd(mine + d[u], 1);
+    }
+    __syncthreads();
+    // scan: thread j owns digit j
+    int total = 0;
+    if ((int)threadIdx.x < digits) {
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) total += hist[w * digits + threadIdx.x];
+      s_total[threadIdx.x] = total;
+    }
+    ptx::cluster_sync();
+    int all = 0, before = 0;                     // of this digit: over the cluster, and in lower blocks
+    if ((int)threadIdx.x < digits) {
+      const uint32_t at = ptx::smem_u32(s_total + threadIdx.x);
+#pragma unroll
+      for (int r = 0; r < kSortCluster; ++r) {
+        int x;
+        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(ptx::map_to_cta(at, r)) : "memory");
+        if (r < rank) before += x;
+        all += x;
+      }
+    }
+    int sum = all;                               // inclusive scan over the digits
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 31) s_warp[warp] = sum;
+    __syncthreads();
+    int base = sum - all + before;
+    for (int w = 0; w < warp; ++w) base += s_warp[w];
+    if ((int)threadIdx.x < digits)
+#pragma unroll 8
+      for (int w = 0; w < kSortWarps; ++w) {
+        const int x = hist[w * digits + threadIdx.x];
+        hist[w * digits + threadIdx.x] = base;
+        base += x;
+      }
+    __syncthreads();
+    // place: in order within a run, equal digits of 32 neighbours by their lanes
+    for (int64_t i0 = begin; i0 < end; i0 += 128) {
+      int k[4], p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t i = i0 + u * 32 + lane;
+        k[u] = i < end ? key_at(i) : -1;
+        p[u] = pass == 0 ? (int)i : i < end ? __ldcg(pos_in + i) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int d = k[u] >= 0 ? (k[u] >> shift) & (digits - 1) : -1;
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, d);
+        if (d >= 0) {
+          const int to = mine[d] + __popc(same & ((1u << lane) - 1));
+          __stcg(key_out + to, k[u]);
+          __stcg(pos_out + to, p[u]);
+        }
+        __syncwarp();
+        if (d >= 0 && (same >> lane) == 1u) mine[d] += __popc(same);     // the highest lane of the digit
+        __syncwarp();
+      }
+    }
+    ptx::cluster_sync();                         // the pass's lists are complete; s_total may be written again
+  }
+  // what follows the last token belongs to no row
+  for (int64_t i = (int64_t)a.n + rank * kSortThreads + threadIdx.x; i < a.n_round; i += kSortCluster * kSortThreads)
+    a.key[(a.passes & 1) ^ 1][i] = a.V;
+}
+
+struct SumArgs {
+  const int* key;
+  const int* pos;
+  int n_round, V, tile;                          // tile: sorted tokens per tile, a multiple of 8 that divides n_round
+  const uint16_t* dY;
+  int64_t lddy;
+  uint16_t* dW;
+  int64_t ldw;
+  int D;
+  float scale;
+  float* part;                                   // [tile][2][D4]: a run from before the tile, a run that goes on
+  int D4;                                        // D rounded up to 8
+  mp_dev_state* st;
+};
+
+// Key of sorted position p; -1 before the first and past the last.
+__device__ __forceinline__ int key_of(const SumArgs& a, int64_t p) { return p < 0 || p >= a.n_round ? -1 : __ldg(a.key + p); }
+
+__device__ __forceinline__ bool store_row(const SumArgs& a, int key, int col, const float (&acc)[8]) {
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f[j] = a.scale * acc[j];
+  const int nv = a.D - col < 8 ? a.D - col : 8;
+  const uint4 q = rows::pack8(f);
+  store_vec(a.dW + (int64_t)key * a.ldw + col, q, nv);
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bad |= j < nv && !(fabsf(f[j]) < 65520.0f);      // what FP16 rounds to a finite number
+  return bad;
+}
+
+constexpr int kSumThreads = 256;
+__global__ void __launch_bounds__(kSumThreads) mp_embedding_sum_kernel(const SumArgs a, int cols, int tiles) {
+  // cols: vectors of 8 columns that a group of threads covers; blockIdx.y picks them
+  const int groups = kSumThreads / cols, group = threadIdx.x / cols;
+  const int64_t t = (int64_t)blockIdx.x * groups + group;
+  const int col = (blockIdx.y * cols + threadIdx.x % cols) * 8;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the sorted lists and the zeros are complete
+  if (group >= groups || t >= tiles || col >= a.D) return;
+  const int64_t p0 = t * a.tile, p1 = p0 + a.tile;
+  const int first = key_of(a, p0), last = key_of(a, p1 - 1), next = key_of(a, p1);
+  if (first >= a.V) return;
+  // the run that comes from before: two tiles long, it belongs to the tile before; else it leaves a partial row
+  const bool from_before = p0 > 0 && key_of(a, p0 - 1) == first;
+  const bool skip_head = from_before && next != first && key_of(a, p0 - a.tile - 1) != first;
+  // the run that goes on, if it begins here: two tiles long, it is finished here
+  const bool goes_on = next == last && last < a.V;
+  const bool finish = goes_on && !(from_before && first == last) && key_of(a, p1 + a.tile) != last;
+  float acc[8] = {};
+  int cur = first;
+  bool head = from_before, bad = false;
+  auto emit = [&](bool open) {                   // open: the run goes on after what was added
+    if (cur >= a.V || (head && skip_head)) return;
+    if (!head && !open) {
+      bad |= store_row(a, cur, col, acc);
+      return;
+    }
+    float* to = a.part + (t * 2 + (head ? 0 : 1)) * a.D4 + col;
+    reinterpret_cast<float4*>(to)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    reinterpret_cast<float4*>(to)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+  };
+  const uint16_t* base = a.dY + col;
+  bool done = false;
+  for (int64_t p = p0; !done && p < (finish ? p1 + a.tile : p1); p += 8) {
+    int k[8], q[8];
+    *reinterpret_cast<int4*>(k) = __ldg(reinterpret_cast<const int4*>(a.key + p));
+    *reinterpret_cast<int4*>(k + 4) = __ldg(reinterpret_cast<const int4*>(a.key + p) + 1);
+    *reinterpret_cast<int4*>(q) = __ldg(reinterpret_cast<const int4*>(a.pos + p));
+    *reinterpret_cast<int4*>(q + 4) = __ldg(reinterpret_cast<const int4*>(a.pos + p) + 1);
+    uint4 v[8];
+    const bool beyond = p >= p1;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool wanted = k[u] < a.V && (!beyond || k[u] == last) && !(skip_head && k[u] == first);
+      v[u] = wanted ? __ldcs(reinterpret_cast<const uint4*>(base + (int64_t)q[u] * a.lddy)) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (done) continue;
+      if (k[u] != cur) {
+        if (beyond) {                            // the run that was to be finished ends
+          done = true;
+          continue;
+        }
+        emit(false);
+        head = false;
+        cur = k[u];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+      }
+      float f[8];
+      rows::Raw8<uint16_t> r;
+      r.q = v[u];
+      r.floats(f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += f[j];
+    }
+  }
+  emit(finish ? false : goes_on);
+  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
+}
+
+// Runs over three tiles or more: the tile in which one begins left its part, every further tile its own.  A block
+// looks through its share of the tiles for the beginnings of such runs; 16 groups of 16 threads
+// (4 columns each) add the parts of a run in 16 pieces, and the pieces in order.
+constexpr int kJoinThreads = 256, kJoinGroups = 16, kJoinCols = 64;
+__global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles) {
+  __shared__ float4 sm[kJoinGroups][16];
+  const int group = threadIdx.x / 16, col = blockIdx.y * kJoinCols + (threadIdx.x % 16) * 4;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete
+  bool bad = false;
+  for (int64_t t0 = blockIdx.x; t0 < tiles; t0 += (int64_t)gridDim.x * kJoinThreads) {
+    // thread x looks at tile t0 + x * blocks
+    const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
+    bool begins = false;
+    if (t < tiles) {
+      const int64_t p0 = t * a.tile, p1 = p0 + a.tile;
+      const int last = key_of(a, p1 - 1);
+      begins = last < a.V && key_of(a, p1) == last && key_of(a, p1 + a.tile) == last &&
+               !(key_of(a, p0) == last && key_of(a, p0 - 1) == last);
+    }
+    __shared__ unsigned found[kJoinThreads / 32];
+    const unsigned votes = __ballot_sync(0xFFFFFFFFu, begins);
+    if ((threadIdx.x & 31) == 0) found[threadIdx.x >> 5] = votes;
+    __syncthreads();
+    for (int x = 0; x < kJoinThreads; ++x) {
+      if (!(found[x >> 5] >> (x & 31) & 1)) {
+        if (found[x >> 5] >> (x & 31) == 0) x |= 31;   // none in the rest of this word
+        continue;
+      }
+      const int64_t b = t0 + (int64_t)x * gridDim.x;
+      const int key = key_of(a, (b + 1) * a.tile - 1);
+      // further tiles whose first token is of this id
+      int more = 0;
+      for (;;) {
+        const int here = __syncthreads_count(key_of(a, (b + 1 + more + threadIdx.x) * a.tile) == key);
+        more += here;
+        if (here < kJoinThreads) break;
+      }
+      const int parts = more + 1, per = (parts + kJoinGroups - 1) / kJoinGroups;
+      const int from = group * per, to = from + per < parts ? from + per : parts;
+      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (col < a.D4)
+#pragma unroll 4
+        for (int i = from; i < to; ++i) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part + ((b + i) * 2 + (i == 0 ? 1 : 0)) * a.D4 + col));
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+      sm[group][threadIdx.x % 16] = s;
+      __syncthreads();
+      if (group == 0 && col < a.D) {
+        for (int g = 1; g < kJoinGroups; ++g) {
+          const float4 v = sm[g][threadIdx.x];
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const float f[4] = {a.scale * s.x, a.scale * s.y, a.scale * s.z, a.scale * s.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < a.D) {
+            const uint16_t h = rows::f2h(f[j]);
+            a.dW[(int64_t)key * a.ldw + col + j] = h;
+            bad |= rows::nonfinite16(h);
+          }
+      }
+      __syncthreads();
+    }
+    __syncthreads();
+  }
+  if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
+}
 
 int check(const char* name, const void* ids, int id_bytes, const void* a16, int64_t lda, const void* b16,
           int64_t ldb, int64_t n, int64_t V, int64_t D) {
@@ -77,7 +400,24 @@ int check(const char* name, const void* ids, int id_bytes, const void* a16, int6
       (reinterpret_cast<uintptr_t>(ids) & (uintptr_t)(id_bytes - 1)))
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: matrices must be 16-byte aligned with pitches that are multiples of 8, "
                          "ids aligned to their width", name);
+  if (D > INT_MAX - 8) return mp::set_error(MP_ERR_TOO_LARGE, "%s: D must be below 2^31 - 8", name);
   return MP_OK;
+}
+
+int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// Sorted tokens per tile: about 8 16-byte loads for each of the threads that fit the GPU at once (148 SMs
+// x 1024), so that a small batch spreads over all SMs and a large one leaves few partial rows.
+int64_t tile_for(int64_t n, int64_t D) {
+  int64_t t = 16;
+  while (t < kTileRound && t * 148 * 1024 < n * ((D + 7) / 8)) t *= 2;
+  return t;
+}
+
+// The workspace: two lists of keys, two of positions, the partial rows of the tiles.
+size_t list_bytes(int64_t n) { return (size_t)round_up(n, kTileRound) * 4; }
+size_t part_bytes(int64_t n, int64_t D) {
+  return (size_t)(round_up(n, kTileRound) / tile_for(n, D)) * 2 * (size_t)round_up(D, 8) * sizeof(float);
 }
 
 }  // namespace
@@ -91,18 +431,18 @@ int mp_embedding_fwd(const void* ids, int id_bytes, const void* W16, int64_t ldw
   if (int rc = check("mp_embedding_fwd", ids, id_bytes, W16, ldw, Y16, ldy, n, V, D)) return rc;
   if (int rc = mp::check_device()) return rc;
   if (n == 0) return MP_OK;
-  const int grid = (int)(n < kMaxBlocks ? n : kMaxBlocks);
-  auto kernel = id_bytes == 8 ? mp_embedding_fwd_kernel<int64_t> : mp_embedding_fwd_kernel<int32_t>;
-  kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(ids, (const uint16_t*)W16, ldw, (uint16_t*)Y16, ldy, n, V, D,
-                                                      pad_id, scale, state ? state->dev : nullptr);
+  const int64_t blocks = (n * ((D + 7) / 8) + kFwdThreads - 1) / kFwdThreads, most = 148 * 8 * 4;
+  mp_embedding_fwd_kernel<<<(unsigned)(blocks < most ? blocks : most), kFwdThreads, 0, (cudaStream_t)stream>>>(
+      ids, id_bytes, (const uint16_t*)W16, ldw, (uint16_t*)Y16, ldy, n, V, (int)D, pad_id, scale,
+      state ? state->dev : nullptr);
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
   return MP_OK;
 }
 
 size_t mp_embedding_bwd_workspace_bytes(int64_t n, int64_t V, int64_t D) {
-  if (n < 0 || V <= 0 || D <= 0 || n >= INT_MAX || V >= INT_MAX) return 0;
-  return (size_t)(V < kMaxBlocks ? V : kMaxBlocks) * (size_t)D * sizeof(float);
+  if (n < 0 || V <= 0 || D <= 0 || n >= INT_MAX - kTileRound || V >= INT_MAX || D > INT_MAX - 8) return 0;
+  return 4 * list_bytes(n) + part_bytes(n, D) + 16;
 }
 
 int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t lddy, void* dW16, int64_t ldw,
@@ -111,20 +451,87 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   if (!dW16 || (n > 0 && (!ids || !dY16)))
     return mp::set_error(MP_ERR_INVALID_ARG, "mp_embedding_bwd: null pointer");
   if (int rc = check("mp_embedding_bwd", ids, id_bytes, dY16, lddy, dW16, ldw, n, V, D)) return rc;
-  if (n >= INT_MAX || V >= INT_MAX)
-    return mp::set_error(MP_ERR_TOO_LARGE, "mp_embedding_bwd: n and V must be below 2^31 - 1");
+  if (n >= INT_MAX - kTileRound || V >= INT_MAX)
+    return mp::set_error(MP_ERR_TOO_LARGE, "mp_embedding_bwd: n and V must be below 2^31 - %d", kTileRound + 1);
   if (workspace && !mp::aligned16(workspace))
     return mp::set_error(MP_ERR_ALIGNMENT, "mp_embedding_bwd: workspace must be 16-byte aligned");
   const size_t need = mp_embedding_bwd_workspace_bytes(n, V, D);
   if (!workspace || workspace_bytes < need)
     return mp::set_error(MP_ERR_NOMEM, "mp_embedding_bwd: workspace of %zu bytes needed", need);
   if (int rc = mp::check_device()) return rc;
-  const int grid = (int)(V < kMaxBlocks ? V : kMaxBlocks);
-  auto kernel = id_bytes == 8 ? mp_embedding_bwd_kernel<int64_t> : mp_embedding_bwd_kernel<int32_t>;
-  kernel<<<grid, kThreads, 0, (cudaStream_t)stream>>>(ids, (const uint16_t*)dY16, lddy, (uint16_t*)dW16, ldw, n, V, D,
-                                                      pad_id, scale, state ? state->dev : nullptr, (float*)workspace);
+  cudaStream_t st = (cudaStream_t)stream;
+  mp_dev_state* dev = state ? state->dev : nullptr;
+  char* ws = (char*)workspace;
+  const size_t lb = list_bytes(n);
+  SortArgs s{};
+  s.ids = ids;
+  s.id_bytes = id_bytes;
+  s.n = (int)n;
+  s.n_round = (int)round_up(n, kTileRound);
+  s.V = (int)V;
+  s.pad_id = pad_id;
+  for (int i = 0; i < 2; ++i) {
+    s.key[i] = (int*)(ws + 2 * i * lb);
+    s.pos[i] = (int*)(ws + (2 * i + 1) * lb);
+  }
+  int bits = 1;                                  // of the largest key, V itself
+  while (bits < 31 && ((int64_t)1 << bits) <= V) ++bits;
+  s.passes = (bits + kMostBits - 1) / kMostBits;
+  s.bits = (bits + s.passes - 1) / s.passes;
+  s.dW = (uint16_t*)dW16;
+  s.ldw = ldw;
+  s.D = (int)D;
+  s.st = dev;
+  const int smem = kSortWarps * (1 << s.bits) * (int)sizeof(int);
+  {
+    static std::mutex mu;
+    static std::map<int, bool> allowed;
+    int device = 0;
+    MP_CUDA_TRY(cudaGetDevice(&device));
+    std::lock_guard<std::mutex> lock(mu);
+    if (!allowed[device]) {
+      MP_CUDA_TRY(cudaFuncSetAttribute(mp_embedding_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kSortWarps * (1 << kMostBits) * (int)sizeof(int)));
+      allowed[device] = true;
+    }
+  }
+  mp_embedding_sort_kernel<<<kSortCluster * 18, kSortThreads, smem, st>>>(s);     // 18 clusters of 8 blocks: 144 of 148 SMs
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
+  if (n == 0) return MP_OK;
+  SumArgs m{};
+  m.key = s.key[(s.passes & 1) ^ 1];
+  m.pos = s.pos[(s.passes & 1) ^ 1];
+  m.n_round = s.n_round;
+  m.V = (int)V;
+  m.tile = (int)tile_for(n, D);
+  m.dY = (const uint16_t*)dY16;
+  m.lddy = lddy;
+  m.dW = (uint16_t*)dW16;
+  m.ldw = ldw;
+  m.D = (int)D;
+  m.scale = scale;
+  m.part = (float*)(ws + 4 * lb);
+  m.D4 = (int)round_up(D, 8);
+  m.st = dev;
+  const int tiles = s.n_round / m.tile, vecs = m.D4 / 8, cols = vecs < kSumThreads ? vecs : kSumThreads;
+  const int groups = kSumThreads / cols;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((tiles + groups - 1) / groups), (unsigned)((vecs + cols - 1) / cols), 1);
+  cfg.blockDim = dim3(kSumThreads, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr;            // resident early, waits on the device for the kernel before
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, tiles));
+  mp::count_launch();
+  if (tiles < 3) return MP_OK;         // no run over three tiles
+  cfg.gridDim = dim3((unsigned)(tiles < 148 ? tiles : 148), (unsigned)((m.D4 + kJoinCols - 1) / kJoinCols), 1);
+  cfg.blockDim = dim3(kJoinThreads, 1, 1);
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles));
+  mp::count_launch();
   return MP_OK;
 }
 
