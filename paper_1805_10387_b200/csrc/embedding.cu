@@ -62,7 +62,7 @@ mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_
 //
 // 1. One cluster of 8 blocks sorts the tokens by id while the rest of the GPU writes zeros over dW, which
 //    takes longer (most rows of a large table get no token of a batch).  The sort is a stable radix
-//    sort of at most 10 bits a pass; each of the 256 warps owns a run of tokens, counts its digits, and
+//    sort of at most 8 bits a pass; each of the 256 warps owns a run of tokens, counts its digits, and
 //    after a scan over digits, blocks and warps places its tokens in order.
 // 2. The sorted tokens are cut into tiles; a group of threads, one for each 8 columns, adds the rows of
 //    dY over its tile and stores a row of dW whenever the id changes.  A run of one id that reaches
@@ -72,8 +72,8 @@ mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_
 // dY is read once and dW written once (rows with tokens twice): HBM bounds it.  No floating-point
 // atomics: the order of every sum follows from the ids alone.
 constexpr int kSortCluster = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kMostBits = 10;
-constexpr int kTileRound = 128;                  // the sorted lists are filled up to a multiple of this
+constexpr int kMostBits = 8, kHistPitch = (1 << kMostBits) + 1;   // odd pitch: a quad's four rows lie in four banks
+constexpr int kTileRound = 128;                  // the sorted lists are filled up to a multiple of this and of every tile
 
 struct SortArgs {
   const void* ids;
@@ -123,12 +123,14 @@ mp_embedding_sort_kernel(const SortArgs a) {
                (int64_t)(gridDim.x - kSortCluster) * kSortThreads);
     return;
   }
-  extern __shared__ int hist[];                  // [warp][digit]
+  __shared__ int hist[kSortWarps][kHistPitch];   // [warp][digit]
   __shared__ int s_total[1 << kMostBits];        // of this block, by digit; the other blocks read it
   __shared__ int s_warp[kSortWarps];
-  const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, digits = 1 << a.bits;
-  int* mine = hist + warp * digits;
-  // runs of whole 32s, in order over blocks and warps
+  const int rank = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mask = (1 << a.bits) - 1;
+  int* mine = hist[warp];
+  // runs of whole 32s, in order over blocks and warps; kStep tokens of a run are worked on at once, and a run
+  // that is no longer stays in registers between counting and placing
+  constexpr int kStep = 128, kU = kStep / 32;
   const int64_t run = (((int64_t)a.n + kSortCluster * kSortThreads - 1) / (kSortCluster * kSortThreads)) * 32;
   const int64_t begin = (rank * kSortWarps + warp) * run;
   const int64_t end = begin + run < a.n ? begin + run : a.n;
@@ -138,79 +140,117 @@ mp_embedding_sort_kernel(const SortArgs a) {
     const int* pos_in = a.pos[(pass & 1) ^ 1];
     int* key_out = a.key[pass & 1];
     int* pos_out = a.pos[pass & 1];
-    auto key_at = [&](int64_t i) { return pass == 0 ? sort_key(a, (int)i) : __ldcg(key_in + i); };
-    for (int j = threadIdx.x; j < kSortWarps * digits; j += kSortThreads) hist[j] = 0;
+    int k[kU], p[kU];
+    unsigned same[kU];                           // lanes with the same digit
+    auto load = [&](int64_t i0, bool with_pos) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int64_t i = i0 + u * 32 + lane;
+        k[u] = i >= end ? -1 : pass == 0 ? sort_key(a, (int)i) : __ldcg(key_in + i);
+        p[u] = pass == 0 ? (int)i : i < end && with_pos ? __ldcg(pos_in + i) : 0;
+      }
+    };
+    auto digit = [&](int key) { return key < 0 ? -1 : (key >> shift) & mask; };
+    auto match = [&] {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {             // a vote a bit: cheaper than the hardware's match of whole values
+        if (u * 32 >= run) break;
+        same[u] = __ballot_sync(0xFFFFFFFFu, k[u] >= 0);
+#pragma unroll
+        for (int bit = 0; bit < kMostBits; ++bit) {
+          if (bit >= a.bits) break;
+          const bool on = k[u] >> (shift + bit) & 1;
+          const unsigned votes = __ballot_sync(0xFFFFFFFFu, on);
+          same[u] &= on ? votes : ~votes;
+        }
+      }
+    };
+    for (int j = threadIdx.x; j < kSortWarps * kHistPitch; j += kSortThreads) (&hist[0][0])[j] = 0;
+    load(begin, run <= kStep);
     __syncthreads();
     // count
-    for (int64_t i0 = begin; i0 < end; i0 += 128) {
-      int d[4];
+    for (int64_t i0 = begin; i0 < end; i0 += kStep) {
+      if (i0 > begin) load(i0, false);
+      match();
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t i = i0 + u * 32 + lane;
-        d[u] = i < end ? (key_at(i) >> shift) & (digits - 1) : -1;
+      for (int u = 0; u < kU; ++u) {             // the highest lane of a digit counts for all
+        if (u * 32 >= run) break;
+        if (k[u] >= 0 && (same[u] >> lane) == 1u) mine[digit(k[u])] += __popc(same[u]);
+        __syncwarp();
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (d[u] >= 0) atomicAdd(mine + d[u], 1);
     }
     __syncthreads();
-    // scan: thread j owns digit j
-    int total = 0;
-    if ((int)threadIdx.x < digits) {
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) total += hist[w * digits + threadIdx.x];
-      s_total[threadIdx.x] = total;
+    // scan: four threads per digit, eight warps' counts each
+    const int dg = threadIdx.x >> 2, q = threadIdx.x & 3;
+    int count[8], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      count[i] = hist[q * 8 + i][dg];
+      sum += count[i];
     }
+    int upto = sum;                              // over this quad's threads up to this one
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, upto, o, 4);
+      if (q >= o) upto += y;
+    }
+    if (q == 3) s_total[dg] = upto;
     ptx::cluster_sync();
     int all = 0, before = 0;                     // of this digit: over the cluster, and in lower blocks
-    if ((int)threadIdx.x < digits) {
-      const uint32_t at = ptx::smem_u32(s_total + threadIdx.x);
+    const uint32_t at = ptx::smem_u32(s_total + dg);
 #pragma unroll
-      for (int r = 0; r < kSortCluster; ++r) {
-        int x;
-        asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(ptx::map_to_cta(at, r)) : "memory");
-        if (r < rank) before += x;
-        all += x;
-      }
+    for (int i = 0; i < kSortCluster / 4; ++i) {
+      const int r = q * (kSortCluster / 4) + i;
+      int x;
+      asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(x) : "r"(ptx::map_to_cta(at, r)) : "memory");
+      all += x;
+      before += r < rank ? x : 0;
     }
-    int sum = all;                               // inclusive scan over the digits
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+      before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
+    }
+    int lower = all;                             // over this warp's eight digits up to this one
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, lower, o);
+      if (lane >= o) lower += y;
+    }
+    if (lane == 31) s_warp[warp] = lower;
+    __syncthreads();
+    int warps = s_warp[lane];                    // over the warps up to this lane's
+    const int own = warps;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xFFFFFFFFu, sum, o);
-      if (lane >= o) sum += y;
+      const int y = __shfl_up_sync(0xFFFFFFFFu, warps, o);
+      if (lane >= o) warps += y;
     }
-    if (lane == 31) s_warp[warp] = sum;
-    __syncthreads();
-    int base = sum - all + before;
-    for (int w = 0; w < warp; ++w) base += s_warp[w];
-    if ((int)threadIdx.x < digits)
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) {
-        const int x = hist[w * digits + threadIdx.x];
-        hist[w * digits + threadIdx.x] = base;
-        base += x;
-      }
+    int base = __shfl_sync(0xFFFFFFFFu, warps - own, warp) + lower - all + before + upto - sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      hist[q * 8 + i][dg] = base;
+      base += count[i];
+    }
     __syncthreads();
     // place: in order within a run, equal digits of 32 neighbours by their lanes
-    for (int64_t i0 = begin; i0 < end; i0 += 128) {
-      int k[4], p[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t i = i0 + u * 32 + lane;
-        k[u] = i < end ? key_at(i) : -1;
-        p[u] = pass == 0 ? (int)i : i < end ? __ldcg(pos_in + i) : 0;
+    for (int64_t i0 = begin; i0 < end; i0 += kStep) {
+      if (run > kStep) {
+        load(i0, true);
+        match();
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int d = k[u] >= 0 ? (k[u] >> shift) & (digits - 1) : -1;
-        const unsigned same = __match_any_sync(0xFFFFFFFFu, d);
+      for (int u = 0; u < kU; ++u) {
+        if (u * 32 >= run) break;
+        const int d = digit(k[u]);
+        int to = 0;
+        if (d >= 0) to = mine[d] + __popc(same[u] & ((1u << lane) - 1));
+        __syncwarp();
         if (d >= 0) {
-          const int to = mine[d] + __popc(same & ((1u << lane) - 1));
+          if ((same[u] >> lane) == 1u) mine[d] = to + 1;
           __stcg(key_out + to, k[u]);
           __stcg(pos_out + to, p[u]);
         }
-        __syncwarp();
-        if (d >= 0 && (same >> lane) == 1u) mine[d] += __popc(same);     // the highest lane of the digit
         __syncwarp();
       }
     }
@@ -237,7 +277,7 @@ struct SumArgs {
 };
 
 // Key of sorted position p; -1 before the first and past the last.
-__device__ __forceinline__ int key_of(const SumArgs& a, int64_t p) { return p < 0 || p >= a.n_round ? -1 : __ldg(a.key + p); }
+__device__ __forceinline__ int key_of(const SumArgs& a, int64_t p) { return p < 0 || p >= a.n_round ? -1 : __ldcg(a.key + p); }
 
 __device__ __forceinline__ bool store_row(const SumArgs& a, int key, int col, const float (&acc)[8]) {
   float f[8];
@@ -252,23 +292,37 @@ __device__ __forceinline__ bool store_row(const SumArgs& a, int key, int col, co
   return bad;
 }
 
-constexpr int kSumThreads = 256;
-__global__ void __launch_bounds__(kSumThreads) mp_embedding_sum_kernel(const SumArgs a, int cols, int tiles) {
+constexpr int kSumThreads = 256, kMostGroups = 32;
+__global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const SumArgs a, int cols, int groups, int tiles) {
   // cols: vectors of 8 columns that a group of threads covers; blockIdx.y picks them
-  const int groups = kSumThreads / cols, group = threadIdx.x / cols;
-  const int64_t t = (int64_t)blockIdx.x * groups + group;
+  extern __shared__ int2 s_list[];               // (key, position) of the groups' tiles and of the tile after them
+  const int group = threadIdx.x / cols, window = (groups + 1) * a.tile;
+  const int64_t t = (int64_t)blockIdx.x * groups + group, begin = (int64_t)blockIdx.x * groups * a.tile;
   const int col = (blockIdx.y * cols + threadIdx.x % cols) * 8;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the sorted lists and the zeros are complete
-  if (group >= groups || t >= tiles || col >= a.D) return;
+  ptx::launch_dependents();                      // the join kernel may look through the lists meanwhile
+  for (int x = threadIdx.x; x < window; x += blockDim.x) {
+    const int64_t p = begin + x;
+    s_list[x] = p < a.n_round ? make_int2(__ldcg(a.key + p), __ldcg(a.pos + p)) : make_int2(INT_MAX, 0);
+  }
   const int64_t p0 = t * a.tile, p1 = p0 + a.tile;
-  const int first = key_of(a, p0), last = key_of(a, p1 - 1), next = key_of(a, p1);
+  int after = 0, ahead = 0, before = 0;
+  if (group < groups) {
+    after = key_of(a, p1 + a.tile);
+    ahead = key_of(a, p0 - 1);
+    before = key_of(a, p0 - a.tile - 1);
+  }
+  __syncthreads();
+  if (group >= groups || t >= tiles || col >= a.D) return;
+  const int2* list = s_list + group * a.tile;
+  const int first = list[0].x, last = list[a.tile - 1].x, next = list[a.tile].x;
   if (first >= a.V) return;
   // the run that comes from before: two tiles long, it belongs to the tile before; else it leaves a partial row
-  const bool from_before = p0 > 0 && key_of(a, p0 - 1) == first;
-  const bool skip_head = from_before && next != first && key_of(a, p0 - a.tile - 1) != first;
+  const bool from_before = ahead == first;
+  const bool skip_head = from_before && next != first && before != first;
   // the run that goes on, if it begins here: two tiles long, it is finished here
   const bool goes_on = next == last && last < a.V;
-  const bool finish = goes_on && !(from_before && first == last) && key_of(a, p1 + a.tile) != last;
+  const bool finish = goes_on && !(from_before && first == last) && after != last;
   float acc[8] = {};
   int cur = first;
   bool head = from_before, bad = false;
@@ -283,31 +337,29 @@ __global__ void __launch_bounds__(kSumThreads) mp_embedding_sum_kernel(const Sum
     reinterpret_cast<float4*>(to)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
   };
   const uint16_t* base = a.dY + col;
+  const int stop = finish ? 2 * a.tile : a.tile;
   bool done = false;
-  for (int64_t p = p0; !done && p < (finish ? p1 + a.tile : p1); p += 8) {
-    int k[8], q[8];
-    *reinterpret_cast<int4*>(k) = __ldg(reinterpret_cast<const int4*>(a.key + p));
-    *reinterpret_cast<int4*>(k + 4) = __ldg(reinterpret_cast<const int4*>(a.key + p) + 1);
-    *reinterpret_cast<int4*>(q) = __ldg(reinterpret_cast<const int4*>(a.pos + p));
-    *reinterpret_cast<int4*>(q + 4) = __ldg(reinterpret_cast<const int4*>(a.pos + p) + 1);
+  for (int p = 0; !done && p < stop; p += 8) {
+    const bool beyond = p >= a.tile;
     uint4 v[8];
-    const bool beyond = p >= p1;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const bool wanted = k[u] < a.V && (!beyond || k[u] == last) && !(skip_head && k[u] == first);
-      v[u] = wanted ? __ldcs(reinterpret_cast<const uint4*>(base + (int64_t)q[u] * a.lddy)) : make_uint4(0, 0, 0, 0);
+      const int2 e = list[p + u];
+      const bool wanted = e.x < a.V && (!beyond || e.x == last) && !(skip_head && e.x == first);
+      v[u] = wanted ? __ldcs(reinterpret_cast<const uint4*>(base + (int64_t)e.y * a.lddy)) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
+      const int k = list[p + u].x;
       if (done) continue;
-      if (k[u] != cur) {
+      if (k != cur) {
         if (beyond) {                            // the run that was to be finished ends
           done = true;
           continue;
         }
         emit(false);
         head = false;
-        cur = k[u];
+        cur = k;
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
       }
@@ -324,23 +376,23 @@ __global__ void __launch_bounds__(kSumThreads) mp_embedding_sum_kernel(const Sum
 }
 
 // Runs over three tiles or more: the tile in which one begins left its part, every further tile its own.  A block
-// looks through its share of the tiles for the beginnings of such runs; 16 groups of 16 threads
-// (4 columns each) add the parts of a run in 16 pieces, and the pieces in order.
-constexpr int kJoinThreads = 256, kJoinGroups = 16, kJoinCols = 64;
+// looks through its share of the tiles for the beginnings of such runs; 4 groups of 64 threads (4
+// columns each) add the parts of a run in 4 pieces, and the pieces in order.
+constexpr int kJoinThreads = 256, kJoinGroups = 4, kJoinLanes = kJoinThreads / kJoinGroups, kJoinCols = kJoinLanes * 4;
 __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles) {
-  __shared__ float4 sm[kJoinGroups][16];
-  const int group = threadIdx.x / 16, col = blockIdx.y * kJoinCols + (threadIdx.x % 16) * 4;
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete
-  bool bad = false;
+  __shared__ float4 sm[kJoinGroups][kJoinLanes];
+  const int group = threadIdx.x / kJoinLanes, col = blockIdx.y * kJoinCols + (threadIdx.x % kJoinLanes) * 4;
+  // (the lists were complete before the sum kernel let this one start: looking through them needs no wait)
+  bool bad = false, waited = false;
   for (int64_t t0 = blockIdx.x; t0 < tiles; t0 += (int64_t)gridDim.x * kJoinThreads) {
     // thread x looks at tile t0 + x * blocks
     const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
     bool begins = false;
     if (t < tiles) {
       const int64_t p0 = t * a.tile, p1 = p0 + a.tile;
-      const int last = key_of(a, p1 - 1);
-      begins = last < a.V && key_of(a, p1) == last && key_of(a, p1 + a.tile) == last &&
-               !(key_of(a, p0) == last && key_of(a, p0 - 1) == last);
+      const int last = key_of(a, p1 - 1), next = key_of(a, p1), after = key_of(a, p1 + a.tile);
+      const int first = key_of(a, p0), ahead = key_of(a, p0 - 1);
+      begins = last < a.V && next == last && after == last && !(first == last && ahead == last);
     }
     __shared__ unsigned found[kJoinThreads / 32];
     const unsigned votes = __ballot_sync(0xFFFFFFFFu, begins);
@@ -360,16 +412,18 @@ __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const S
         more += here;
         if (here < kJoinThreads) break;
       }
+      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete
+      waited = true;
       const int parts = more + 1, per = (parts + kJoinGroups - 1) / kJoinGroups;
       const int from = group * per, to = from + per < parts ? from + per : parts;
       float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       if (col < a.D4)
-#pragma unroll 4
+#pragma unroll 8
         for (int i = from; i < to; ++i) {
           const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part + ((b + i) * 2 + (i == 0 ? 1 : 0)) * a.D4 + col));
           s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
-      sm[group][threadIdx.x % 16] = s;
+      sm[group][threadIdx.x % kJoinLanes] = s;
       __syncthreads();
       if (group == 0 && col < a.D) {
         for (int g = 1; g < kJoinGroups; ++g) {
@@ -389,6 +443,7 @@ __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const S
     }
     __syncthreads();
   }
+  if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");     // no block is done before the sum kernel is
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 
@@ -401,6 +456,33 @@ int check(const char* name, const void* ids, int id_bytes, const void* a16, int6
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: matrices must be 16-byte aligned with pitches that are multiples of 8, "
                          "ids aligned to their width", name);
   if (D > INT_MAX - 8) return mp::set_error(MP_ERR_TOO_LARGE, "%s: D must be below 2^31 - 8", name);
+  return MP_OK;
+}
+
+// Clusters of the sort kernel that are resident at once, asked once per device.  (A GPU's processing clusters hold
+// whole clusters of 8 only: 16 on a B200.  Two more would start when the first have left, and the zeros
+// would take twice as long.)
+int resident_clusters(int* out) {
+  static std::mutex mu;
+  static std::map<int, int> resident;
+  int dev = 0;
+  MP_CUDA_TRY(cudaGetDevice(&dev));
+  std::lock_guard<std::mutex> lock(mu);
+  int& have = resident[dev];
+  if (have == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kSortCluster * 18, 1, 1);
+    cfg.blockDim = dim3(kSortThreads, 1, 1);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = kSortCluster;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&have, mp_embedding_sort_kernel, &cfg));
+    if (have < 2) have = 2;                      // the sort's and one that writes zeros
+  }
+  *out = have;
   return MP_OK;
 }
 
@@ -482,20 +564,9 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   s.ldw = ldw;
   s.D = (int)D;
   s.st = dev;
-  const int smem = kSortWarps * (1 << s.bits) * (int)sizeof(int);
-  {
-    static std::mutex mu;
-    static std::map<int, bool> allowed;
-    int device = 0;
-    MP_CUDA_TRY(cudaGetDevice(&device));
-    std::lock_guard<std::mutex> lock(mu);
-    if (!allowed[device]) {
-      MP_CUDA_TRY(cudaFuncSetAttribute(mp_embedding_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       kSortWarps * (1 << kMostBits) * (int)sizeof(int)));
-      allowed[device] = true;
-    }
-  }
-  mp_embedding_sort_kernel<<<kSortCluster * 18, kSortThreads, smem, st>>>(s);     // 18 clusters of 8 blocks: 144 of 148 SMs
+  int clusters = 0;
+  if (int rc = resident_clusters(&clusters)) return rc;
+  mp_embedding_sort_kernel<<<(unsigned)(kSortCluster * clusters), kSortThreads, 0, st>>>(s);
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
   if (n == 0) return MP_OK;
@@ -515,21 +586,24 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   m.D4 = (int)round_up(D, 8);
   m.st = dev;
   const int tiles = s.n_round / m.tile, vecs = m.D4 / 8, cols = vecs < kSumThreads ? vecs : kSumThreads;
-  const int groups = kSumThreads / cols;
+  int groups = kSumThreads / cols;
+  if (groups > kMostGroups) groups = kMostGroups;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((tiles + groups - 1) / groups), (unsigned)((vecs + cols - 1) / cols), 1);
-  cfg.blockDim = dim3(kSumThreads, 1, 1);
+  cfg.blockDim = dim3((unsigned)round_up(cols * groups, 32), 1, 1);
+  cfg.dynamicSmemBytes = (size_t)(groups + 1) * m.tile * sizeof(int2);      // 33 KiB at most
   cfg.stream = st;
   cudaLaunchAttribute attr;            // resident early, waits on the device for the kernel before
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, tiles));
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, groups, tiles));
   mp::count_launch();
   if (tiles < 3) return MP_OK;         // no run over three tiles
   cfg.gridDim = dim3((unsigned)(tiles < 148 ? tiles : 148), (unsigned)((m.D4 + kJoinCols - 1) / kJoinCols), 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
+  cfg.dynamicSmemBytes = 0;
   MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles));
   mp::count_launch();
   return MP_OK;

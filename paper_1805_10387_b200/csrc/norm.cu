@@ -466,10 +466,10 @@ mp_block_norm_sum_kernel(const float* partial, int slabs, int D, uint16_t* dg_pr
   __shared__ float sm[kSumThreads / 32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
   uint16_t* out = which == 0 ? dg_pre : which == 1 ? dg_post : dgate;
-  if (out == nullptr) return;
   const int c = blockIdx.x * 32 + lane;
   const int per = (slabs + 7) / 8, s0 = warp * per, s1 = min(slabs, s0 + per);
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete and visible
+  if (out == nullptr) return;
   float v = 0.0f;
   if (c < D)
 #pragma unroll 8
