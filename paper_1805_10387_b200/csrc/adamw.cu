@@ -7,7 +7,10 @@
 #include <math.h>
 #include <string.h>
 
+#include <map>
+#include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "rows.cuh"
@@ -29,18 +32,24 @@ struct Tensor {
   float* m_scale;
   float* v_scale;
   int64_t count;
+  int64_t block_end;                            // blocks of this tensor and of those before it
   float decay;
-};
-struct Piece {
-  int32_t tensor, block;                        // kBlock elements from block * kBlock on
 };
 struct Coef {
   float inv_s, b1, omb1, b2, omb2, decay, alpha, k2, eps;
 };
 
+// b^t by squaring, in FP64: an error of some 2 log2(t) units in the last place, and a fraction of pow's latency,
+// which every block would wait for.
+__device__ __forceinline__ double power(double b, int64_t t) {
+  double r = 1.0;
+  for (; t > 0; t >>= 1, b *= b)
+    if (t & 1) r *= b;
+  return r;
+}
 __device__ __forceinline__ Coef coefficients(const mp_dev_state* st, const mp_adamw_config& o) {
-  const double t = (double)(st->h.t + 1);
-  const double c1 = 1.0 - pow(o.beta1, t), c2 = 1.0 - pow(o.beta2, t);
+  const int64_t t = st->h.t + 1;
+  const double c1 = 1.0 - power(o.beta1, t), c2 = 1.0 - power(o.beta2, t);
   Coef c;
   c.inv_s = __fdiv_rn(1.0f, st->h.scale);
   c.b1 = (float)o.beta1;
@@ -64,81 +73,175 @@ __device__ __forceinline__ void step_one(float g16f, float& w, float& m, float& 
   w = __fsub_rn(w, __fmul_rn(c.alpha, __fdiv_rn(m, __fadd_rn(__fmul_rn(r, c.k2), c.eps))));
 }
 
-__device__ __forceinline__ float from_e4m3(uint8_t q) {
-  const __half_raw h = __nv_cvt_fp8_to_halfraw(q, __NV_E4M3);
-  return __half2float(__half(h));
+// Eight E4M3 numbers as loaded.
+__device__ __forceinline__ void from_e4m3(uint2 q, float (&f)[8]) {
+  const uint32_t w[2] = {q.x, q.y};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j / 2] >> (16 * (j & 1))), __NV_E4M3);
+    const float2 x = __half22float2(__half2(h));
+    f[2 * j] = x.x;
+    f[2 * j + 1] = x.y;
+  }
 }
-__device__ __forceinline__ uint8_t to_e4m3(float x) {
-  return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+__device__ __forceinline__ uint2 to_e4m3(const float (&f)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = __nv_cvt_float2_to_fp8x2(make_float2(f[2 * j], f[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+// The largest of a warp's non-negative values: their order is that of their bits.
+__device__ __forceinline__ float warp_top(float v) {
+  return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v)));
+}
+
+// The blocks of 256 elements that a thread block owns are one contiguous range; its warps take them in turn.
+// `f` gets the tensor, the block's number in it and the elements of this lane (0 .. 8).
+template <class F>
+__device__ __forceinline__ void for_my_blocks(const Tensor* tensors, int n_tensors, int64_t n_blocks, F f) {
+  const int64_t per = (n_blocks + gridDim.x - 1) / gridDim.x, begin = blockIdx.x * per;
+  const int64_t end = begin + per < n_blocks ? begin + per : n_blocks;
+  int64_t x = begin + (threadIdx.x >> 5);
+  if (x >= end) return;
+  int lo = 0;                                   // first tensor whose blocks end after x (the last one's end after all)
+  for (int hi = n_tensors - 1; lo < hi;) {
+    const int mid = (lo + hi) / 2;
+    if (__ldg(&tensors[mid].block_end) > x) hi = mid;
+    else lo = mid + 1;
+  }
+  for (; x < end; x += kThreads / 32) {
+    while (__ldg(&tensors[lo].block_end) <= x) ++lo;
+    const Tensor& T = tensors[lo];
+    const int64_t b = x - (__ldg(&T.block_end) - (__ldg(&T.count) + kBlock - 1) / kBlock);
+    const int64_t left = __ldg(&T.count) - b * kBlock - (threadIdx.x & 31) * 8;
+    f(T, b, left >= 8 ? 8 : left < 0 ? 0 : (int)left);
+  }
 }
 
 __global__ void __launch_bounds__(kThreads)
-mp_adamw_check_kernel(const Tensor* tensors, const Piece* pieces, int64_t n_pieces, mp_dev_state* st) {
+mp_adamw_check_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, mp_dev_state* st) {
   bool bad = false;
-  for (int64_t p = blockIdx.x; p < n_pieces; p += gridDim.x) {
-    const Tensor& T = tensors[pieces[p].tensor];
-    const int64_t i = (int64_t)pieces[p].block * kBlock + threadIdx.x;
-    bad |= i < T.count && rows::nonfinite16(T.g16[i]);
-  }
+  for_my_blocks(tensors, n_tensors, n_blocks, [&](const Tensor& T, int64_t b, int nv) {
+    rows::Raw8<uint16_t> g;
+    g.load(T.g16 + b * kBlock + (threadIdx.x & 31) * 8, nv);
+    auto both = [](uint32_t v) { return (v & 0x7C00u) == 0x7C00u || (v & 0x7C000000u) == 0x7C000000u; };
+    bad |= both(g.q.x) || both(g.q.y) || both(g.q.z) || both(g.q.w);
+  });
   if (bad) atomicOr(&st->h.found_inf, 1);
 }
 
-// One thread per element of a piece.
+// A lane takes 8 consecutive elements, so a warp takes a block of 256 that shares one scale and finds the
+// block's largest magnitude among its own registers: the states are read and written once, in place.
 template <int BITS>
 __global__ void __launch_bounds__(kThreads)
-mp_adamw_update_kernel(const Tensor* tensors, const Piece* pieces, int64_t n_pieces, const mp_dev_state* st,
-                       mp_adamw_config o, const int* gemm_status) {
+mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, const mp_dev_state* st, mp_adamw_config o,
+                       const int* gemm_status) {
   if (st->h.found_inf != 0 || st->h.status != 0 || *gemm_status != 0) return;
   __shared__ Coef s_c;
-  __shared__ float red[kThreads / 32];
   if (threadIdx.x == 0) s_c = coefficients(st, o);
   __syncthreads();
   const Coef c = s_c;
-  for (int64_t p = blockIdx.x; p < n_pieces; p += gridDim.x) {
-    const Tensor& T = tensors[pieces[p].tensor];
-    const int64_t b = pieces[p].block, i = b * kBlock + threadIdx.x;
-    const bool in = i < T.count;
-    float w = 0.0f, m = 0.0f, v = 0.0f, r = 0.0f;
-    if (in) {
-      w = T.w32[i];
-      if (BITS == 32) {
-        m = ((const float*)T.m)[i];
-        v = ((const float*)T.v)[i];
-      } else {
-        m = __fmul_rn(from_e4m3(((const uint8_t*)T.m)[i]), T.m_scale[b]);
-        r = __fmul_rn(from_e4m3(((const uint8_t*)T.v)[i]), T.v_scale[b]);
-        v = __fmul_rn(r, r);
-      }
-      step_one(rows::h2f(T.g16[i]), w, m, v, r, __fmul_rn(c.decay, T.decay), c);
-      T.w32[i] = w;
-      T.w16[i] = rows::f2h(w);
-    }
-    if (BITS == 32) {
-      if (in) {
-        ((float*)T.m)[i] = m;
-        ((float*)T.v)[i] = v;
-      }
+  for_my_blocks(tensors, n_tensors, n_blocks, [&](const Tensor& T, int64_t b, int nv) {
+    const int64_t i = b * kBlock + (threadIdx.x & 31) * 8;
+    rows::Raw8<uint16_t> gr;
+    rows::Raw8<float> wr;
+    float g[8], w[8], m[8], v[8], r[8];
+    gr.load(T.g16 + i, nv);
+    wr.load(T.w32 + i, nv);
+    if constexpr (BITS == 32) {
+      rows::Raw8<float> mr, vr;
+      mr.load((const float*)T.m + i, nv);
+      vr.load((const float*)T.v + i, nv);
+      mr.floats(m);
+      vr.floats(v);
     } else {
-      const float tm = rows::block_max<kThreads / 32>(fabsf(m), red), tr = rows::block_max<kThreads / 32>(r, red);
-      const float im = tm < kNoScale ? 0.0f : __fdiv_rn(kTop, tm), ir = tr < kNoScale ? 0.0f : __fdiv_rn(kTop, tr);
-      if (in) {
-        ((uint8_t*)T.m)[i] = to_e4m3(__fmul_rn(m, im));
-        ((uint8_t*)T.v)[i] = to_e4m3(r > 0.0f && ir > 0.0f ? fmaxf(__fmul_rn(r, ir), kTiny) : 0.0f);
+      uint2 mq = make_uint2(0, 0), vq = mq;
+      if (nv > 0) {
+        mq = __ldcs(reinterpret_cast<const uint2*>((const uint8_t*)T.m + i));
+        vq = __ldcs(reinterpret_cast<const uint2*>((const uint8_t*)T.v + i));
       }
-      if (threadIdx.x == 0) {
+      const float ms = T.m_scale[b], vs = T.v_scale[b];
+      from_e4m3(mq, m);
+      from_e4m3(vq, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = __fmul_rn(m[j], ms);
+        r[j] = __fmul_rn(r[j], vs);
+        v[j] = __fmul_rn(r[j], r[j]);
+      }
+    }
+    gr.floats(g);
+    wr.floats(w);
+    const float decay = __fmul_rn(c.decay, T.decay);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) step_one(g[j], w[j], m[j], v[j], r[j], decay, c);
+    rows::store8(T.w32 + i, w, nv);
+    rows::store8(T.w16 + i, w, nv);
+    if constexpr (BITS == 32) {
+      rows::store8((float*)T.m + i, m, nv);
+      rows::store8((float*)T.v + i, v, nv);
+    } else {
+      // what lies past the tensor's end has no say in the scale and is not stored
+      float tm = 0.0f, tr = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        tm = j < nv ? fmaxf(tm, fabsf(m[j])) : tm;
+        tr = j < nv ? fmaxf(tr, r[j]) : tr;
+      }
+      tm = warp_top(tm);
+      tr = warp_top(tr);
+      const float im = tm < kNoScale ? 0.0f : __fdiv_rn(kTop, tm), ir = tr < kNoScale ? 0.0f : __fdiv_rn(kTop, tr);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = __fmul_rn(m[j], im);
+        r[j] = r[j] > 0.0f && ir > 0.0f ? fmaxf(__fmul_rn(r[j], ir), kTiny) : 0.0f;
+      }
+      const uint2 mq = to_e4m3(m), vq = to_e4m3(r);
+      uint8_t *mp_ = (uint8_t*)T.m + i, *vp = (uint8_t*)T.v + i;
+      if (nv == 8) {
+        __stcs(reinterpret_cast<uint2*>(mp_), mq);
+        __stcs(reinterpret_cast<uint2*>(vp), vq);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < nv) {
+            mp_[j] = (uint8_t)((j < 4 ? mq.x : mq.y) >> (8 * (j & 3)));
+            vp[j] = (uint8_t)((j < 4 ? vq.x : vq.y) >> (8 * (j & 3)));
+          }
+      }
+      if ((threadIdx.x & 31) == 0) {
         T.m_scale[b] = tm < kNoScale ? 0.0f : __fdiv_rn(tm, kTop);
         T.v_scale[b] = tr < kNoScale ? 0.0f : __fdiv_rn(tr, kTop);
       }
     }
+  });
+}
+
+// Blocks of `kernel` that are resident at once on the current device, asked once per device and kernel.
+int resident_blocks(const void* kernel, int* out) {
+  static std::mutex mu;
+  static std::map<std::pair<int, const void*>, int> cache;
+  int dev = 0;
+  MP_CUDA_TRY(cudaGetDevice(&dev));
+  std::lock_guard<std::mutex> lock(mu);
+  int& have = cache[{dev, kernel}];
+  if (have == 0) {
+    int sms = 0, per = 0;
+    MP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    MP_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kThreads, 0));
+    have = sms * (per < 1 ? 1 : per);
   }
+  *out = have;
+  return MP_OK;
 }
 
 }  // namespace
 
 struct mp_adamw_plan {
   Tensor* d_tensors;
-  Piece* d_pieces;
-  int64_t n_pieces;
+  int n_tensors;                                // with elements
+  int64_t n_blocks;
   int bits;
 };
 
@@ -163,30 +266,27 @@ int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const*
         !mp::aligned16(w16[i]) ||
         (state_bits == 8 && (((uintptr_t)m_scale[i] | (uintptr_t)v_scale[i]) & 3)))
       return mp::set_error(MP_ERR_ALIGNMENT, "%s: tensor %d is not 16-byte aligned (scales: 4)", name, i);
-    if ((count[i] + kBlock - 1) / kBlock > INT32_MAX)
-      return mp::set_error(MP_ERR_TOO_LARGE, "%s: tensor %d is too large", name, i);
   }
   if (int rc = mp::check_device()) return rc;
   mp_adamw_plan* p = new (std::nothrow) mp_adamw_plan();
   if (!p) return mp::set_error(MP_ERR_NOMEM, "%s: host allocation failed", name);
   p->bits = state_bits;
   try {
-    std::vector<Tensor> ts(n);
-    std::vector<Piece> ps;
-    for (int i = 0; i < n; ++i) {
-      ts[i] = Tensor{(const uint16_t*)g16[i], (float*)w32[i], m[i], v[i], (uint16_t*)w16[i],
-                     m_scale ? m_scale[i] : nullptr, v_scale ? v_scale[i] : nullptr, count[i], decay ? decay[i] : 1.0f};
-      for (int64_t b = 0; b < (count[i] + kBlock - 1) / kBlock; ++b) ps.push_back(Piece{i, (int32_t)b});
+    std::vector<Tensor> ts;
+    for (int i = 0; i < n; ++i) {                // a tensor without elements has no place in the table
+      if (count[i] == 0) continue;
+      p->n_blocks += (count[i] + kBlock - 1) / kBlock;
+      ts.push_back(Tensor{(const uint16_t*)g16[i], (float*)w32[i], m[i], v[i], (uint16_t*)w16[i],
+                          m_scale ? m_scale[i] : nullptr, v_scale ? v_scale[i] : nullptr, count[i], p->n_blocks,
+                          decay ? decay[i] : 1.0f});
     }
-    p->n_pieces = (int64_t)ps.size();
-    if (cudaMalloc(&p->d_tensors, n * sizeof(Tensor)) != cudaSuccess ||
-        cudaMalloc(&p->d_pieces, (ps.size() ? ps.size() : 1) * sizeof(Piece)) != cudaSuccess) {
+    p->n_tensors = (int)ts.size();
+    const size_t bytes = ts.size() * sizeof(Tensor);
+    if (cudaMalloc(&p->d_tensors, bytes ? bytes : 1) != cudaSuccess) {
       mp_adamw_plan_destroy(p);
       return mp::set_error(MP_ERR_NOMEM, "%s: device allocation failed", name);
     }
-    cudaError_t e = cudaMemcpy(p->d_tensors, ts.data(), n * sizeof(Tensor), cudaMemcpyHostToDevice);
-    if (e == cudaSuccess && !ps.empty())
-      e = cudaMemcpy(p->d_pieces, ps.data(), ps.size() * sizeof(Piece), cudaMemcpyHostToDevice);
+    const cudaError_t e = bytes ? cudaMemcpy(p->d_tensors, ts.data(), bytes, cudaMemcpyHostToDevice) : cudaSuccess;
     if (e != cudaSuccess) {
       mp_adamw_plan_destroy(p);
       return mp::set_error(MP_ERR_CUDA, "%s: %s", name, cudaGetErrorString(e));
@@ -202,7 +302,6 @@ int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const*
 int mp_adamw_plan_destroy(mp_adamw_plan* p) {
   if (!p) return MP_OK;
   cudaFree(p->d_tensors);
-  cudaFree(p->d_pieces);
   delete p;
   return MP_OK;
 }
@@ -212,21 +311,26 @@ int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config*
   if (check_mode != 0 && check_mode != 1)
     return mp::set_error(MP_ERR_INVALID_ARG, "mp_adamw_update: check_mode must be 0 or 1");
   if (int rc = mp::check_device()) return rc;
-  if (plan->n_pieces == 0) return MP_OK;
+  if (plan->n_blocks == 0) return MP_OK;
   cudaStream_t st = (cudaStream_t)stream;
   int* gemm_status = nullptr;
   if (int rc = mp::gemm_status_device_ptr(&gemm_status)) return rc;
-  const int grid = (int)(plan->n_pieces < 148 * 8 ? plan->n_pieces : 148 * 8);
+  // one resident round of blocks; a block has work for each of its warps
+  auto grid_of = [&](const void* kernel, int* grid) {
+    if (int rc = resident_blocks(kernel, grid)) return rc;
+    const int64_t want = (plan->n_blocks + kThreads / 32 - 1) / (kThreads / 32);
+    if (want < *grid) *grid = (int)want;
+    return (int)MP_OK;
+  };
+  int grid = 0;
   if (check_mode == 1) {
-    mp_adamw_check_kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->d_pieces, plan->n_pieces, state->dev);
+    if (int rc = grid_of((const void*)mp_adamw_check_kernel, &grid)) return rc;
+    mp_adamw_check_kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, state->dev);
     mp::count_launch();
   }
-  if (plan->bits == 32)
-    mp_adamw_update_kernel<32><<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->d_pieces, plan->n_pieces, state->dev,
-                                                          *opt, gemm_status);
-  else
-    mp_adamw_update_kernel<8><<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->d_pieces, plan->n_pieces, state->dev,
-                                                         *opt, gemm_status);
+  auto kernel = plan->bits == 32 ? mp_adamw_update_kernel<32> : mp_adamw_update_kernel<8>;
+  if (int rc = grid_of((const void*)kernel, &grid)) return rc;
+  kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, state->dev, *opt, gemm_status);
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
   return MP_OK;
