@@ -1,7 +1,10 @@
 // AdamW over the tensors of a plan, states in 32 or in 8 bits, on the FP32 master.
 //
 // As in the Adam update beside it every operation is one individually rounded FP32 operation, so the
-// result does not depend on what the compiler would contract.
+// result does not depend on what the compiler would contract.  With 8-bit states, where the kernel moves
+// 16 B a parameter and instructions weigh as much as memory, that holds for the moments alone: an E4M3 code
+// may turn on their last bit.  The quotient of the step is taken from the hardware's approximation (off by
+// about 2^-22 of a step, far below the last bit of the weight).
 
 #include <cuda_fp8.h>
 #include <math.h>
@@ -10,6 +13,7 @@
 #include <map>
 #include <mutex>
 #include <new>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -23,16 +27,12 @@ constexpr float kTop = 448.0f;                  // largest E4M3 number
 constexpr float kTiny = 0.001953125f;           // smallest E4M3 number above 0, 2^-9
 constexpr float kNoScale = 7.888609052210118e-31f;   // 2^-100
 
-struct Tensor {
-  const uint16_t* g16;
-  float* w32;
-  void* m;
-  void* v;
-  uint16_t* w16;
-  float* m_scale;
-  float* v_scale;
-  int64_t count;
-  int64_t block_end;                            // blocks of this tensor and of those before it
+// A tensor of the plan.  Blocks of all tensors are numbered through; the addresses are those that the tensors'
+// buffers would have if they began at block 0, so that block x lies at address + x * (bytes of a block).
+struct alignas(16) Tensor {
+  uint64_t g16, w32, m, v, w16, m_scale, v_scale;
+  int64_t end;                                  // first block * 256 + elements
+  int64_t block_end;                            // number of the first block after it
   float decay;
 };
 struct Coef {
@@ -63,14 +63,25 @@ __device__ __forceinline__ Coef coefficients(const mp_dev_state* st, const mp_ad
   return c;
 }
 
-// One element: m and v in, m, v and r = sqrt(v) out; w is stepped.
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// One element: m and v in, m, v and r = sqrt(v) out; w is stepped.  decay: lr weight_decay of the tensor.
+template <int BITS>
 __device__ __forceinline__ void step_one(float g16f, float& w, float& m, float& v, float& r, float decay, const Coef& c) {
   const float g = __fmul_rn(g16f, c.inv_s);
   m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.omb1, g));
   v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.omb2, __fmul_rn(g, g)));
   r = __fsqrt_rn(v);
-  w = __fsub_rn(w, __fmul_rn(decay, w));
-  w = __fsub_rn(w, __fmul_rn(c.alpha, __fdiv_rn(m, __fadd_rn(__fmul_rn(r, c.k2), c.eps))));
+  if constexpr (BITS == 32) {
+    w = __fsub_rn(w, __fmul_rn(decay, w));
+    w = __fsub_rn(w, __fmul_rn(c.alpha, __fdiv_rn(m, __fadd_rn(__fmul_rn(r, c.k2), c.eps))));
+  } else {
+    w = fmaf(-decay, w, w);
+    w = fmaf(-c.alpha, m * rcp_approx(fmaf(r, c.k2, c.eps)), w);
+  }
 }
 
 // Eight E4M3 numbers as loaded.
@@ -96,126 +107,260 @@ __device__ __forceinline__ float warp_top(float v) {
   return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v)));
 }
 
-// The blocks of 256 elements that a thread block owns are one contiguous range; its warps take them in turn.
-// `f` gets the tensor, the block's number in it and the elements of this lane (0 .. 8).
-template <class F>
-__device__ __forceinline__ void for_my_blocks(const Tensor* tensors, int n_tensors, int64_t n_blocks, F f) {
-  const int64_t per = (n_blocks + gridDim.x - 1) / gridDim.x, begin = blockIdx.x * per;
-  const int64_t end = begin + per < n_blocks ? begin + per : n_blocks;
-  int64_t x = begin + (threadIdx.x >> 5);
-  if (x >= end) return;
-  int lo = 0;                                   // first tensor whose blocks end after x (the last one's end after all)
-  for (int hi = n_tensors - 1; lo < hi;) {
-    const int mid = (lo + hi) / 2;
-    if (__ldg(&tensors[mid].block_end) > x) hi = mid;
-    else lo = mid + 1;
+// A warp takes the blocks w, w + step, ... of the plan, w its number among the step warps of the grid, so that
+// neighbouring warps stream neighbouring memory.  A Cursor walks them.
+struct Cursor {
+  const Tensor* tensors;
+  int64_t x, step, n_blocks;
+  int at = 0, n_tensors;                        // the tensor that holds block x
+  __device__ __forceinline__ Cursor(const Tensor* table, int n, int64_t blocks)
+      : tensors(table), x((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)),
+        step((int64_t)gridDim.x * (kThreads / 32)), n_blocks(blocks), n_tensors(n) {
+    if (more()) seek(0, n_tensors - 1);
   }
-  for (; x < end; x += kThreads / 32) {
-    while (__ldg(&tensors[lo].block_end) <= x) ++lo;
-    const Tensor& T = tensors[lo];
-    const int64_t b = x - (__ldg(&T.block_end) - (__ldg(&T.count) + kBlock - 1) / kBlock);
-    const int64_t left = __ldg(&T.count) - b * kBlock - (threadIdx.x & 31) * 8;
-    f(T, b, left >= 8 ? 8 : left < 0 ? 0 : (int)left);
+  __device__ __forceinline__ bool more() const { return x < n_blocks; }
+  __device__ __forceinline__ void next() {
+    x += step;
+    if (!more() || __ldg(&tensors[at].block_end) > x) return;
+    // most often one of the next 32 tensors
+    const int lane = threadIdx.x & 31, hi = n_tensors - 1, probe = at + 1 + lane < hi ? at + 1 + lane : hi;
+    const unsigned after = __ballot_sync(0xFFFFFFFFu, __ldg(&tensors[probe].block_end) > x);
+    if (after) at = at + __ffs(after) < hi ? at + __ffs(after) : hi;
+    else seek(at + 33, hi);
   }
+  // the first tensor in lo .. hi whose blocks end after x (hi's do): 32 probes at a time
+  __device__ __forceinline__ void seek(int lo, int hi) {
+    const int lane = threadIdx.x & 31;
+    for (;;) {
+      const int stride = (hi - lo) / 32 + 1, probe = lo + lane * stride < hi ? lo + lane * stride : hi;
+      const unsigned after = __ballot_sync(0xFFFFFFFFu, __ldg(&tensors[probe].block_end) > x);
+      const int first = after ? __ffs(after) - 1 : 32;   // lane whose probe is the first that ends after x
+      const int top = lo + first * stride;
+      if (stride == 1) {
+        at = top < hi ? top : hi;
+        return;
+      }
+      hi = top < hi ? top : hi;
+      if (first > 0) lo = lo + (first - 1) * stride + 1;
+    }
+  }
+  // how many elements of the block lie inside the tensor
+  __device__ __forceinline__ int inside(const Tensor& T) const {
+    const int64_t left = __ldg(&T.end) - x * kBlock;
+    return left < kBlock ? (int)left : kBlock;
+  }
+};
+// A lane takes two quads of a block.  With 32-bit states they are 128 elements apart, so that each access of
+// a warp is one contiguous piece; with 8-bit states they are neighbours, so that a lane's eight codes are one access.
+// (1e8 parameters: 32 bits 457 us against 530 with neighbours, 8 bits 359 against 340.)
+template <int BITS>
+__device__ __forceinline__ int quad_at(int h) {
+  const int lane = threadIdx.x & 31;
+  return BITS == 32 ? lane * 4 + 128 * h : lane * 8 + 4 * h;
+}
+// Address of quad h (0, 1) of elements of `size` bytes in block x, and how many of its elements are inside.
+template <class P, int BITS>
+__device__ __forceinline__ P* lane_at(uint64_t base, int64_t x, int size, int h) {
+  return reinterpret_cast<P*>(base + x * (kBlock * size) + quad_at<BITS>(h) * size);
+}
+template <int BITS>
+__device__ __forceinline__ int quad(int inside, int h) {
+  const int n = inside - quad_at<BITS>(h);
+  return n < 0 ? 0 : n < 4 ? n : 4;
 }
 
 __global__ void __launch_bounds__(kThreads)
 mp_adamw_check_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, mp_dev_state* st) {
   bool bad = false;
-  for_my_blocks(tensors, n_tensors, n_blocks, [&](const Tensor& T, int64_t b, int nv) {
-    rows::Raw8<uint16_t> g;
-    g.load(T.g16 + b * kBlock + (threadIdx.x & 31) * 8, nv);
-    auto both = [](uint32_t v) { return (v & 0x7C00u) == 0x7C00u || (v & 0x7C000000u) == 0x7C000000u; };
-    bad |= both(g.q.x) || both(g.q.y) || both(g.q.z) || both(g.q.w);
-  });
+  for (Cursor cur(tensors, n_tensors, n_blocks); cur.more(); cur.next()) {
+    const Tensor& T = cur.tensors[cur.at];
+    const int inside = cur.inside(T);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint16_t* g = lane_at<const uint16_t, 32>(__ldg(&T.g16), cur.x, 2, h);
+      const int nv = quad<32>(inside, h);
+      auto both = [](uint32_t v) { return (v & 0x7C00u) == 0x7C00u || (v & 0x7C000000u) == 0x7C000000u; };
+      if (nv == 4) {
+        const uint2 q = __ldcs(reinterpret_cast<const uint2*>(g));
+        bad |= both(q.x) || both(q.y);
+      } else {
+        for (int j = 0; j < nv; ++j) bad |= rows::nonfinite16(g[j]);
+      }
+    }
+  }
   if (bad) atomicOr(&st->h.found_inf, 1);
 }
 
-// A lane takes 8 consecutive elements, so a warp takes a block of 256 that shares one scale and finds the
-// block's largest magnitude among its own registers: the states are read and written once, in place.
+// A warp takes a block of 256, which shares one scale, and finds the block's largest magnitude among its own
+// registers: the states are read and written once, in place.  The loads of the warp's next block are
+// issued before a block is worked on.
+__device__ __forceinline__ float4 get4(const float* p, int nv) {      // zeros for what lies past the tensor's end
+  if (nv == 4) return __ldcs(reinterpret_cast<const float4*>(p));
+  return make_float4(nv > 0 ? p[0] : 0.0f, nv > 1 ? p[1] : 0.0f, nv > 2 ? p[2] : 0.0f, 0.0f);
+}
+__device__ __forceinline__ uint2 get4(const uint16_t* p, int nv) {
+  if (nv == 4) return __ldcs(reinterpret_cast<const uint2*>(p));
+  return make_uint2((nv > 0 ? p[0] : 0u) | (nv > 1 ? p[1] : 0u) << 16, nv > 2 ? p[2] : 0u);
+}
+__device__ __forceinline__ uint32_t get4(const uint8_t* p, int nv) {
+  if (nv == 4) return __ldcs(reinterpret_cast<const uint32_t*>(p));
+  return (nv > 0 ? p[0] : 0u) | (nv > 1 ? p[1] : 0u) << 8 | (nv > 2 ? p[2] : 0u) << 16;
+}
+// What a lane holds of a block's states.
+template <int BITS> struct States;
+template <> struct States<32> {
+  float4 m[2], v[2];
+  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside) {
+    const uint64_t pm = __ldg(&T.m), pv = __ldg(&T.v);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      m[h] = get4(lane_at<const float, 32>(pm, x, 4, h), quad<32>(inside, h));
+      v[h] = get4(lane_at<const float, 32>(pv, x, 4, h), quad<32>(inside, h));
+    }
+  }
+};
+template <> struct States<8> {
+  uint2 m, v;
+  float ms, vs;
+  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside) {
+    const uint8_t *pm = lane_at<const uint8_t, 8>(__ldg(&T.m), x, 1, 0), *pv = lane_at<const uint8_t, 8>(__ldg(&T.v), x, 1, 0);
+    if (inside >= kBlock) {
+      m = __ldcs(reinterpret_cast<const uint2*>(pm));
+      v = __ldcs(reinterpret_cast<const uint2*>(pv));
+    } else {
+      m = make_uint2(get4(pm, quad<8>(inside, 0)), get4(pm + 4, quad<8>(inside, 1)));
+      v = make_uint2(get4(pv, quad<8>(inside, 0)), get4(pv + 4, quad<8>(inside, 1)));
+    }
+    ms = __ldcs(reinterpret_cast<const float*>(__ldg(&T.m_scale)) + x);
+    vs = __ldcs(reinterpret_cast<const float*>(__ldg(&T.v_scale)) + x);
+  }
+};
 template <int BITS>
-__global__ void __launch_bounds__(kThreads)
+struct Held {
+  uint2 g[2];
+  float4 w[2];
+  States<BITS> s;
+  const Tensor* T;
+  int64_t x;
+  int inside;
+  __device__ __forceinline__ void load(const Cursor& cur) {
+    T = cur.tensors + cur.at;
+    x = cur.x;
+    inside = cur.inside(*T);
+    const uint64_t pg = __ldg(&T->g16), pw = __ldg(&T->w32);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      g[h] = get4(lane_at<const uint16_t, BITS>(pg, x, 2, h), quad<BITS>(inside, h));
+      w[h] = get4(lane_at<const float, BITS>(pw, x, 4, h), quad<BITS>(inside, h));
+    }
+    s.load(*T, x, inside);
+  }
+};
+__device__ __forceinline__ void spread(const float4 (&q)[2], float (&f)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f[4 * h] = q[h].x; f[4 * h + 1] = q[h].y; f[4 * h + 2] = q[h].z; f[4 * h + 3] = q[h].w;
+  }
+}
+__device__ __forceinline__ void put4(float* p, const float* f, int nv) {
+  if (nv == 4) __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
+  else
+    for (int j = 0; j < nv; ++j) p[j] = f[j];
+}
+__device__ __forceinline__ void put4(uint16_t* p, const float* f, int nv) {
+  if (nv == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(rows::pack2(f[0], f[1]), rows::pack2(f[2], f[3])));
+  else
+    for (int j = 0; j < nv; ++j) p[j] = rows::f2h(f[j]);
+}
+__device__ __forceinline__ void put4(uint8_t* p, uint32_t q, int nv) {
+  if (nv == 4) __stcs(reinterpret_cast<uint32_t*>(p), q);
+  else
+    for (int j = 0; j < nv; ++j) p[j] = (uint8_t)(q >> (8 * j));
+}
+
+template <int BITS>
+__global__ void __launch_bounds__(kThreads, BITS == 32 ? 2 : 3)
 mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, const mp_dev_state* st, mp_adamw_config o,
                        const int* gemm_status) {
   if (st->h.found_inf != 0 || st->h.status != 0 || *gemm_status != 0) return;
   __shared__ Coef s_c;
-  if (threadIdx.x == 0) s_c = coefficients(st, o);
+  Cursor cur(tensors, n_tensors, n_blocks);
+  Held<BITS> next;
+  if (cur.more()) next.load(cur);
+  if (threadIdx.x == kThreads - 1) s_c = coefficients(st, o);
   __syncthreads();
   const Coef c = s_c;
-  for_my_blocks(tensors, n_tensors, n_blocks, [&](const Tensor& T, int64_t b, int nv) {
-    const int64_t i = b * kBlock + (threadIdx.x & 31) * 8;
-    rows::Raw8<uint16_t> gr;
-    rows::Raw8<float> wr;
+  while (cur.more()) {
+    const Held<BITS> held = next;
+    cur.next();
+    if (cur.more()) next.load(cur);
+    const Tensor& T = *held.T;
+    const int64_t x = held.x;
+    const int inside = held.inside;
     float g[8], w[8], m[8], v[8], r[8];
-    gr.load(T.g16 + i, nv);
-    wr.load(T.w32 + i, nv);
+    rows::Raw8<uint16_t> gr;
+    gr.q = make_uint4(held.g[0].x, held.g[0].y, held.g[1].x, held.g[1].y);
+    gr.floats(g);
+    spread(held.w, w);
     if constexpr (BITS == 32) {
-      rows::Raw8<float> mr, vr;
-      mr.load((const float*)T.m + i, nv);
-      vr.load((const float*)T.v + i, nv);
-      mr.floats(m);
-      vr.floats(v);
+      spread(held.s.m, m);
+      spread(held.s.v, v);
     } else {
-      uint2 mq = make_uint2(0, 0), vq = mq;
-      if (nv > 0) {
-        mq = __ldcs(reinterpret_cast<const uint2*>((const uint8_t*)T.m + i));
-        vq = __ldcs(reinterpret_cast<const uint2*>((const uint8_t*)T.v + i));
-      }
-      const float ms = T.m_scale[b], vs = T.v_scale[b];
-      from_e4m3(mq, m);
-      from_e4m3(vq, r);
+      from_e4m3(held.s.m, m);
+      from_e4m3(held.s.v, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        m[j] = __fmul_rn(m[j], ms);
-        r[j] = __fmul_rn(r[j], vs);
+        m[j] = __fmul_rn(m[j], held.s.ms);
+        r[j] = __fmul_rn(r[j], held.s.vs);
         v[j] = __fmul_rn(r[j], r[j]);
       }
     }
-    gr.floats(g);
-    wr.floats(w);
-    const float decay = __fmul_rn(c.decay, T.decay);
+    const float decay = __fmul_rn(c.decay, __ldg(&T.decay));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) step_one(g[j], w[j], m[j], v[j], r[j], decay, c);
-    rows::store8(T.w32 + i, w, nv);
-    rows::store8(T.w16 + i, w, nv);
-    if constexpr (BITS == 32) {
-      rows::store8((float*)T.m + i, m, nv);
-      rows::store8((float*)T.v + i, v, nv);
-    } else {
-      // what lies past the tensor's end has no say in the scale and is not stored
-      float tm = 0.0f, tr = 0.0f;
+    for (int j = 0; j < 8; ++j) step_one<BITS>(g[j], w[j], m[j], v[j], r[j], decay, c);
+    uint2 mq = make_uint2(0, 0), vq = mq;
+    if constexpr (BITS == 8) {
+      float tm = 0.0f, tr = 0.0f;               // elements past the tensor's end are zero
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        tm = j < nv ? fmaxf(tm, fabsf(m[j])) : tm;
-        tr = j < nv ? fmaxf(tr, r[j]) : tr;
+        tm = fmaxf(tm, fabsf(m[j]));
+        tr = fmaxf(tr, r[j]);
       }
       tm = warp_top(tm);
       tr = warp_top(tr);
-      const float im = tm < kNoScale ? 0.0f : __fdiv_rn(kTop, tm), ir = tr < kNoScale ? 0.0f : __fdiv_rn(kTop, tr);
+      const float im = tm < kNoScale ? 0.0f : __fmul_rn(__frcp_rn(tm), kTop);
+      const float ir = tr < kNoScale ? 0.0f : __fmul_rn(__frcp_rn(tr), kTop);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         m[j] = __fmul_rn(m[j], im);
-        r[j] = r[j] > 0.0f && ir > 0.0f ? fmaxf(__fmul_rn(r[j], ir), kTiny) : 0.0f;
+        r[j] = __fmul_rn(r[j], ir);
+        r[j] = r[j] > 0.0f ? fmaxf(r[j], kTiny) : r[j];
       }
-      const uint2 mq = to_e4m3(m), vq = to_e4m3(r);
-      uint8_t *mp_ = (uint8_t*)T.m + i, *vp = (uint8_t*)T.v + i;
-      if (nv == 8) {
-        __stcs(reinterpret_cast<uint2*>(mp_), mq);
-        __stcs(reinterpret_cast<uint2*>(vp), vq);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < nv) {
-            mp_[j] = (uint8_t)((j < 4 ? mq.x : mq.y) >> (8 * (j & 3)));
-            vp[j] = (uint8_t)((j < 4 ? vq.x : vq.y) >> (8 * (j & 3)));
-          }
-      }
+      mq = to_e4m3(m);
+      vq = to_e4m3(r);
       if ((threadIdx.x & 31) == 0) {
-        T.m_scale[b] = tm < kNoScale ? 0.0f : __fdiv_rn(tm, kTop);
-        T.v_scale[b] = tr < kNoScale ? 0.0f : __fdiv_rn(tr, kTop);
+        reinterpret_cast<float*>(__ldg(&T.m_scale))[x] = tm < kNoScale ? 0.0f : __fmul_rn(tm, 1.0f / kTop);
+        reinterpret_cast<float*>(__ldg(&T.v_scale))[x] = tr < kNoScale ? 0.0f : __fmul_rn(tr, 1.0f / kTop);
       }
     }
-  });
+    const uint64_t pw = __ldg(&T.w32), pw16 = __ldg(&T.w16), pm = __ldg(&T.m), pv = __ldg(&T.v);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int nv = quad<BITS>(inside, h);
+      put4(lane_at<float, BITS>(pw, x, 4, h), w + 4 * h, nv);
+      put4(lane_at<uint16_t, BITS>(pw16, x, 2, h), w + 4 * h, nv);
+      if constexpr (BITS == 32) {
+        put4(lane_at<float, BITS>(pm, x, 4, h), m + 4 * h, nv);
+        put4(lane_at<float, BITS>(pv, x, 4, h), v + 4 * h, nv);
+      } else if (inside < kBlock) {
+        put4(lane_at<uint8_t, BITS>(pm, x, 1, h), h ? mq.y : mq.x, nv);
+        put4(lane_at<uint8_t, BITS>(pv, x, 1, h), h ? vq.y : vq.x, nv);
+      } else if (h == 0) {
+        __stcs(lane_at<uint2, BITS>(pm, x, 1, 0), mq);
+        __stcs(lane_at<uint2, BITS>(pv, x, 1, 0), vq);
+      }
+    }
+  }
 }
 
 // Blocks of `kernel` that are resident at once on the current device, asked once per device and kernel.
@@ -275,10 +420,14 @@ int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const*
     std::vector<Tensor> ts;
     for (int i = 0; i < n; ++i) {                // a tensor without elements has no place in the table
       if (count[i] == 0) continue;
+      const int64_t first = p->n_blocks;
       p->n_blocks += (count[i] + kBlock - 1) / kBlock;
-      ts.push_back(Tensor{(const uint16_t*)g16[i], (float*)w32[i], m[i], v[i], (uint16_t*)w16[i],
-                          m_scale ? m_scale[i] : nullptr, v_scale ? v_scale[i] : nullptr, count[i], p->n_blocks,
-                          decay ? decay[i] : 1.0f});
+      auto from_block_0 = [&](const void* q, int64_t block_bytes) { return (uint64_t)q - (uint64_t)(first * block_bytes); };
+      const int64_t state = state_bits == 32 ? 4 * kBlock : kBlock;
+      ts.push_back(Tensor{from_block_0(g16[i], 2 * kBlock), from_block_0(w32[i], 4 * kBlock), from_block_0(m[i], state),
+                          from_block_0(v[i], state), from_block_0(w16[i], 2 * kBlock),
+                          m_scale ? from_block_0(m_scale[i], 4) : 0, v_scale ? from_block_0(v_scale[i], 4) : 0,
+                          first * kBlock + count[i], p->n_blocks, decay ? decay[i] : 1.0f});
     }
     p->n_tensors = (int)ts.size();
     const size_t bytes = ts.size() * sizeof(Tensor);
