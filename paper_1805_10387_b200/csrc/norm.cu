@@ -8,126 +8,16 @@
 
 namespace {
 
-// ---------------------------------------------------------------- forward
-//
-// A row belongs to a group of TPR threads, each with C vectors of 8 elements, so the row stays in
-// registers between the two norms: x and y are read once and x_out and n written once.  8 B an element
-// (FP16 residual, shared gate) against some 20 FP32 operations: HBM bounds it.
-constexpr int kFwdThreads = 256;
-
-template <class XT, int TPR, int C>
-__global__ void __launch_bounds__(TPR > kFwdThreads ? TPR : kFwdThreads)
-mp_block_norm_fwd_kernel(int kind, float eps, float res_scale, const XT* x, int64_t ldx, const uint16_t* y, int64_t ldy,
-                         const uint16_t* g_post, const uint16_t* gate, int64_t ldgate, XT* x_out, int64_t ldxo,
-                         const uint16_t* g_pre, uint16_t* nn, int64_t ldn, float* stats, int64_t M, int D) {
-  constexpr int THREADS = TPR > kFwdThreads ? TPR : kFwdThreads, G = THREADS / TPR;
-  __shared__ float red_all[G][32];
-  const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
-  float* red = red_all[group];
-  int parity = 0;
-  const int64_t m = (int64_t)blockIdx.x * G + group;
-  // groups of part of a warp stay until the shuffles are over; larger groups may leave
-  const bool live = m < M;
-  if (TPR >= 32 && !live) return;
-  const float inv_d = 1.0f / (float)D;
-  int nv[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int left = D - (c * TPR + t) * 8;
-    nv[c] = !live || left < 0 ? 0 : left < 8 ? left : 8;
-  }
-  rows::Raw8<XT> xr[C];
-  rows::Raw8<uint16_t> yr[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) xr[c].load(x + m * ldx + (c * TPR + t) * 8, nv[c]);
-  // mean and 1/sqrt of a row that `at` gives chunk by chunk
-  auto moments = [&](auto at, float& mean, float& root) {
-    float s[1] = {0.0f};
-    mean = 0.0f;
-    if (kind == MP_NORM_LAYER) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float f[8];
-        at(c, f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[0] += f[j];
-      }
-      rows::group_sum<TPR, 1>(s, red, parity);
-      mean = s[0] * inv_d;
-    }
-    float q[1] = {0.0f};
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float f[8];
-      at(c, f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = f[j] - mean;
-        if (nv[c] == 8 || j < nv[c]) q[0] = fmaf(v, v, q[0]);
-      }
-    }
-    rows::group_sum<TPR, 1>(q, red, parity);
-    root = rsqrtf(fmaf(q[0], inv_d, eps));
-  };
-  float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float xo[C][8];
-#pragma unroll
-  for (int c = 0; c < C; ++c) xr[c].floats(xo[c]);
-  if (g_post != nullptr) {
-#pragma unroll
-    for (int c = 0; c < C; ++c) yr[c].load(y + m * ldy + (c * TPR + t) * 8, nv[c]);
-    moments([&](int c, float (&f)[8]) { yr[c].floats(f); }, st.x, st.y);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (nv[c] == 0) continue;
-      const int col = (c * TPR + t) * 8;
-      rows::Raw8<uint16_t> gr;
-      float f[8], gp[8];
-      yr[c].floats(f);
-      gr.load_cached(g_post + col, nv[c]);
-      gr.floats(gp);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = (f[j] - st.x) * st.y * gp[j];
-      if (gate != nullptr) {
-        if (ldgate == 0) gr.load_cached(gate + col, nv[c]);
-        else gr.load(gate + m * ldgate + col, nv[c]);
-        gr.floats(gp);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] *= gp[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) xo[c][j] = fmaf(res_scale, xo[c][j], f[j]);
-      rows::store8(x_out + m * ldxo + col, xo[c], nv[c]);
-    }
-  }
-  moments([&](int c, float (&f)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = xo[c][j];
-  }, st.z, st.w);
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    if (nv[c] == 0) continue;
-    const int col = (c * TPR + t) * 8;
-    rows::Raw8<uint16_t> gr;
-    float gq[8];
-    gr.load_cached(g_pre + col, nv[c]);
-    gr.floats(gq);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) gq[j] *= (xo[c][j] - st.z) * st.w;
-    rows::store8(nn + m * ldn + col, gq, nv[c]);
-  }
-  if (stats != nullptr && t == 0 && live) reinterpret_cast<float4*>(stats)[m] = st;
-}
-
-// ---------------------------------------------------------------- backward
-//
-// Persistent blocks of 512 threads; a group of TPR threads walks the rows r, r + step, ...  Each
-// thread fetches its own vectors of the next rows (x_out, y, dn, dx_out, a gate matrix) into its
-// own slots of shared memory with asynchronous copies, so the loads of the following rows are in
-// flight while a row is worked on, and no thread waits for another's copy.  The sums over the rows
-// (dg_pre, dg_post, dgate) stay in the registers of the thread that owns the columns; at the end
-// the groups of a block add theirs in order through shared memory and the block writes one partial row.
-constexpr int kBwdThreads = 512;
+// Rows of up to 8192 elements, forward and backward: persistent blocks of 512 threads.  A group of TPR
+// threads, each with two vectors of 8 columns, walks the rows r, r + step, ...  Each thread fetches its own
+// vectors of the next rows into its own slots of shared memory with asynchronous copies (zeros for what
+// lies past the row), so the loads of the following rows are in flight while a row is worked on and no
+// thread waits for another's copy; the row stays in registers and shared memory between the norms, so
+// that everything is read once and written once.  What depends on the column alone (the gains, the
+// gate vector) stays in the thread's registers over all rows.
+// An element costs 8 B of HBM traffic forward and 12 B backward (FP16, shared gate) against some 17 and 36
+// instructions: HBM bounds both if the instructions stay few.
+constexpr int kRowThreads = 512, kC = 2;
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
@@ -139,6 +29,277 @@ __device__ __forceinline__ void copy_wait(int stages) {     // all but the newes
   else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
+// One array of rows that a kernel reads: its vectors c of this thread lie in the slots slot + c * XS.
+template <class T>
+struct Stream {
+  static constexpr int XS = sizeof(T) / 2;       // 16-byte slots of a vector
+  const T* row;                                  // this thread's first column in the row to fetch next
+  int64_t hop;                                   // elements from one of the group's rows to its next
+  int slot;
+  __device__ __forceinline__ Stream(const void* p, int64_t ld, int64_t first, int64_t step, int t, int& slots)
+      : row(static_cast<const T*>(p) + first * ld + t * 8), hop(step * ld), slot(slots) {
+    if (p != nullptr) slots += kC * XS;
+  }
+  template <int TPR>
+  __device__ __forceinline__ void fetch(uint32_t stage, const int (&nv)[kC], bool inside) {
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int h = 0; h < XS; ++h)
+        copy16(stage + (slot + c * XS + h) * (kRowThreads * 16), row + c * TPR * 8 + h * 4, inside && nv[c] > 4 * h);
+    row += hop;
+  }
+  __device__ __forceinline__ void read(const uint4* stage, int c, int nv, float (&f)[8]) const {
+    rows::Raw8<T> r;
+    uint4* q = reinterpret_cast<uint4*>(&r);
+#pragma unroll
+    for (int h = 0; h < XS; ++h) q[h] = stage[(slot + c * XS + h) * kRowThreads];
+    if (nv > 0 && nv < 8) r.keep(nv);            // a vector across the row's end: its padding may hold anything
+    r.floats(f);
+  }
+};
+
+// ---------------------------------------------------------------- forward
+struct FwdArgs {
+  float eps, res_scale;
+  const void* x; int64_t ldx;
+  const uint16_t* y; int64_t ldy;
+  const uint16_t *g_post, *gate; int64_t ldgate;
+  void* x_out; int64_t ldxo;
+  const uint16_t* g_pre;
+  uint16_t* n; int64_t ldn;
+  float* stats;
+  int64_t M;
+  int D;
+  int stages;      // rows in flight per group, the one at work included (2 .. 4)
+  int slots;       // 16-byte slots per thread and stage
+};
+
+// Sums of a vector's elements and of their squares about `mean`; of a vector across the row's end only what is inside.
+__device__ __forceinline__ void add_squares(const float (&f)[8], float mean, int nv, float& q) {
+  if (nv == 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q = fmaf(f[j] - mean, f[j] - mean, q);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < nv) q = fmaf(f[j] - mean, f[j] - mean, q);
+  }
+}
+template <int TPR, bool LAYER>
+__device__ __forceinline__ float2 moments(const float (&f)[kC][8], const int (&nv)[kC], float inv_d, float eps, float* red,
+                                          int& parity) {
+  float mean = 0.0f;
+  if constexpr (LAYER) {
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[0] += f[c][j];     // zeros past the row's end
+    rows::group_sum<TPR, 1>(s, red, parity);
+    mean = s[0] * inv_d;
+  }
+  float q[1] = {0.0f};
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    if constexpr (LAYER) {
+      add_squares(f[c], mean, nv[c], q[0]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[0] = fmaf(f[c][j], f[c][j], q[0]);
+    }
+  }
+  rows::group_sum<TPR, 1>(q, red, parity);
+  return make_float2(mean, rsqrtf(fmaf(q[0], inv_d, eps)));
+}
+
+template <class XT, int TPR, bool LAYER>
+__global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const FwdArgs a) {
+  constexpr int G = kRowThreads / TPR;
+  extern __shared__ uint4 slots[];
+  __shared__ float red_all[G][2 * 16];
+  const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  float* red = red_all[group];
+  int parity = 0, used = 0;
+  const bool has_y = a.g_post != nullptr, matrix = a.gate != nullptr && a.ldgate != 0;
+  const float inv_d = 1.0f / (float)a.D;
+  int nv[kC];
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    const int left = a.D - (c * TPR + t) * 8;
+    nv[c] = left < 0 ? 0 : left < 8 ? left : 8;
+  }
+  const int64_t step = (int64_t)gridDim.x * G, first = (int64_t)blockIdx.x * G + group;
+  // the row that decides when the loop ends: that of the warp's first group, so that a warp stays whole
+  const int64_t lead = TPR >= 32 ? first : (int64_t)blockIdx.x * G + (threadIdx.x & ~31) / TPR;
+  Stream<XT> sx(a.x, a.ldx, first, step, t, used);
+  Stream<uint16_t> sy(a.y, a.ldy, first, step, t, used), sg(matrix ? a.gate : nullptr, a.ldgate, first, step, t, used);
+  const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(slots)) + threadIdx.x * 16;
+  int64_t ahead = first;
+  auto fetch = [&](int stage) {
+    const bool inside = ahead < a.M;
+    if (TPR < 32 || inside) {
+      const uint32_t at = base + (uint32_t)(stage * a.slots) * (kRowThreads * 16);
+      sx.template fetch<TPR>(at, nv, inside);
+      if (has_y) sy.template fetch<TPR>(at, nv, inside);
+      if (matrix) sg.template fetch<TPR>(at, nv, inside);
+    }
+    ahead += step;
+    copy_commit();
+  };
+  for (int s = 0; s + 1 < a.stages; ++s) fetch(s);
+  float q[kC][8], gq[kC][8];                     // g_post * gate (a gate matrix comes with the row), g_pre
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    const int col = (c * TPR + t) * 8;
+    rows::Raw8<uint16_t> r;
+    r.load_cached(a.g_pre + col, nv[c]);
+    r.floats(gq[c]);
+    if (has_y) {
+      float g[8];
+      r.load_cached(a.g_post + col, nv[c]);
+      r.floats(q[c]);
+      if (a.gate != nullptr && !matrix) {
+        r.load_cached(a.gate + col, nv[c]);
+        r.floats(g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[c][j] *= g[j];
+      }
+    }
+  }
+  int stage = 0;
+  int64_t m = first;
+  for (int64_t lm = lead; lm < a.M; lm += step, m += step) {
+    const bool live = TPR >= 32 || m < a.M;
+    fetch(stage == 0 ? a.stages - 1 : stage - 1);        // the slots of the row before this one
+    copy_wait(a.stages);
+    const uint4* mine = slots + threadIdx.x + (int64_t)stage * a.slots * kRowThreads;
+    float xo[kC][8];
+    float2 my = make_float2(0.0f, 0.0f);
+    if (has_y) {
+      float y[kC][8];
+#pragma unroll
+      for (int c = 0; c < kC; ++c) sy.read(mine, c, nv[c], y[c]);
+      my = moments<TPR, LAYER>(y, nv, inv_d, a.eps, red, parity);
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        float g[8];
+        sx.read(mine, c, nv[c], xo[c]);
+        if (matrix) sg.read(mine, c, nv[c], g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float h = LAYER ? (y[c][j] - my.x) * my.y : y[c][j] * my.y;
+          xo[c][j] = fmaf(h, matrix ? q[c][j] * g[j] : q[c][j], a.res_scale * xo[c][j]);
+        }
+        if (live && nv[c] > 0)
+          rows::store8(reinterpret_cast<XT*>(a.x_out) + m * a.ldxo + (c * TPR + t) * 8, xo[c], nv[c]);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < kC; ++c) sx.read(mine, c, nv[c], xo[c]);
+    }
+    const float2 mx = moments<TPR, LAYER>(xo, nv, inv_d, a.eps, red, parity);
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) xo[c][j] = (LAYER ? xo[c][j] - mx.x : xo[c][j]) * mx.y * gq[c][j];
+      if (live && nv[c] > 0) rows::store8(a.n + m * a.ldn + (c * TPR + t) * 8, xo[c], nv[c]);
+    }
+    if (a.stats != nullptr && t == 0 && live) reinterpret_cast<float4*>(a.stats)[m] = make_float4(my.x, my.y, mx.x, mx.y);
+    stage = stage + 1 == a.stages ? 0 : stage + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// Longer rows: a block per row, the row in registers, one row after the other.
+template <class XT, bool LAYER>
+__global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_wide_kernel(const FwdArgs a) {
+  constexpr int TPR = kRowThreads, C = 4;
+  __shared__ float red[2 * 16];
+  int parity = 0;
+  const float inv_d = 1.0f / (float)a.D;
+  auto moments_of = [&](const float (&f)[C][8]) {
+    float mean = 0.0f;
+    if constexpr (LAYER) {
+      float s[1] = {0.0f};
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[0] += f[c][j];
+      rows::group_sum<TPR, 1>(s, red, parity);
+      mean = s[0] * inv_d;
+    }
+    float q[1] = {0.0f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int left = a.D - (c * TPR + (int)threadIdx.x) * 8;
+      add_squares(f[c], mean, left < 0 ? 0 : left < 8 ? left : 8, q[0]);
+    }
+    rows::group_sum<TPR, 1>(q, red, parity);
+    return make_float2(mean, rsqrtf(fmaf(q[0], inv_d, a.eps)));
+  };
+  for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
+    float xo[C][8];
+    float2 my = make_float2(0.0f, 0.0f);
+    rows::Raw8<XT> xr;
+    rows::Raw8<uint16_t> r;
+    auto col_of = [&](int c) { return (c * TPR + (int)threadIdx.x) * 8; };
+    auto nv_of = [&](int c) { const int left = a.D - col_of(c); return left < 0 ? 0 : left < 8 ? left : 8; };
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      xr.load(reinterpret_cast<const XT*>(a.x) + m * a.ldx + col_of(c), nv_of(c));
+      xr.floats(xo[c]);
+    }
+    if (a.g_post != nullptr) {
+      float y[C][8];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        r.load(a.y + m * a.ldy + col_of(c), nv_of(c));
+        r.floats(y[c]);
+      }
+      my = moments_of(y);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int col = col_of(c), nv = nv_of(c);
+        if (nv == 0) continue;
+        float g[8];
+        r.load_cached(a.g_post + col, nv);
+        r.floats(g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[c][j] = (y[c][j] - my.x) * my.y * g[j];
+        if (a.gate != nullptr) {
+          r.load(a.gate + m * a.ldgate + col, nv);
+          r.floats(g);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[c][j] *= g[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) xo[c][j] = fmaf(a.res_scale, xo[c][j], y[c][j]);
+        rows::store8(reinterpret_cast<XT*>(a.x_out) + m * a.ldxo + col, xo[c], nv);
+      }
+    }
+    const float2 mx = moments_of(xo);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = col_of(c), nv = nv_of(c);
+      if (nv == 0) continue;
+      float g[8];
+      r.load_cached(a.g_pre + col, nv);
+      r.floats(g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] *= (xo[c][j] - mx.x) * mx.y;
+      rows::store8(a.n + m * a.ldn + col, g, nv);
+    }
+    if (a.stats != nullptr && threadIdx.x == 0) reinterpret_cast<float4*>(a.stats)[m] = make_float4(my.x, my.y, mx.x, mx.y);
+  }
+}
+
+// ---------------------------------------------------------------- backward
+//
+// The sums over the rows stay in the registers of the thread that owns the columns: two of them, since
+// with a gate vector dg_post and dgate are the same sum S = sum gx yhat times a factor of the column
+// (dg_post = gate S, dgate = g_post S), and with a gate matrix dgate is no sum.  At the end the groups of a block
+// add theirs in order through shared memory and the block writes one partial row of each.
 struct BwdArgs {
   int kind;
   float res_scale;
@@ -154,168 +315,138 @@ struct BwdArgs {
   uint16_t* dgate; int64_t lddgate;
   int64_t M;
   int D;
-  float* partial;
+  float* partial;  // [block][2][D]
   int stages;      // rows in flight per group, the one at work included (2 .. 4)
   int slots;       // 16-byte slots per thread and stage
 };
 
-template <class XT, int TPR, int C>
-__global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_kernel(const BwdArgs a) {
-  constexpr int G = kBwdThreads / TPR, XS = sizeof(XT) / 2;      // XS: slots of one vector of the residual type
+template <class XT, int TPR, bool LAYER, bool MATRIX>
+__global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const BwdArgs a) {
+  constexpr int G = kRowThreads / TPR, N = LAYER ? 2 : 1;        // N: row sums that a norm's backward needs
   extern __shared__ uint4 slots[];
-  __shared__ float red_all[G][2 * 16 * 2];
+  __shared__ float red_all[G][2 * 16 * N];
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   float* red = red_all[group];
-  int parity = 0;
-  const bool has_y = a.g_post != nullptr, matrix = a.gate != nullptr && a.ldgate != 0, layer = a.kind == MP_NORM_LAYER;
-  const float inv_d = 1.0f / (float)a.D;
-  const XT* x_out = reinterpret_cast<const XT*>(a.x_out);
-  const XT* dx_out = reinterpret_cast<const XT*>(a.dx_out);
-  int nv[C];
+  int parity = 0, used = 0;
+  const bool has_y = a.g_post != nullptr, has_up = a.dx_out != nullptr;
+  const float inv_d = 1.0f / (float)a.D, res = has_y ? a.res_scale : 1.0f;
+  int nv[kC];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
+  for (int c = 0; c < kC; ++c) {
     const int left = a.D - (c * TPR + t) * 8;
     nv[c] = left < 0 ? 0 : left < 8 ? left : 8;
   }
   const int64_t step = (int64_t)gridDim.x * G, first = (int64_t)blockIdx.x * G + group;
-  // the row that decides when the loop ends: that of the warp's first group, so that a warp stays whole
   const int64_t lead = TPR >= 32 ? first : (int64_t)blockIdx.x * G + (threadIdx.x & ~31) / TPR;
+  Stream<XT> sx(a.x_out, a.ldxo, first, step, t, used), su(a.dx_out, a.lddxo, first, step, t, used);
+  Stream<uint16_t> sd(a.dn, a.lddn, first, step, t, used), sy(a.y, a.ldy, first, step, t, used),
+      sg(MATRIX ? a.gate : nullptr, a.ldgate, first, step, t, used);
   const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(slots)) + threadIdx.x * 16;
-  // slot order of a vector c: x_out (XS), dx_out (XS), dn, y, gate; slot s of a stage lies at s * threads
-  auto fetch = [&](int64_t m, int stage) {
-    if (m < a.M) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * 8;
-        uint32_t at = base + (uint32_t)(stage * a.slots + c * (a.slots / C)) * (kBwdThreads * 16);
-        auto next = [&] { const uint32_t r = at; at += kBwdThreads * 16; return r; };
-#pragma unroll
-        for (int h = 0; h < XS; ++h) copy16(next(), x_out + m * a.ldxo + col + 4 * h, nv[c] > 4 * h);
-        if (dx_out != nullptr)
-#pragma unroll
-          for (int h = 0; h < XS; ++h) copy16(next(), dx_out + m * a.lddxo + col + 4 * h, nv[c] > 4 * h);
-        copy16(next(), a.dn + m * a.lddn + col, nv[c] > 0);
-        if (has_y) copy16(next(), a.y + m * a.ldy + col, nv[c] > 0);
-        if (matrix) copy16(next(), a.gate + m * a.ldgate + col, nv[c] > 0);
-      }
+  int64_t ahead = first;
+  auto fetch = [&](int stage) {
+    const bool inside = ahead < a.M;
+    if (TPR < 32 || inside) {
+      const uint32_t at = base + (uint32_t)(stage * a.slots) * (kRowThreads * 16);
+      sx.template fetch<TPR>(at, nv, inside);
+      if (has_up) su.template fetch<TPR>(at, nv, inside);
+      sd.template fetch<TPR>(at, nv, inside);
+      if (has_y) sy.template fetch<TPR>(at, nv, inside);
+      if (MATRIX) sg.template fetch<TPR>(at, nv, inside);
     }
+    ahead += step;
     copy_commit();
   };
-  float s_pre[C][8] = {}, s_post[C][8] = {}, s_gate[C][8] = {};
-  for (int s = 0; s + 1 < a.stages; ++s) fetch(first + s * step, s);
+  for (int s = 0; s + 1 < a.stages; ++s) fetch(s);
+  float q[kC][8], gq[kC][8];                     // g_post * gate (a gate matrix comes with the row), g_pre
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    const int col = (c * TPR + t) * 8;
+    rows::Raw8<uint16_t> r;
+    r.load_cached(a.g_pre + col, nv[c]);
+    r.floats(gq[c]);
+    if (has_y) {
+      float g[8];
+      r.load_cached(a.g_post + col, nv[c]);
+      r.floats(q[c]);
+      if (!MATRIX && a.gate != nullptr) {
+        r.load_cached(a.gate + col, nv[c]);
+        r.floats(g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[c][j] *= g[j];
+      }
+    }
+  }
+  float s_pre[kC][8] = {}, s_y[kC][8] = {};
   int stage = 0;
   int64_t m = first;
   for (int64_t lm = lead; lm < a.M; lm += step, m += step) {
     const bool live = TPR >= 32 || m < a.M;
-    // the slots of the row before this one are free: fetch into them
-    fetch(m + (a.stages - 1) * step, stage == 0 ? a.stages - 1 : stage - 1);
-    copy_wait(a.stages);
+    fetch(stage == 0 ? a.stages - 1 : stage - 1);        // the slots of the row before this one
     const float4 st = live ? __ldg(reinterpret_cast<const float4*>(a.stats) + m) : make_float4(0, 0, 0, 0);
-    int nvr[C];
+    copy_wait(a.stages);
+    const uint4* mine = slots + threadIdx.x + (int64_t)stage * a.slots * kRowThreads;
+    float gx[kC][8], hat[kC][8];
+    float ab[N] = {};
 #pragma unroll
-    for (int c = 0; c < C; ++c) nvr[c] = live ? nv[c] : 0;
-    float gx[C][8], xhat[C][8], dn[C][8];
-    float ab[2] = {0.0f, 0.0f};
-    const uint4* mine = slots + threadIdx.x + (int64_t)stage * a.slots * kBwdThreads;
-    auto raw16 = [&](int c, int slot) {
-      rows::Raw8<uint16_t> r;
-      r.q = mine[(c * (a.slots / C) + slot) * kBwdThreads];
-      r.keep(nvr[c]);
-      return r;
-    };
-    auto rawx = [&](int c, int slot) {
-      rows::Raw8<XT> r;
-      uint4* q = reinterpret_cast<uint4*>(&r);
-#pragma unroll
-      for (int h = 0; h < XS; ++h) q[h] = mine[(c * (a.slots / C) + slot + h) * kBwdThreads];
-      r.keep(nvr[c]);
-      return r;
-    };
-    const int s_dn = dx_out != nullptr ? 2 * XS : XS;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float g[8];
-      rows::Raw8<uint16_t> gr;
-      rawx(c, 0).floats(xhat[c]);
-      raw16(c, s_dn).floats(dn[c]);
-      gr.load_cached(a.g_pre + (c * TPR + t) * 8, nv[c]);
-      gr.floats(g);
+    for (int c = 0; c < kC; ++c) {
+      float dn[8];
+      sx.read(mine, c, nv[c], hat[c]);
+      sd.read(mine, c, nv[c], dn);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        xhat[c][j] = (xhat[c][j] - st.z) * st.w;
-        const float d = dn[c][j] * g[j];
-        gx[c][j] = d;
-        ab[0] = fmaf(d, xhat[c][j], ab[0]);
-        ab[1] += d;
+        hat[c][j] = (LAYER ? hat[c][j] - st.z : hat[c][j]) * st.w;
+        gx[c][j] = dn[j] * gq[c][j];
+        s_pre[c][j] = fmaf(dn[j], hat[c][j], s_pre[c][j]);
+        ab[0] = fmaf(gx[c][j], hat[c][j], ab[0]);
+        if constexpr (LAYER) ab[1] += gx[c][j];
       }
     }
-    rows::group_sum<TPR, 2>(ab, red, parity);
-    const float sa = ab[0] * inv_d, sb = layer ? ab[1] * inv_d : 0.0f;
-    float ef[2] = {0.0f, 0.0f};
+    rows::group_sum<TPR, N>(ab, red, parity);
+    const float sa = ab[0] * inv_d;
+    float sb = 0.0f;
+    if constexpr (LAYER) sb = ab[1] * inv_d;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (nvr[c] == 0) continue;
+    for (int c = 0; c < kC; ++c) {
       float up[8] = {};
-      if (dx_out != nullptr) rawx(c, XS).floats(up);
+      if (has_up) su.read(mine, c, nv[c], up);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        s_pre[c][j] = fmaf(dn[c][j], xhat[c][j], s_pre[c][j]);
-        gx[c][j] = fmaf(gx[c][j] - fmaf(xhat[c][j], sa, sb), st.w, up[j]);
-        up[j] = has_y ? a.res_scale * gx[c][j] : gx[c][j];
+        gx[c][j] = fmaf(fmaf(-hat[c][j], sa, LAYER ? gx[c][j] - sb : gx[c][j]), st.w, up[j]);
+        up[j] = res * gx[c][j];
       }
-      rows::store8(reinterpret_cast<XT*>(a.dx) + m * a.lddx + (c * TPR + t) * 8, up, nvr[c]);
+      if (live && nv[c] > 0) rows::store8(reinterpret_cast<XT*>(a.dx) + m * a.lddx + (c * TPR + t) * 8, up, nv[c]);
     }
     if (has_y) {
-      // from here on xhat holds yhat, and dn the product gate * g_post
+      float ef[N] = {};
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = (c * TPR + t) * 8;
-        float g[8], gp[8];
-        rows::Raw8<uint16_t> gr;
-        raw16(c, s_dn + 1).floats(xhat[c]);
-        gr.load_cached(a.g_post + col, nvr[c]);
-        gr.floats(gp);
-        if (a.gate != nullptr) {
-          if (matrix) gr = raw16(c, s_dn + 2);
-          else gr.load_cached(a.gate + col, nvr[c]);
-          gr.floats(g);
-          float dg[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            xhat[c][j] = (xhat[c][j] - st.x) * st.y;
-            const float gy = gx[c][j] * xhat[c][j];
-            dg[j] = gy * gp[j];
-            s_post[c][j] = fmaf(gy, g[j], s_post[c][j]);
-            dn[c][j] = g[j] * gp[j];
-          }
-          if (matrix) rows::store8(a.dgate + m * a.lddgate + col, dg, nvr[c]);
-          else if (nvr[c] != 0)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s_gate[c][j] += dg[j];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            xhat[c][j] = (xhat[c][j] - st.x) * st.y;
-            s_post[c][j] = fmaf(gx[c][j], xhat[c][j], s_post[c][j]);
-            dn[c][j] = gp[j];
-          }
-        }
+      for (int c = 0; c < kC; ++c) {             // hat: yhat from here on
+        float g[8], dg[8];
+        sy.read(mine, c, nv[c], hat[c]);
+        if (MATRIX) sg.read(mine, c, nv[c], g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float d = gx[c][j] * dn[c][j];
-          ef[0] = fmaf(d, xhat[c][j], ef[0]);
-          ef[1] += d;
-          gx[c][j] = d;
+          hat[c][j] = (LAYER ? hat[c][j] - st.x : hat[c][j]) * st.y;
+          float gy = gx[c][j] * hat[c][j];
+          gx[c][j] *= MATRIX ? q[c][j] * g[j] : q[c][j];
+          ef[0] = fmaf(gx[c][j], hat[c][j], ef[0]);
+          if constexpr (LAYER) ef[1] += gx[c][j];
+          if (MATRIX) {
+            dg[j] = gy * q[c][j];
+            gy *= g[j];
+          }
+          s_y[c][j] += gy;
         }
+        if (MATRIX && live && nv[c] > 0) rows::store8(a.dgate + m * a.lddgate + (c * TPR + t) * 8, dg, nv[c]);
       }
-      rows::group_sum<TPR, 2>(ef, red, parity);
-      const float se = ef[0] * inv_d, sf = layer ? ef[1] * inv_d : 0.0f;
+      rows::group_sum<TPR, N>(ef, red, parity);
+      const float se = ef[0] * inv_d;
+      float sf = 0.0f;
+      if constexpr (LAYER) sf = ef[1] * inv_d;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if (nvr[c] == 0) continue;
+      for (int c = 0; c < kC; ++c) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) gx[c][j] = (gx[c][j] - fmaf(xhat[c][j], se, sf)) * st.y;
-        rows::store8(a.dy + m * a.lddy + (c * TPR + t) * 8, gx[c], nvr[c]);
+        for (int j = 0; j < 8; ++j) gx[c][j] = fmaf(-hat[c][j], se, LAYER ? gx[c][j] - sf : gx[c][j]) * st.y;
+        if (live && nv[c] > 0) rows::store8(a.dy + m * a.lddy + (c * TPR + t) * 8, gx[c], nv[c]);
       }
     }
     stage = stage + 1 == a.stages ? 0 : stage + 1;
@@ -324,25 +455,24 @@ __global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_kernel(const
   __syncthreads();                               // the slots become the groups' sums
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   float* sums = reinterpret_cast<float*>(slots);                 // [group][D rounded up to whole vectors]
-  const int width = C * TPR * 8;
-  auto reduce = [&](float (&s)[C][8], int which) {
+  const int width = kC * TPR * 8;
+  auto reduce = [&](float (&s)[kC][8], int which) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int j = 0; j < 8; j += 4)
         *reinterpret_cast<float4*>(sums + group * width + (c * TPR + t) * 8 + j) =
             make_float4(s[c][j], s[c][j + 1], s[c][j + 2], s[c][j + 3]);
     __syncthreads();
-    for (int col = threadIdx.x; col < a.D; col += kBwdThreads) {
+    for (int col = threadIdx.x; col < a.D; col += kRowThreads) {
       float v = sums[col];
       for (int g = 1; g < G; ++g) v += sums[g * width + col];
-      a.partial[((int64_t)blockIdx.x * 3 + which) * a.D + col] = v;
+      a.partial[((int64_t)blockIdx.x * 2 + which) * a.D + col] = v;
     }
     __syncthreads();
   };
   reduce(s_pre, 0);
-  if (has_y) reduce(s_post, 1);
-  if (has_y && a.gate != nullptr && !matrix) reduce(s_gate, 2);
+  if (has_y) reduce(s_y, 1);
 }
 
 // Rows of more than 8192 elements: the sums over the rows no longer fit the registers of a block
@@ -350,16 +480,16 @@ __global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_kernel(const
 // from L2.
 constexpr int kWide = 8192;
 template <class XT>
-__global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_wide_kernel(const BwdArgs a) {
-  constexpr int TPR = kBwdThreads;
-  extern __shared__ float wide_sums[];           // dg_pre, dg_post, dgate
+__global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_wide_kernel(const BwdArgs a) {
+  constexpr int TPR = kRowThreads;
+  extern __shared__ float wide_sums[];           // the two sums over the rows
   __shared__ float red[2 * 16 * 2];
   int parity = 0;
   const bool has_y = a.g_post != nullptr, matrix = a.gate != nullptr && a.ldgate != 0, layer = a.kind == MP_NORM_LAYER;
   const float inv_d = 1.0f / (float)a.D;
   const XT* x_out = reinterpret_cast<const XT*>(a.x_out);
   const XT* dx_out = reinterpret_cast<const XT*>(a.dx_out);
-  for (int c = threadIdx.x; c < 3 * a.D; c += TPR) wide_sums[c] = 0.0f;
+  for (int c = threadIdx.x; c < 2 * a.D; c += TPR) wide_sums[c] = 0.0f;
   __syncthreads();
   for (int64_t m = blockIdx.x; m < a.M; m += gridDim.x) {
     const float4 st = __ldg(reinterpret_cast<const float4*>(a.stats) + m);
@@ -441,10 +571,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_wide_kernel(
           dg[j] = gx[j] * yhat[j] * gp[j];
           dy[j] = (gx[j] * q[j] - fmaf(yhat[j], se, sf)) * st.y;
         }
-        for (int j = 0; j < nv; ++j) s[a.D + j] = fmaf(gx[j] * g[j], yhat[j], s[a.D + j]);
+        for (int j = 0; j < nv; ++j) s[a.D + j] = fmaf(matrix ? gx[j] * g[j] : gx[j], yhat[j], s[a.D + j]);
         if (matrix) rows::store8(a.dgate + m * a.lddgate + col, dg, nv);
-        else
-          for (int j = 0; j < nv; ++j) s[2 * a.D + j] += dg[j];
         rows::store8(a.dy + m * a.lddy + col, dy, nv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) gx[j] *= a.res_scale;
@@ -454,26 +582,25 @@ __global__ void __launch_bounds__(kBwdThreads, 1) mp_block_norm_bwd_wide_kernel(
   }
   __syncthreads();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  for (int c = threadIdx.x; c < 3 * a.D; c += TPR) a.partial[(int64_t)blockIdx.x * 3 * a.D + c] = wide_sums[c];
+  for (int c = threadIdx.x; c < 2 * a.D; c += TPR) a.partial[(int64_t)blockIdx.x * 2 * a.D + c] = wide_sums[c];
 }
 
-// Adds the blocks' partial rows in order, rounds, stores and inspects.  A block owns 32 columns of
-// one of the three sums; its 8 warps take the slabs in eight runs, each with several loads in flight.
+// Adds the blocks' partial rows in order, rounds, stores and inspects.  A block owns 32 columns of one of
+// the two sums; its 8 warps take the slabs in eight runs, each with several loads in flight.  gate: the gate
+// vector, NULL without one; then the second sum gives dgate too.
 constexpr int kSumThreads = 256;
 __global__ void __launch_bounds__(kSumThreads)
-mp_block_norm_sum_kernel(const float* partial, int slabs, int D, uint16_t* dg_pre, uint16_t* dg_post, uint16_t* dgate,
-                         mp_dev_state* st) {
+mp_block_norm_sum_kernel(const float* partial, int slabs, int D, const uint16_t* g_post, const uint16_t* gate,
+                         uint16_t* dg_pre, uint16_t* dg_post, uint16_t* dgate, mp_dev_state* st) {
   __shared__ float sm[kSumThreads / 32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
-  uint16_t* out = which == 0 ? dg_pre : which == 1 ? dg_post : dgate;
   const int c = blockIdx.x * 32 + lane;
   const int per = (slabs + 7) / 8, s0 = warp * per, s1 = min(slabs, s0 + per);
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete and visible
-  if (out == nullptr) return;
   float v = 0.0f;
   if (c < D)
 #pragma unroll 8
-    for (int s = s0; s < s1; ++s) v += partial[((int64_t)s * 3 + which) * D + c];
+    for (int s = s0; s < s1; ++s) v += partial[((int64_t)s * 2 + which) * D + c];
   sm[warp][lane] = v;
   __syncthreads();
   if (warp != 0) return;
@@ -482,23 +609,34 @@ mp_block_norm_sum_kernel(const float* partial, int slabs, int D, uint16_t* dg_pr
     float v = sm[0][lane];
 #pragma unroll
     for (int w = 1; w < kSumThreads / 32; ++w) v += sm[w][lane];
-    const uint16_t h = rows::f2h(v);
-    out[c] = h;
-    bad = rows::nonfinite16(h);
+    auto put = [&](uint16_t* out, float x) {
+      const uint16_t h = rows::f2h(x);
+      out[c] = h;
+      bad |= rows::nonfinite16(h);
+    };
+    if (which == 0) {
+      put(dg_pre, v);
+    } else if (gate == nullptr) {
+      put(dg_post, v);
+    } else {
+      const float g = rows::h2f(gate[c]), p = rows::h2f(g_post[c]);
+      put(dg_post, g * v);
+      put(dgate, p * v);
+    }
   }
   if (st != nullptr && __any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&st->h.found_inf, 1);
 }
 
 constexpr int64_t kSms = 148;          // most blocks that the backward pass runs, and partial rows that it writes
 
-// Threads per row of the backward kernels (2 vectors each) and of the forward kernels (1 to 4).
-int bwd_tpr(int64_t D) {
+// Threads per row, two vectors of 8 columns each.
+int tpr_for(int64_t D) {
   int tpr = 8;
-  while (tpr < 512 && (int64_t)tpr * 16 < D) tpr *= 2;
+  while (tpr < 512 && (int64_t)tpr * 16 < D) tpr *= tpr == 8 ? 4 : 2;
   return tpr;
 }
-int64_t bwd_blocks(int64_t M, int64_t D) {
-  const int64_t per = D > kWide ? 1 : kBwdThreads / bwd_tpr(D);
+int64_t blocks_for(int64_t M, int64_t D) {
+  const int64_t per = D > kWide ? 1 : kRowThreads / tpr_for(D);
   const int64_t blocks = (M + per - 1) / per;
   return blocks < 1 ? 1 : blocks < kSms ? blocks : kSms;
 }
@@ -517,67 +655,67 @@ int allow_smem(const void* kernel, size_t bytes) {
   return MP_OK;
 }
 
-struct FwdCall {
-  int kind;
-  float eps, res_scale;
-  const void* x; int64_t ldx;
-  const void* y; int64_t ldy;
-  const void *g_post, *gate; int64_t ldgate;
-  void* x_out; int64_t ldxo;
-  const void* g_pre;
-  void* n; int64_t ldn;
-  float* stats;
-  int64_t M, D;
-};
+// Stages of `slots` 16-byte slots per thread that fit the shared memory, 2 to 4 (the slots of a stage are 14 at
+// most, 112 KiB, so two always fit).
+constexpr size_t kMostSmem = 224 << 10;
+size_t stages_for(int slots, int* stages) {
+  const size_t stage = (size_t)slots * kRowThreads * 16;
+  const int fit = (int)(kMostSmem / stage);
+  *stages = fit > 4 ? 4 : fit;
+  return *stages * stage;
+}
 
-template <class XT, int TPR, int C>
-void fwd_launch(const FwdCall& f, cudaStream_t st) {
-  constexpr int THREADS = TPR > kFwdThreads ? TPR : kFwdThreads, G = THREADS / TPR;
-  mp_block_norm_fwd_kernel<XT, TPR, C><<<(unsigned)((f.M + G - 1) / G), THREADS, 0, st>>>(
-      f.kind, f.eps, f.res_scale, (const XT*)f.x, f.ldx, (const uint16_t*)f.y, f.ldy, (const uint16_t*)f.g_post,
-      (const uint16_t*)f.gate, f.ldgate, (XT*)f.x_out, f.ldxo, (const uint16_t*)f.g_pre, (uint16_t*)f.n, f.ldn,
-      f.stats, f.M, (int)f.D);
+template <class XT, int TPR>
+int fwd_launch(FwdArgs a, bool layer, int blocks, cudaStream_t st) {
+  const int xs = sizeof(XT) / 2;
+  a.slots = kC * (xs + (a.g_post ? 1 : 0) + (a.gate && a.ldgate ? 1 : 0));
+  const size_t smem = stages_for(a.slots, &a.stages);
+  auto kernel = layer ? mp_block_norm_fwd_kernel<XT, TPR, true> : mp_block_norm_fwd_kernel<XT, TPR, false>;
+  if (int rc = allow_smem((const void*)kernel, kMostSmem)) return rc;
+  kernel<<<blocks, kRowThreads, smem, st>>>(a);
+  return MP_OK;
 }
 template <class XT>
-void fwd_dispatch(const FwdCall& f, cudaStream_t st) {
-  if (f.D <= 128) fwd_launch<XT, 8, 2>(f, st);
-  else if (f.D <= 256) fwd_launch<XT, 16, 2>(f, st);
-  else if (f.D <= 512) fwd_launch<XT, 32, 2>(f, st);
-  else if (f.D <= 1024) fwd_launch<XT, 32, 4>(f, st);
-  else if (f.D <= 2048) fwd_launch<XT, 64, 4>(f, st);
-  else if (f.D <= 4096) fwd_launch<XT, 128, 4>(f, st);
-  else if (f.D <= 8192) fwd_launch<XT, 256, 4>(f, st);
-  else fwd_launch<XT, 512, 4>(f, st);
+int fwd_dispatch(const FwdArgs& a, bool layer, int blocks, cudaStream_t st) {
+  if (a.D > kWide) {
+    if (layer) mp_block_norm_fwd_wide_kernel<XT, true><<<blocks, kRowThreads, 0, st>>>(a);
+    else mp_block_norm_fwd_wide_kernel<XT, false><<<blocks, kRowThreads, 0, st>>>(a);
+    return MP_OK;
+  }
+  switch (tpr_for(a.D)) {
+    case 8: return fwd_launch<XT, 8>(a, layer, blocks, st);
+    case 32: return fwd_launch<XT, 32>(a, layer, blocks, st);
+    case 64: return fwd_launch<XT, 64>(a, layer, blocks, st);
+    case 128: return fwd_launch<XT, 128>(a, layer, blocks, st);
+    case 256: return fwd_launch<XT, 256>(a, layer, blocks, st);
+    default: return fwd_launch<XT, 512>(a, layer, blocks, st);
+  }
 }
 
 template <class XT, int TPR>
 int bwd_launch(BwdArgs a, int blocks, cudaStream_t st) {
-  constexpr int C = 2;
-  const bool has_y = a.g_post != nullptr, matrix = a.gate != nullptr && a.ldgate != 0;
+  const bool matrix = a.gate != nullptr && a.ldgate != 0, layer = a.kind == MP_NORM_LAYER;
   const int xs = sizeof(XT) / 2;
-  a.slots = C * (xs + (a.dx_out ? xs : 0) + 1 + (has_y ? 1 : 0) + (matrix ? 1 : 0));
-  const size_t stage = (size_t)a.slots * kBwdThreads * 16, most = 224 << 10;
-  a.stages = (int)(most / stage);
-  a.stages = a.stages > 4 ? 4 : a.stages;        // slots are 14 at most: 112 KiB a stage, so two always fit
-  size_t smem = a.stages * stage;
-  const size_t sums = (size_t)kBwdThreads * C * 8 * sizeof(float);
+  a.slots = kC * (xs + (a.dx_out ? xs : 0) + 1 + (a.g_post ? 1 : 0) + (matrix ? 1 : 0));
+  size_t smem = stages_for(a.slots, &a.stages);
+  const size_t sums = (size_t)kRowThreads * kC * 8 * sizeof(float);
   if (smem < sums) smem = sums;
-  auto kernel = mp_block_norm_bwd_kernel<XT, TPR, C>;
-  if (int rc = allow_smem((const void*)kernel, most)) return rc;
-  kernel<<<blocks, kBwdThreads, smem, st>>>(a);
+  auto kernel = layer ? matrix ? mp_block_norm_bwd_kernel<XT, TPR, true, true> : mp_block_norm_bwd_kernel<XT, TPR, true, false>
+                      : matrix ? mp_block_norm_bwd_kernel<XT, TPR, false, true> : mp_block_norm_bwd_kernel<XT, TPR, false, false>;
+  if (int rc = allow_smem((const void*)kernel, kMostSmem)) return rc;
+  kernel<<<blocks, kRowThreads, smem, st>>>(a);
   return MP_OK;
 }
 template <class XT>
 int bwd_dispatch(const BwdArgs& a, int blocks, cudaStream_t st) {
   if (a.D > kWide) {
-    const size_t smem = (size_t)3 * a.D * sizeof(float);
+    const size_t smem = (size_t)2 * a.D * sizeof(float);
     if (int rc = allow_smem((const void*)mp_block_norm_bwd_wide_kernel<XT>, smem)) return rc;
-    mp_block_norm_bwd_wide_kernel<XT><<<blocks, kBwdThreads, smem, st>>>(a);
+    mp_block_norm_bwd_wide_kernel<XT><<<blocks, kRowThreads, smem, st>>>(a);
     return MP_OK;
   }
-  switch (bwd_tpr(a.D)) {
+  switch (tpr_for(a.D)) {
     case 8: return bwd_launch<XT, 8>(a, blocks, st);
-    case 16: return bwd_launch<XT, 16>(a, blocks, st);
     case 32: return bwd_launch<XT, 32>(a, blocks, st);
     case 64: return bwd_launch<XT, 64>(a, blocks, st);
     case 128: return bwd_launch<XT, 128>(a, blocks, st);
@@ -613,9 +751,13 @@ int mp_block_norm_fwd(int kind, float eps, float res_scale, const void* x, int x
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: buffers must be 16-byte aligned, rows start on 16-byte boundaries", name);
   if (int rc = mp::check_device()) return rc;
   if (M == 0) return MP_OK;
-  const FwdCall f{kind, eps, res_scale, x, ldx, y16, ldy, g_post16, gate16, ldgate, x_out, ldxo, g_pre16, n16, ldn, stats, M, D};
-  if (x_bytes == 4) fwd_dispatch<float>(f, (cudaStream_t)stream);
-  else fwd_dispatch<uint16_t>(f, (cudaStream_t)stream);
+  const FwdArgs a{eps, res_scale, x, ldx, (const uint16_t*)y16, ldy, (const uint16_t*)g_post16, (const uint16_t*)gate16,
+                  ldgate, x_out, ldxo, (const uint16_t*)g_pre16, (uint16_t*)n16, ldn, stats, M, (int)D, 0, 0};
+  const int blocks = (int)blocks_for(M, D);
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool layer = kind == MP_NORM_LAYER;
+  if (int rc = x_bytes == 4 ? fwd_dispatch<float>(a, layer, blocks, st) : fwd_dispatch<uint16_t>(a, layer, blocks, st))
+    return rc;
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
   return MP_OK;
@@ -623,7 +765,7 @@ int mp_block_norm_fwd(int kind, float eps, float res_scale, const void* x, int x
 
 size_t mp_block_norm_bwd_workspace_bytes(int64_t M, int64_t D) {
   if (M < 0 || D <= 0 || D > MP_NORM_MAX_D) return 0;
-  return (size_t)bwd_blocks(M, D) * 3 * (size_t)D * sizeof(float);
+  return (size_t)blocks_for(M, D) * 2 * (size_t)D * sizeof(float);
 }
 
 int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn, const void* dx_out,
@@ -655,7 +797,7 @@ int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn,
   if (!workspace || workspace_bytes < need)
     return mp::set_error(MP_ERR_NOMEM, "%s: workspace of %zu bytes needed", name, need);
   if (int rc = mp::check_device()) return rc;
-  const int blocks = (int)bwd_blocks(M, D);
+  const int blocks = (int)blocks_for(M, D);
   cudaStream_t st = (cudaStream_t)stream;
   const BwdArgs a{kind, res_scale, (const uint16_t*)dn16, lddn, dx_out, lddxo, x_out, ldxo, (const uint16_t*)y16, ldy,
                   (const uint16_t*)g_post16, (const uint16_t*)gate16, ldgate, (const uint16_t*)g_pre16, stats, dx, lddx,
@@ -663,7 +805,7 @@ int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn,
   if (int rc = x_bytes == 4 ? bwd_dispatch<float>(a, blocks, st) : bwd_dispatch<uint16_t>(a, blocks, st)) return rc;
   MP_CUDA_TRY(cudaGetLastError());
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((D + 31) / 32), g_post16 ? 3 : 1, 1);
+  cfg.gridDim = dim3((unsigned)((D + 31) / 32), g_post16 ? 2 : 1, 1);
   cfg.blockDim = dim3(kSumThreads, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute attr;            // resident early, waits on the device for the partial rows
@@ -672,7 +814,8 @@ int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn,
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_block_norm_sum_kernel, (const float*)workspace, blocks, (int)D,
-                                 (uint16_t*)dg_pre16, (uint16_t*)dg_post16, ldgate == 0 ? (uint16_t*)dgate16 : nullptr,
+                                 (const uint16_t*)g_post16, ldgate == 0 ? (const uint16_t*)gate16 : nullptr,
+                                 (uint16_t*)dg_pre16, (uint16_t*)dg_post16, (uint16_t*)dgate16,
                                  state ? state->dev : (mp_dev_state*)nullptr));
   mp::count_launch(2);
   MP_CUDA_TRY(cudaGetLastError());
