@@ -153,7 +153,9 @@ def _check(rc: int):
 
 
 def _stream():
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    """The current torch stream of the current device (read without building a Stream object: the small calls
+    are bound by the host, and that alone took 3 us of them)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _dev(t: torch.Tensor, dtype) -> int:
@@ -367,32 +369,44 @@ def mp_check_finite(g16, state):
 
 # ---- operators of a token model ----
 
-def _ids(t):
-    """(pointer, bytes per id) of a contiguous vector of int32 or int64 ids."""
-    if not t.is_cuda or t.dtype not in (torch.int64, torch.int32) or t.dim() != 1 or not t.is_contiguous():
+def _ids(t, n=None):
+    """(pointer, bytes per id) of a contiguous vector of n int32 or int64 ids."""
+    size = _ID_BYTES.get(t.dtype)
+    if size is None or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
         raise TypeError(f"expected a contiguous CUDA vector of int32 or int64, got {t.device} {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr(), t.element_size()
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"expected {n} ids, got {t.shape[0]}")
+    return t.data_ptr(), size
+
+
+_ID_BYTES = {torch.int64: 8, torch.int32: 4}
 
 
 def _vec(t, n, dtype):
     """Pointer of a contiguous vector of n elements (None stays None)."""
     if t is None:
         return None
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"expected a contiguous vector of {n}, got {tuple(t.shape)}")
-    return _dev(t, dtype)
+    if t.dtype is not dtype or not t.is_cuda:
+        raise TypeError(f"expected a CUDA tensor of {dtype}, got {t.device} {t.dtype}")
+    return t.data_ptr()
 
 
 def _rows(t, shape, dtypes):
     """(pointer, pitch) of a row-major matrix of the given shape."""
-    if t.dim() != 2 or tuple(t.shape) != shape or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"expected a {shape} matrix with unit column stride, got {tuple(t.shape)}, {t.stride()}")
-    if not t.is_cuda or t.dtype not in dtypes:
+    if t.shape != shape:
+        raise ValueError(f"expected a {shape} matrix, got {tuple(t.shape)}")
+    if t.dtype not in dtypes or not t.is_cuda:
         raise TypeError(f"expected a CUDA tensor of {dtypes}, got {t.device} {t.dtype}")
-    if t.shape[0] > 1:
-        return t.data_ptr(), t.stride(0)
-    a = 16 // t.element_size()                       # the pitch of a single row does not matter
-    return t.data_ptr(), (t.shape[1] + a - 1) // a * a
+    pitch, one = t.stride()
+    r, c = shape
+    if one != 1 and c > 1:
+        raise ValueError(f"expected unit column stride, got {t.stride()}")
+    if r <= 1:                                       # the pitch of a single row does not matter
+        a = 8 if t.dtype is torch.float16 else 4
+        pitch = (c + a - 1) // a * a
+    return t.data_ptr(), pitch
 
 
 _F16, _X = (torch.float16,), (torch.float16, torch.float32)
@@ -430,8 +444,16 @@ def _gate(gate16, M, D):
     return (_vec(gate16, D, torch.float16), 0) if gate16.dim() == 1 else _rows(gate16, (M, D), _F16)
 
 
+def _stats(t, M):
+    if t is None:
+        return None
+    if t.shape != (M, 4) or not t.is_contiguous():
+        raise ValueError(f"expected contiguous stats [{M}, 4], got {tuple(t.shape)}")
+    return _dev(t, torch.float32)
+
+
 def _same(a, b, what):
-    if a.dtype != b.dtype:
+    if a.dtype is not b.dtype:
         raise TypeError(f"{what} must have one type, got {a.dtype} and {b.dtype}")
 
 
@@ -448,12 +470,10 @@ def mp_block_norm_fwd(x, g_pre16, n16, stats=None, y16=None, g_post16=None, gate
         pxo, ldxo = _rows(x_out, (M, D), _X)
         _same(x, x_out, "x and x_out")
     pg, ldg = _gate(gate16, M, D)
-    if stats is not None and (tuple(stats.shape) != (M, 4) or not stats.is_contiguous()):
-        raise ValueError(f"expected contiguous stats [{M}, 4]")
     _check(lib().mp_block_norm_fwd(kind, eps, res_scale, px, x.element_size(), ldx, py, ldy,
                                    _vec(g_post16, D, torch.float16), pg, ldg, pxo, ldxo,
                                    _vec(g_pre16, D, torch.float16), pn, ldn,
-                                   None if stats is None else _dev(stats, torch.float32), M, D, _stream()))
+                                   _stats(stats, M), M, D, _stream()))
 
 
 def mp_block_norm_bwd_workspace_bytes(M: int, D: int) -> int:
@@ -479,12 +499,10 @@ def mp_block_norm_bwd(dn16, x_out, g_pre16, stats, dx, dg_pre16, dx_out=None, y1
     pdg, lddg = _gate(dgate16, M, D)
     if gate16 is not None and dgate16 is not None and gate16.dim() != dgate16.dim():
         raise ValueError("dgate16 must have the form of gate16")
-    if tuple(stats.shape) != (M, 4) or not stats.is_contiguous():
-        raise ValueError(f"expected contiguous stats [{M}, 4]")
     ws, size = _ws(workspace)
     _check(lib().mp_block_norm_bwd(kind, res_scale, pdn, lddn, pu, ldu, px, x_out.element_size(), ldx, py, ldy,
                                    _vec(g_post16, D, torch.float16), pg, ldg, _vec(g_pre16, D, torch.float16),
-                                   _dev(stats, torch.float32), pdx, lddx, pdy, lddy, _vec(dg_post16, D, torch.float16),
+                                   _stats(stats, M), pdx, lddx, pdy, lddy, _vec(dg_post16, D, torch.float16),
                                    pdg, lddg, _vec(dg_pre16, D, torch.float16), M, D, _handle(state), ws, size,
                                    _stream()))
 
@@ -495,9 +513,7 @@ def mp_policy_loss(logits16, targets, old_logp, advantage, weight, logp, token_l
     logits times grad_scale and the loss scale of `state` (dlogits16 None: forward only)."""
     N, V = logits16.shape
     z, ldl = _rows(logits16, (N, V), _F16)
-    if targets.shape[0] != N:
-        raise ValueError(f"expected {N} targets, got {targets.shape[0]}")
-    t, nb = _ids(targets)
+    t, nb = _ids(targets, N)
     dz, lddl = (None, 0) if dlogits16 is None else _rows(dlogits16, (N, V), _F16)
     cfg = PolicyConfig(clip_lo, clip_hi, kl_coef, grad_scale)
     f = torch.float32
@@ -510,9 +526,7 @@ def mp_token_logp(logits16, targets, logp, weight=None, state=None):
     """logp[i] = log softmax(logits16[i])[targets[i]]; 0 where weight is 0."""
     N, V = logits16.shape
     z, ldl = _rows(logits16, (N, V), _F16)
-    if targets.shape[0] != N:
-        raise ValueError(f"expected {N} targets, got {targets.shape[0]}")
-    t, nb = _ids(targets)
+    t, nb = _ids(targets, N)
     _check(lib().mp_token_logp(z, ldl, t, nb, _vec(weight, N, torch.float32), N, V, _vec(logp, N, torch.float32),
                                _handle(state), _stream()))
 
