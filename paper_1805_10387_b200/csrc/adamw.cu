@@ -27,8 +27,10 @@ constexpr float kTop = 448.0f;                  // largest E4M3 number
 constexpr float kTiny = 0.001953125f;           // smallest E4M3 number above 0, 2^-9
 constexpr float kNoScale = 7.888609052210118e-31f;   // 2^-100
 
-// A tensor of the plan.  Blocks of all tensors are numbered through; the addresses are those that the tensors'
-// buffers would have if they began at block 0, so that block x lies at address + x * (bytes of a block).
+// A tensor of the plan.  Blocks of all tensors are numbered through, each tensor beginning at a multiple of
+// kMostUnit; the addresses are those that the tensors' buffers would have if they began at block 0, so that
+// block x lies at address + x * (bytes of a block).
+constexpr int kMostUnit = 8;
 struct alignas(16) Tensor {
   uint64_t g16, w32, m, v, w16, m_scale, v_scale;
   int64_t end;                                  // first block * 256 + elements
@@ -107,22 +109,35 @@ __device__ __forceinline__ float warp_top(float v) {
   return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(v)));
 }
 
-// A warp takes the blocks w, w + step, ... of the plan, w its number among the step warps of the grid, so that
-// neighbouring warps stream neighbouring memory.  A Cursor walks them.
+// A warp takes the units w, w + step, ... of the plan, w its number among the step warps of the grid, so that
+// neighbouring warps stream neighbouring memory.  A unit is 1, 2, 4 or 8 neighbouring blocks: the 8-bit states'
+// scales of a unit are one access of the warp.  (One 4-byte access a block cost a fifth of the time.)  A Cursor
+// walks a warp's blocks.
 struct Cursor {
   const Tensor* tensors;
-  int64_t x, step, n_blocks;
-  int at = 0, n_tensors;                        // the tensor that holds block x
-  __device__ __forceinline__ Cursor(const Tensor* table, int n, int64_t blocks)
-      : tensors(table), x((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)),
-        step((int64_t)gridDim.x * (kThreads / 32)), n_blocks(blocks), n_tensors(n) {
+  int64_t x, hop, n_blocks;                     // hop: from the end of one unit to the beginning of the warp's next
+  int unit, at = 0, n_tensors;                  // at: the tensor that holds block x
+  __device__ __forceinline__ Cursor(const Tensor* table, int n, int64_t blocks, int unit_blocks)
+      : tensors(table), x(((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * unit_blocks),
+        hop(((int64_t)gridDim.x * (kThreads / 32) - 1) * unit_blocks), n_blocks(blocks), unit(unit_blocks), n_tensors(n) {
     if (more()) seek(0, n_tensors - 1);
+    settle();
   }
   __device__ __forceinline__ bool more() const { return x < n_blocks; }
   __device__ __forceinline__ void next() {
-    x += step;
-    if (!more() || __ldg(&tensors[at].block_end) > x) return;
-    // most often one of the next 32 tensors
+    ++x;
+    if ((x & (unit - 1)) == 0) x += hop;
+    settle();
+  }
+  // finds the tensor, and passes over the numbers that no tensor fills
+  __device__ __forceinline__ void settle() {
+    while (more()) {
+      if (__ldg(&tensors[at].block_end) <= x) forward();
+      if (__ldg(&tensors[at].end) > x * kBlock) return;
+      x = (x | (unit - 1)) + 1 + hop;
+    }
+  }
+  __device__ __forceinline__ void forward() {   // most often one of the next 32 tensors
     const int lane = threadIdx.x & 31, hi = n_tensors - 1, probe = at + 1 + lane < hi ? at + 1 + lane : hi;
     const unsigned after = __ballot_sync(0xFFFFFFFFu, __ldg(&tensors[probe].block_end) > x);
     if (after) at = at + __ffs(after) < hi ? at + __ffs(after) : hi;
@@ -170,9 +185,9 @@ __device__ __forceinline__ int quad(int inside, int h) {
 }
 
 __global__ void __launch_bounds__(kThreads)
-mp_adamw_check_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, mp_dev_state* st) {
+mp_adamw_check_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, int unit, mp_dev_state* st) {
   bool bad = false;
-  for (Cursor cur(tensors, n_tensors, n_blocks); cur.more(); cur.next()) {
+  for (Cursor cur(tensors, n_tensors, n_blocks, unit); cur.more(); cur.next()) {
     const Tensor& T = cur.tensors[cur.at];
     const int inside = cur.inside(T);
 #pragma unroll
@@ -210,7 +225,7 @@ __device__ __forceinline__ uint32_t get4(const uint8_t* p, int nv) {
 template <int BITS> struct States;
 template <> struct States<32> {
   float4 m[2], v[2];
-  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside) {
+  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside, int) {
     const uint64_t pm = __ldg(&T.m), pv = __ldg(&T.v);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -221,8 +236,8 @@ template <> struct States<32> {
 };
 template <> struct States<8> {
   uint2 m, v;
-  float ms, vs;
-  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside) {
+  float ms = 0.0f, vs = 0.0f;                   // lane l: the scales of block l of the unit
+  __device__ __forceinline__ void load(const Tensor& T, int64_t x, int inside, int unit) {
     const uint8_t *pm = lane_at<const uint8_t, 8>(__ldg(&T.m), x, 1, 0), *pv = lane_at<const uint8_t, 8>(__ldg(&T.v), x, 1, 0);
     if (inside >= kBlock) {
       m = __ldcs(reinterpret_cast<const uint2*>(pm));
@@ -231,8 +246,11 @@ template <> struct States<8> {
       m = make_uint2(get4(pm, quad<8>(inside, 0)), get4(pm + 4, quad<8>(inside, 1)));
       v = make_uint2(get4(pv, quad<8>(inside, 0)), get4(pv + 4, quad<8>(inside, 1)));
     }
-    ms = __ldcs(reinterpret_cast<const float*>(__ldg(&T.m_scale)) + x);
-    vs = __ldcs(reinterpret_cast<const float*>(__ldg(&T.v_scale)) + x);
+    const int lane = threadIdx.x & 31;
+    if ((x & (unit - 1)) == 0 && lane < unit && (x + lane) * kBlock < __ldg(&T.end)) {
+      ms = __ldcs(reinterpret_cast<const float*>(__ldg(&T.m_scale)) + x + lane);
+      vs = __ldcs(reinterpret_cast<const float*>(__ldg(&T.v_scale)) + x + lane);
+    }
   }
 };
 template <int BITS>
@@ -253,7 +271,7 @@ struct Held {
       g[h] = get4(lane_at<const uint16_t, BITS>(pg, x, 2, h), quad<BITS>(inside, h));
       w[h] = get4(lane_at<const float, BITS>(pw, x, 4, h), quad<BITS>(inside, h));
     }
-    s.load(*T, x, inside);
+    s.load(*T, x, inside, cur.unit);
   }
 };
 __device__ __forceinline__ void spread(const float4 (&q)[2], float (&f)[8]) {
@@ -280,11 +298,12 @@ __device__ __forceinline__ void put4(uint8_t* p, uint32_t q, int nv) {
 
 template <int BITS>
 __global__ void __launch_bounds__(kThreads, BITS == 32 ? 2 : 3)
-mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, const mp_dev_state* st, mp_adamw_config o,
-                       const int* gemm_status) {
+mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, int unit, const mp_dev_state* st,
+                       mp_adamw_config o, const int* gemm_status) {
   if (st->h.found_inf != 0 || st->h.status != 0 || *gemm_status != 0) return;
   __shared__ Coef s_c;
-  Cursor cur(tensors, n_tensors, n_blocks);
+  Cursor cur(tensors, n_tensors, n_blocks, unit);
+  float new_ms = 0.0f, new_vs = 0.0f;           // lane l: of block l of the unit
   Held<BITS> next;
   if (cur.more()) next.load(cur);
   if (threadIdx.x == kThreads - 1) s_c = coefficients(st, o);
@@ -308,10 +327,12 @@ mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, c
     } else {
       from_e4m3(held.s.m, m);
       from_e4m3(held.s.v, r);
+      const float ms = __shfl_sync(0xFFFFFFFFu, held.s.ms, (int)x & (unit - 1));
+      const float vs = __shfl_sync(0xFFFFFFFFu, held.s.vs, (int)x & (unit - 1));
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        m[j] = __fmul_rn(m[j], held.s.ms);
-        r[j] = __fmul_rn(r[j], held.s.vs);
+        m[j] = __fmul_rn(m[j], ms);
+        r[j] = __fmul_rn(r[j], vs);
         v[j] = __fmul_rn(r[j], r[j]);
       }
     }
@@ -338,9 +359,15 @@ mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, c
       }
       mq = to_e4m3(m);
       vq = to_e4m3(r);
-      if ((threadIdx.x & 31) == 0) {
-        reinterpret_cast<float*>(__ldg(&T.m_scale))[x] = tm < kNoScale ? 0.0f : __fmul_rn(tm, 1.0f / kTop);
-        reinterpret_cast<float*>(__ldg(&T.v_scale))[x] = tr < kNoScale ? 0.0f : __fmul_rn(tr, 1.0f / kTop);
+      const int lane = threadIdx.x & 31, of_unit = (int)x & (unit - 1);
+      if (lane == of_unit) {
+        new_ms = tm < kNoScale ? 0.0f : __fmul_rn(tm, 1.0f / kTop);
+        new_vs = tr < kNoScale ? 0.0f : __fmul_rn(tr, 1.0f / kTop);
+      }
+      if ((of_unit == unit - 1 || (x + 1) * kBlock >= __ldg(&T.end)) && lane <= of_unit) {
+        const int64_t first = x - of_unit;
+        __stcs(reinterpret_cast<float*>(__ldg(&T.m_scale)) + first + lane, new_ms);
+        __stcs(reinterpret_cast<float*>(__ldg(&T.v_scale)) + first + lane, new_vs);
       }
     }
     const uint64_t pw = __ldg(&T.w32), pw16 = __ldg(&T.w16), pm = __ldg(&T.m), pv = __ldg(&T.v);
@@ -421,7 +448,7 @@ int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const*
     for (int i = 0; i < n; ++i) {                // a tensor without elements has no place in the table
       if (count[i] == 0) continue;
       const int64_t first = p->n_blocks;
-      p->n_blocks += (count[i] + kBlock - 1) / kBlock;
+      p->n_blocks += (count[i] + kBlock * kMostUnit - 1) / (kBlock * kMostUnit) * kMostUnit;
       auto from_block_0 = [&](const void* q, int64_t block_bytes) { return (uint64_t)q - (uint64_t)(first * block_bytes); };
       const int64_t state = state_bits == 32 ? 4 * kBlock : kBlock;
       ts.push_back(Tensor{from_block_0(g16[i], 2 * kBlock), from_block_0(w32[i], 4 * kBlock), from_block_0(m[i], state),
@@ -464,22 +491,25 @@ int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config*
   cudaStream_t st = (cudaStream_t)stream;
   int* gemm_status = nullptr;
   if (int rc = mp::gemm_status_device_ptr(&gemm_status)) return rc;
-  // one resident round of blocks; a block has work for each of its warps
-  auto grid_of = [&](const void* kernel, int* grid) {
+  // One resident round of blocks; units as large as leaves every warp four.
+  auto shape = [&](const void* kernel, int most_unit, int* grid, int* unit) {
     if (int rc = resident_blocks(kernel, grid)) return rc;
-    const int64_t want = (plan->n_blocks + kThreads / 32 - 1) / (kThreads / 32);
+    const int64_t warps = (int64_t)*grid * (kThreads / 32);
+    *unit = most_unit;
+    while (*unit > 1 && plan->n_blocks < 4 * warps * *unit) *unit /= 2;
+    const int64_t want = (plan->n_blocks / *unit + kThreads / 32 - 1) / (kThreads / 32);
     if (want < *grid) *grid = (int)want;
     return (int)MP_OK;
   };
-  int grid = 0;
+  int grid = 0, unit = 0;
   if (check_mode == 1) {
-    if (int rc = grid_of((const void*)mp_adamw_check_kernel, &grid)) return rc;
-    mp_adamw_check_kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, state->dev);
+    if (int rc = shape((const void*)mp_adamw_check_kernel, 1, &grid, &unit)) return rc;
+    mp_adamw_check_kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, unit, state->dev);
     mp::count_launch();
   }
   auto kernel = plan->bits == 32 ? mp_adamw_update_kernel<32> : mp_adamw_update_kernel<8>;
-  if (int rc = grid_of((const void*)kernel, &grid)) return rc;
-  kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, state->dev, *opt, gemm_status);
+  if (int rc = shape((const void*)kernel, plan->bits == 32 ? 1 : kMostUnit, &grid, &unit)) return rc;
+  kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, unit, state->dev, *opt, gemm_status);
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
   return MP_OK;
