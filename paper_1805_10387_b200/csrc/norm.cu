@@ -40,13 +40,24 @@ struct Stream {
       : row(static_cast<const T*>(p) + first * ld + t * 8), hop(step * ld), slot(slots) {
     if (p != nullptr) slots += kC * XS;
   }
+  // FP32: the 2 n halves of the vectors of n <= 32 neighbouring threads are copied in their order in memory, so
+  // that an access of the warp touches whole sectors; a half lands in its owner's slot, wherever that is.
+  // (Each thread copying both halves of its own vector fetched every sector twice.)
   template <int TPR>
-  __device__ __forceinline__ void fetch(uint32_t stage, const int (&nv)[kC], bool inside) {
+  __device__ __forceinline__ void fetch(uint32_t stage, const int (&nv)[kC], int D, int t, bool inside) {
 #pragma unroll
     for (int c = 0; c < kC; ++c)
+      if constexpr (XS == 1) {
+        copy16(stage + (slot + c) * (kRowThreads * 16), row + c * TPR * 8, inside && nv[c] > 0);
+      } else {
+        constexpr int n = TPR < 32 ? TPR : 32;
 #pragma unroll
-      for (int h = 0; h < XS; ++h)
-        copy16(stage + (slot + c * XS + h) * (kRowThreads * 16), row + c * TPR * 8 + h * 4, inside && nv[c] > 4 * h);
+        for (int h = 0; h < 2; ++h) {
+          const int piece = h * n + t % n, shift = piece / 2 - t % n, half = piece & 1;   // shift: to the owner
+          copy16(stage + ((slot + c * 2 + half) * kRowThreads + shift) * 16, row + (c * TPR + shift) * 8 + half * 4,
+                 inside && D > (c * TPR + t + shift) * 8 + half * 4);
+        }
+      }
     row += hop;
   }
   __device__ __forceinline__ void read(const uint4* stage, int c, int nv, float (&f)[8]) const {
@@ -58,6 +69,26 @@ struct Stream {
     r.floats(f);
   }
 };
+
+// Stores a vector of the residual type at p.  FP32: two neighbouring threads exchange halves first, so that
+// each store of the pair is 32 contiguous bytes.  Every thread of the warp calls; `live`: the row exists.
+__device__ __forceinline__ void put(uint16_t* p, const float (&f)[8], int nv, int, bool live) {
+  if (live && nv > 0) rows::store8(p, f, nv);
+}
+__device__ __forceinline__ void put(float* p, const float (&f)[8], int nv, int t, bool live) {
+  const bool odd = t & 1;
+  float o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = __shfl_xor_sync(0xFFFFFFFFu, odd ? f[j] : f[4 + j], 1);
+  const bool both = __shfl_sync(0xFFFFFFFFu, nv, threadIdx.x | 1) == 8;      // then the even thread's is whole too
+  if (!live) return;
+  if (both) {
+    __stcs(reinterpret_cast<float4*>(odd ? p - 4 : p), odd ? make_float4(o[0], o[1], o[2], o[3]) : make_float4(f[0], f[1], f[2], f[3]));
+    __stcs(reinterpret_cast<float4*>(odd ? p + 4 : p + 8), odd ? make_float4(f[4], f[5], f[6], f[7]) : make_float4(o[0], o[1], o[2], o[3]));
+  } else if (nv > 0) {
+    rows::store8(p, f, nv);
+  }
+}
 
 // ---------------------------------------------------------------- forward
 struct FwdArgs {
@@ -117,7 +148,7 @@ template <class XT, int TPR, bool LAYER>
 __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const FwdArgs a) {
   constexpr int G = kRowThreads / TPR;
   extern __shared__ uint4 slots[];
-  __shared__ float red_all[G][2 * 16];
+  __shared__ float red_all[G][rows::red_floats<TPR, 1>];
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   float* red = red_all[group];
   int parity = 0, used = 0;
@@ -140,9 +171,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const
     const bool inside = ahead < a.M;
     if (TPR < 32 || inside) {
       const uint32_t at = base + (uint32_t)(stage * a.slots) * (kRowThreads * 16);
-      sx.template fetch<TPR>(at, nv, inside);
-      if (has_y) sy.template fetch<TPR>(at, nv, inside);
-      if (matrix) sg.template fetch<TPR>(at, nv, inside);
+      sx.template fetch<TPR>(at, nv, a.D, t, inside);
+      if (has_y) sy.template fetch<TPR>(at, nv, a.D, t, inside);
+      if (matrix) sg.template fetch<TPR>(at, nv, a.D, t, inside);
     }
     ahead += step;
     copy_commit();
@@ -171,8 +202,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const
   int64_t m = first;
   for (int64_t lm = lead; lm < a.M; lm += step, m += step) {
     const bool live = TPR >= 32 || m < a.M;
-    fetch(stage == 0 ? a.stages - 1 : stage - 1);        // the slots of the row before this one
+    if (sizeof(XT) == 4) __syncwarp();           // everyone has read the slots of the row before this one
+    fetch(stage == 0 ? a.stages - 1 : stage - 1);
     copy_wait(a.stages);
+    if (sizeof(XT) == 4) __syncwarp();           // the others' copies into this thread's slots are complete too
     const uint4* mine = slots + threadIdx.x + (int64_t)stage * a.slots * kRowThreads;
     float xo[kC][8];
     float2 my = make_float2(0.0f, 0.0f);
@@ -191,8 +224,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const
           const float h = LAYER ? (y[c][j] - my.x) * my.y : y[c][j] * my.y;
           xo[c][j] = fmaf(h, matrix ? q[c][j] * g[j] : q[c][j], a.res_scale * xo[c][j]);
         }
-        if (live && nv[c] > 0)
-          rows::store8(reinterpret_cast<XT*>(a.x_out) + m * a.ldxo + (c * TPR + t) * 8, xo[c], nv[c]);
+        put(reinterpret_cast<XT*>(a.x_out) + m * a.ldxo + (c * TPR + t) * 8, xo[c], nv[c], t, live);
       }
     } else {
 #pragma unroll
@@ -215,7 +247,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_kernel(const
 template <class XT, bool LAYER>
 __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_fwd_wide_kernel(const FwdArgs a) {
   constexpr int TPR = kRowThreads, C = 4;
-  __shared__ float red[2 * 16];
+  __shared__ float red[rows::red_floats<TPR, 1>];
   int parity = 0;
   const float inv_d = 1.0f / (float)a.D;
   auto moments_of = [&](const float (&f)[C][8]) {
@@ -324,7 +356,7 @@ template <class XT, int TPR, bool LAYER, bool MATRIX>
 __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const BwdArgs a) {
   constexpr int G = kRowThreads / TPR, N = LAYER ? 2 : 1;        // N: row sums that a norm's backward needs
   extern __shared__ uint4 slots[];
-  __shared__ float red_all[G][2 * 16 * N];
+  __shared__ float red_all[G][rows::red_floats<TPR, N>];
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   float* red = red_all[group];
   int parity = 0, used = 0;
@@ -347,11 +379,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const
     const bool inside = ahead < a.M;
     if (TPR < 32 || inside) {
       const uint32_t at = base + (uint32_t)(stage * a.slots) * (kRowThreads * 16);
-      sx.template fetch<TPR>(at, nv, inside);
-      if (has_up) su.template fetch<TPR>(at, nv, inside);
-      sd.template fetch<TPR>(at, nv, inside);
-      if (has_y) sy.template fetch<TPR>(at, nv, inside);
-      if (MATRIX) sg.template fetch<TPR>(at, nv, inside);
+      sx.template fetch<TPR>(at, nv, a.D, t, inside);
+      if (has_up) su.template fetch<TPR>(at, nv, a.D, t, inside);
+      sd.template fetch<TPR>(at, nv, a.D, t, inside);
+      if (has_y) sy.template fetch<TPR>(at, nv, a.D, t, inside);
+      if (MATRIX) sg.template fetch<TPR>(at, nv, a.D, t, inside);
     }
     ahead += step;
     copy_commit();
@@ -381,9 +413,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const
   int64_t m = first;
   for (int64_t lm = lead; lm < a.M; lm += step, m += step) {
     const bool live = TPR >= 32 || m < a.M;
-    fetch(stage == 0 ? a.stages - 1 : stage - 1);        // the slots of the row before this one
+    if (sizeof(XT) == 4) __syncwarp();           // everyone has read the slots of the row before this one
+    fetch(stage == 0 ? a.stages - 1 : stage - 1);
     const float4 st = live ? __ldg(reinterpret_cast<const float4*>(a.stats) + m) : make_float4(0, 0, 0, 0);
     copy_wait(a.stages);
+    if (sizeof(XT) == 4) __syncwarp();           // the others' copies into this thread's slots are complete too
     const uint4* mine = slots + threadIdx.x + (int64_t)stage * a.slots * kRowThreads;
     float gx[kC][8], hat[kC][8];
     float ab[N] = {};
@@ -414,7 +448,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const
         gx[c][j] = fmaf(fmaf(-hat[c][j], sa, LAYER ? gx[c][j] - sb : gx[c][j]), st.w, up[j]);
         up[j] = res * gx[c][j];
       }
-      if (live && nv[c] > 0) rows::store8(reinterpret_cast<XT*>(a.dx) + m * a.lddx + (c * TPR + t) * 8, up, nv[c]);
+      put(reinterpret_cast<XT*>(a.dx) + m * a.lddx + (c * TPR + t) * 8, up, nv[c], t, live);
     }
     if (has_y) {
       float ef[N] = {};
@@ -483,7 +517,7 @@ template <class XT>
 __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_wide_kernel(const BwdArgs a) {
   constexpr int TPR = kRowThreads;
   extern __shared__ float wide_sums[];           // the two sums over the rows
-  __shared__ float red[2 * 16 * 2];
+  __shared__ float red[rows::red_floats<TPR, 2>];
   int parity = 0;
   const bool has_y = a.g_post != nullptr, matrix = a.gate != nullptr && a.ldgate != 0, layer = a.kind == MP_NORM_LAYER;
   const float inv_d = 1.0f / (float)a.D;
@@ -586,21 +620,21 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_wide_kernel(
 }
 
 // Adds the blocks' partial rows in order, rounds, stores and inspects.  A block owns 32 columns of one of
-// the two sums; its 8 warps take the slabs in eight runs, each with several loads in flight.  gate: the gate
+// the two sums; its 32 warps take the slabs in runs of at most five, all of them in flight at once.  gate: the gate
 // vector, NULL without one; then the second sum gives dgate too.
-constexpr int kSumThreads = 256;
+constexpr int kSumThreads = 1024;
 __global__ void __launch_bounds__(kSumThreads)
 mp_block_norm_sum_kernel(const float* partial, int slabs, int D, const uint16_t* g_post, const uint16_t* gate,
                          uint16_t* dg_pre, uint16_t* dg_post, uint16_t* dgate, mp_dev_state* st) {
   __shared__ float sm[kSumThreads / 32][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
   const int c = blockIdx.x * 32 + lane;
-  const int per = (slabs + 7) / 8, s0 = warp * per, s1 = min(slabs, s0 + per);
+  const int per = (slabs + 31) / 32, s0 = warp * per, s1 = min(slabs, s0 + per);
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete and visible
   float v = 0.0f;
   if (c < D)
-#pragma unroll 8
-    for (int s = s0; s < s1; ++s) v += partial[((int64_t)s * 2 + which) * D + c];
+#pragma unroll 5
+    for (int s = s0; s < s1; ++s) v += __ldcg(partial + ((int64_t)s * 2 + which) * D + c);
   sm[warp][lane] = v;
   __syncthreads();
   if (warp != 0) return;

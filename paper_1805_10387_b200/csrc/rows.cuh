@@ -49,13 +49,15 @@ __device__ __forceinline__ float block_max(float v, float* sm) {
   return t;
 }
 
-// ---- rows split over groups of TPR threads (8 .. 512, a power of two) ----
+// ---- rows split over groups of TPR threads (8 .. 1024, a power of two) ----
 //
 // Sum of N values over the threads of a group, the same in every thread of it.  Groups of at most 32
 // threads stay inside a warp (every lane of the warp must call); larger ones exchange the warps'
-// sums through `red` (2 x 16 x N floats for each group) and a barrier of their own.  Two calls in a
+// sums through `red` (red_floats for each group) and a barrier of their own.  Two calls in a
 // row use the two halves of `red`: a warp that reaches the call after next has passed the next
 // call's barrier, so everyone has read this call's values.
+template <int TPR, int N>
+constexpr int red_floats = TPR > 32 ? 2 * (TPR / 32) * N : 1;
 template <int TPR, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float* red, int& parity) {
 #pragma unroll
@@ -65,7 +67,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* red, int& parity
   if constexpr (TPR > 32) {
     constexpr int W = TPR / 32;
     const int warp = (threadIdx.x % TPR) >> 5;
-    float* half = red + parity * 16 * N;
+    float* half = red + parity * W * N;
     parity ^= 1;
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
