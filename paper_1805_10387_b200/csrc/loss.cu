@@ -237,7 +237,7 @@ __device__ __forceinline__ uint4 live8(uint4 q, int nv) {
 }
 __device__ __forceinline__ uint4 no_words() { return make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2); }
 
-// ---- rows of up to 8192 words: a group of TPR threads per row, the row in registers ----
+// ---- rows of up to 512 words: a group of TPR threads per row, the row in registers ----
 constexpr int kGroupThreads = 256;
 template <int TPR, int C>
 __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(const LossArgs a) {
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 
-// ---- rows of more than 8192 words: CL blocks of a cluster per row, the row in their shared memory ----
+// ---- rows of more than 512 words: CL blocks of a cluster per row, the row in their shared memory ----
 //
 // Persistent clusters, several blocks an SM: while one block sums a row or writes its gradient, the
 // others' rows are on their way.  A block holds its part of a row, each thread its own vectors, which its own
@@ -301,11 +301,12 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
 // Small blocks: with 128 threads and at most 32 KiB of a row (up to six blocks an SM) the blocks drift
 // apart and the loads of some cover the arithmetic of others.  8192 x 32768 with 128 threads and 32 KiB
 // 189 us, 64 KiB 195, 16 KiB 223; 256 threads and 64 KiB 206; 512 threads 209; one block of 1024 threads
-// with rows fetched two ahead 221.
+// with rows fetched two ahead 221.  (Rows in the registers of groups, as above for short ones, are slower from
+// 512 words on: 20000 x 5000 229 us against 87, 40000 x 600 93 against 76.)
 constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
 constexpr int kPartWords = 16 * kRowThreads * 8;  // words of a row that a block takes if a cluster of 8 can
 template <int CL>
-__global__ void __launch_bounds__(kRowThreads, 6) mp_policy_loss_row_kernel(const LossArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 8) mp_policy_loss_row_kernel(const LossArgs a) {
   extern __shared__ uint4 slots[];                // [vectors]
   __shared__ Sum2 s_part[2][kRowWarps];
   __shared__ Sum2 s_block[2][CL];
@@ -474,8 +475,6 @@ int dispatch(const LossArgs& a, cudaStream_t st) {
   if (a.V <= 32) group_launch<4, 1>(a, st);
   else if (a.V <= 128) group_launch<8, 2>(a, st);
   else if (a.V <= 512) group_launch<32, 2>(a, st);
-  else if (a.V <= 2048) group_launch<32, 8>(a, st);
-  else if (a.V <= 8192) group_launch<128, 8>(a, st);
   else if (a.V <= kPartWords) return row_launch<1>(a, st);
   else if (a.V <= 2 * kPartWords) return row_launch<2>(a, st);
   else if (a.V <= 4 * kPartWords) return row_launch<4>(a, st);
