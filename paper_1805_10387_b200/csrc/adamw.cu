@@ -5,6 +5,12 @@
 // 16 B a parameter and instructions weigh as much as memory, that holds for the moments alone: an E4M3 code
 // may turn on their last bit.  The quotient of the step is taken from the hardware's approximation (off by
 // about 2^-22 of a step, far below the last bit of the weight).
+//
+// 28 B a parameter with 32-bit states, 16 B and two scales for each 256 parameters with 8-bit ones: HBM bounds both.
+// Measured on a B200, 1e8 parameters: 32 bits 457 - 463 us (6.1 TB/s), 8 bits 329 us in one tensor or 500 (4.9 TB/s;
+// leaving out the root, the quotient and the codes changes that by 2 %).  What was tried: asynchronous copies into
+// shared memory two or three blocks ahead (32 bits 530, 8 bits 420 us), four blocks of threads an SM instead of
+// three (8 bits 409), two (401).
 
 #include <cuda_fp8.h>
 #include <math.h>
@@ -111,7 +117,7 @@ __device__ __forceinline__ float warp_top(float v) {
 
 // A warp takes the units w, w + step, ... of the plan, w its number among the step warps of the grid, so that
 // neighbouring warps stream neighbouring memory.  A unit is 1, 2, 4 or 8 neighbouring blocks: the 8-bit states'
-// scales of a unit are one access of the warp.  (One 4-byte access a block cost a fifth of the time.)  A Cursor
+// scales of a unit are one access of the warp.  (With one 4-byte access a block: 370 us instead of 329.)  A Cursor
 // walks a warp's blocks.
 struct Cursor {
   const Tensor* tensors;
@@ -167,7 +173,7 @@ struct Cursor {
 };
 // A lane takes two quads of a block.  With 32-bit states they are 128 elements apart, so that each access of
 // a warp is one contiguous piece; with 8-bit states they are neighbours, so that a lane's eight codes are one access.
-// (1e8 parameters: 32 bits 457 us against 530 with neighbours, 8 bits 359 against 340.)
+// (1e8 parameters, asynchronous copies: 32 bits 663 us with neighbours, 530 so; 8 bits: no difference beyond 3 %.)
 template <int BITS>
 __device__ __forceinline__ int quad_at(int h) {
   const int lane = threadIdx.x & 31;

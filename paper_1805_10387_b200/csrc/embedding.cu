@@ -70,8 +70,13 @@ mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_
 //    into the next tile is finished by the tile in which it begins; a run over three tiles or more leaves
 //    one FP32 partial row in each tile.
 // 3. The partial rows of such runs are added in order.
-// dY is read once and dW written once (rows with tokens twice): HBM bounds it.  No floating-point
-// atomics: the order of every sum follows from the ids alone.
+// dY is read once and dW written once (rows with tokens twice).  No floating-point atomics: the order of
+// every sum follows from the ids alone.  Measured on a B200: 8192 x 1024 into 32768 rows 30 us (sort 11 with the zeros
+// beside it, sums 8, join 5, and the gaps), 25600 x 1600 into 29 rows 35 us; HBM alone would need 13 each.  What
+// is left is the latency of the sort's passes (about 5 us each: ids, counts, scan over the cluster, placement) and of
+// three dependent kernels.  A block per table row that looked through all ids took 639 and 3051 us.  Tried without
+// gain: fetching dY into L2 during the sort (the sums are not bound by HBM's latency), 16 rows in flight per
+// thread instead of 8 (fewer blocks fit).
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kMostBits = 8, kHistPitch = (1 << kMostBits) + 1;   // odd pitch: a quad's four rows lie in four banks
 constexpr int kTileRound = 128;                  // the sorted lists are filled up to a multiple of this and of every tile

@@ -15,8 +15,12 @@ namespace {
 // thread waits for another's copy; the row stays in registers and shared memory between the norms, so
 // that everything is read once and written once.  What depends on the column alone (the gains, the
 // gate vector) stays in the thread's registers over all rows.
-// An element costs 8 B of HBM traffic forward and 12 B backward (FP16, shared gate) against some 17 and 36
-// instructions: HBM bounds both if the instructions stay few.
+// An element costs 8 B of HBM traffic forward and 12 B backward (FP16, shared gate), and some 20 and 50
+// instructions.  Measured on a B200: forward 8192 x 1024 16.4 us (4.1 TB/s), backward 25600 x 1600 112 us (4.4 TB/s):
+// backward the instructions weigh as much as HBM (half of the issue slots; a fifth of the lanes idle at a width of
+// 1600).  One row per block without prefetch took 70 and 2184 us, rows in registers of groups that come and
+// go 22.6 us forward.  Tried for the backward pass and slower: 1024 threads with one vector each (150 us, spilled
+// registers), 384 threads (125 us), the rows' addresses recomputed instead of kept (122 us).
 constexpr int kRowThreads = 512, kC = 2;
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {
@@ -783,6 +787,8 @@ int mp_block_norm_fwd(int kind, float eps, float res_scale, const void* x, int x
       bad_ptr16(y16) || bad_ptr16(g_post16) || bad_ptr16(gate16) || bad_ptr16(x_out) || bad_ptr16(g_pre16) ||
       bad_ptr16(n16) || bad_ptr16(stats))
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: buffers must be 16-byte aligned, rows start on 16-byte boundaries", name);
+  if ((x_out && x_out == x && ldxo != ldx) || (n16 && n16 == y16 && ldn != ldy))
+    return mp::set_error(MP_ERR_INVALID_ARG, "%s: a result in an input's place needs its pitch", name);
   if (int rc = mp::check_device()) return rc;
   if (M == 0) return MP_OK;
   const FwdArgs a{eps, res_scale, x, ldx, (const uint16_t*)y16, ldy, (const uint16_t*)g_post16, (const uint16_t*)gate16,
@@ -827,6 +833,9 @@ int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn,
       bad_ptr16(stats) || bad_ptr16(dx) || bad_ptr16(dy16) || bad_ptr16(dg_post16) || bad_ptr16(dgate16) ||
       bad_ptr16(dg_pre16) || bad_ptr16(workspace))
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: buffers must be 16-byte aligned, rows start on 16-byte boundaries", name);
+  if ((dx && dx == dx_out && lddx != lddxo) || (dy16 && ((dy16 == dn16 && lddy != lddn) || (dy16 == y16 && lddy != ldy))) ||
+      (dgate16 && dgate16 == gate16 && lddgate != ldgate))
+    return mp::set_error(MP_ERR_INVALID_ARG, "%s: a result in an input's place needs its pitch", name);
   const size_t need = mp_block_norm_bwd_workspace_bytes(M, D);
   if (!workspace || workspace_bytes < need)
     return mp::set_error(MP_ERR_NOMEM, "%s: workspace of %zu bytes needed", name, need);

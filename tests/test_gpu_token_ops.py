@@ -464,6 +464,36 @@ def test_block_norm_rows_past_32_bit_offsets(mp):
     assert not x[0].any() and not dn[70000].any()
 
 
+@pytest.mark.parametrize("M,D", [(1, 3), (9, 10), (40, 1001), (5, 2500), (3, 8201)])
+@pytest.mark.parametrize("kind", [0, 1])
+def test_fp32_rows_that_start_every_four_elements(mp, M, D, kind):
+    """The FP32 residual with the narrowest pitch: the same bits as with a wide one, and nothing past the rows."""
+    g, x, y, gp, gq, gt = norm_inputs(M, D, 1, "shared", 6)
+    pitch = up(D, 4)
+
+    def narrow(fill=None):
+        buf = torch.full((M * pitch + 8,), 7.0, device="cuda")
+        view = buf[:M * pitch].view(M, pitch)[:, :D]
+        if fill is not None:
+            view.copy_(fill)
+        return view, lambda: bool((buf[M * pitch:] == 7).all() and (buf[:M * pitch].view(M, pitch)[:, D:] == 7).all())
+    half = lambda: torch.zeros(M, up(D), dtype=torch.float16, device="cuda")[:, :D]  # noqa: E731
+    vec = lambda: torch.zeros(up(D), dtype=torch.float16, device="cuda")[:D]  # noqa: E731
+    y, dn, upg = y.contiguous() if D % 8 == 0 else padded(y)[0], padded(rand(g, M, D))[0], rand(g, M, D, dtype=torch.float32)
+    ws = torch.empty(mp.mp_block_norm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device="cuda")
+    got = []
+    for make in (narrow, lambda fill=None: (padded(fill)[0] if fill is not None else out(M, D, torch.float32)[0], lambda: True)):
+        (xi, _), (xo, ok1), (ui, _), (dx, ok2) = make(x), make(), make(upg), make()
+        nn, stats, dy = half(), torch.zeros(M, 4, device="cuda"), half()
+        dg = [vec() for _ in range(3)]
+        mp.mp_block_norm_fwd(xi, gq, nn, stats, y16=y, g_post16=gp, gate16=gt, x_out=xo, kind=kind)
+        mp.mp_block_norm_bwd(dn, xo, gq, stats, dx, dg[0], dx_out=ui, y16=y, g_post16=gp, gate16=gt, dy16=dy, dg_post16=dg[1],
+                             dgate16=dg[2], kind=kind, workspace=ws)
+        assert ok1() and ok2()
+        got.append([t.clone() for t in (xo, nn, stats, dx, dy, *dg)])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 # ------------------------------------------------------------------------------ policy loss
 
 def loss64(z, t, old, ref, adv, w, lo, hi, kl, scale, V):

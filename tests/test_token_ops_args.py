@@ -93,6 +93,15 @@ def test_block_norm_refusals(p16):
     need = mp.mp_block_norm_bwd_workspace_bytes(4, 8)
     assert need > 0 and _norm_bwd(L, p16, nb=need - 1) == NOMEM
     assert mp.mp_block_norm_bwd_workspace_bytes(4, mp.MP_NORM_MAX_D + 1) == 0
+    # a result in an input's place has its pitch
+    q = p16 + 1024
+    apart = dict(x=q, y=q + 256, n=q + 512, xo=q + 768)
+    for a, b in (("x", "xo"), ("y", "n")):
+        assert _norm_fwd(L, p16, **{**apart, a: p16, b: p16, "ld" + b: 16}) == INV
+    for a, b in (("up", "dx"), ("dn", "dy"), ("y", "dy")):
+        k = dict(up=q, dn=q + 128, y=q + 256, dx=q + 384, dy=q + 512)
+        assert _norm_bwd(L, p16, **{**k, a: p16, b: p16, "ld" + b: 16}) == INV
+    assert _norm_bwd(L, p16, gate=p16, dgate=p16, ldgate=8, lddgate=16, dx=q, dy=q + 128) == INV
     # FP32 rows may start every 4 elements (M = 0: nothing is launched)
     assert _norm_fwd(L, p16, xb=4, ldx=12, ldxo=12, M=0) not in (INV, ALIGN)
     assert _norm_fwd(L, p16, xb=4, ldx=10, ldxo=12, M=0) == ALIGN
@@ -117,6 +126,7 @@ def test_policy_loss_refusals(p16):
     assert _loss(L, p16, N=-1) == INV and _loss(L, p16, V=0) == INV and _loss(L, p16, idb=3) == INV
     big = 524288 + 8
     assert _loss(L, p16, V=big, ldl=big, lddl=big) == LARGE
+    assert _loss(L, p16, dz=p16, lddl=16) == INV
     assert _loss(L, p16, ldl=4) == INV and _loss(L, p16, lddl=4) == INV
     assert _loss(L, p16, ldl=12) == ALIGN and _loss(L, p16, lddl=12) == ALIGN
     assert _loss(L, p16, z=p16 + 2) == ALIGN and _loss(L, p16, t=p16 + 4) == ALIGN and _loss(L, p16, adv=p16 + 2) == ALIGN
