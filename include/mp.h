@@ -349,8 +349,8 @@ size_t mp_block_norm_bwd_workspace_bytes(int64_t M, int64_t D);
  *   dz_j = rn16( grad_scale * S * w * dl/dlp * ([j = t] - exp(z_j) / sum exp(z)) )
  * S: the loss scale of `state` (1 without a state).  Where r A equals its clipped value the gradient is
  * that of r A.  logp[i] = lp, token_loss[i] = w l, loss[0] = sum_i token_loss[i] (fixed order; may be
- * NULL).  A row of weight 0 is masked: nothing of it is read, its outputs are 0.  ref_logp NULL: no
- * KL term.  A target outside 0 .. V-1 in a row that is not masked gives NaN for the row's outputs
+ * NULL).  A row of weight 0 is masked: nothing of it is read, its outputs are 0.  ref_logp NULL or
+ * kl_coef 0: no KL term.  A target outside 0 .. V-1 in a row that is not masked gives NaN for the row's outputs
  * and sets state->status.  logits16 [N,V] ldl >= V, dlogits16 [N,V] lddl >= V; dlogits16 may be
  * logits16 itself (same pitch), or NULL for the forward pass alone.  targets: N integers of id_bytes
  * (4 or 8) bytes.  N = 0 is legal (loss 0).  V is at most MP_POLICY_MAX_V. */

@@ -58,8 +58,10 @@ __device__ __forceinline__ Token load_token(const LossArgs& a, int64_t i) {
 }
 __device__ __forceinline__ void token_terms(const LossArgs& a, const Token& t, float lp, float& loss, float& dlp) {
   const float A = t.advantage;
-  const float r = expf(lp - t.old_logp);
-  const float plain = r * A, clipped = fminf(fmaxf(r, 1.0f - a.lo), 1.0f + a.hi) * A;
+  const float x = lp - t.old_logp, r = expf(x);
+  // a ratio past FP32 is finite all the same where its exponent is: 0 times it is 0, not a NaN
+  const bool none = A == 0.0f && x < INFINITY;
+  const float plain = none ? A : r * A, clipped = none ? A : fminf(fmaxf(r, 1.0f - a.lo), 1.0f + a.hi) * A;
   loss = plain <= clipped ? -plain : -clipped;
   dlp = plain <= clipped ? -plain : 0.0f;
   if (plain != plain) loss = dlp = plain;          // a NaN shows in the loss and the gradient
@@ -537,7 +539,8 @@ int mp_policy_loss(const void* logits16, int64_t ldl, const void* targets, int i
   if (!cfg) return mp::set_error(MP_ERR_INVALID_ARG, "mp_policy_loss: null configuration");
   if (!(cfg->clip_lo >= 0.0f) || !(cfg->clip_hi >= 0.0f) || !isfinite(cfg->kl_coef) || !isfinite(cfg->grad_scale))
     return mp::set_error(MP_ERR_INVALID_ARG, "mp_policy_loss: bad configuration");
-  const LossArgs a{(const uint16_t*)logits16, ldl, targets, id_bytes, old_logp, ref_logp, advantage, weight, N, V,
+  const float* ref = cfg->kl_coef != 0.0f ? ref_logp : nullptr;   // a factor of 0: no KL term, however far ref_logp is
+  const LossArgs a{(const uint16_t*)logits16, ldl, targets, id_bytes, old_logp, ref, advantage, weight, N, V,
                    cfg->clip_lo, cfg->clip_hi, cfg->kl_coef, cfg->grad_scale, (uint16_t*)dlogits16, lddl, logp,
                    token_loss, state ? state->dev : nullptr};
   return launch("mp_policy_loss", a, loss, true, stream);
