@@ -71,8 +71,8 @@ mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_
 //    one FP32 partial row in each tile.
 // 3. The partial rows of such runs are added in order.
 // dY is read once and dW written once (rows with tokens twice).  No floating-point atomics: the order of
-// every sum follows from the ids alone.  Measured on a B200: 8192 x 1024 into 32768 rows 30 us (sort 11 with the zeros
-// beside it, sums 8, join 5, and the gaps), 25600 x 1600 into 29 rows 35 us; HBM alone would need 13 each.  What
+// every sum follows from the ids alone.  Measured on a B200: 8192 x 1024 into 32768 rows 33 us (sort 11 with the zeros
+// beside it, sums 8, join 7, and the gaps), 25600 x 1600 into 29 rows 37 us; HBM alone would need 13 each.  What
 // is left is the latency of the sort's passes (about 5 us each: ids, counts, scan over the cluster, placement) and of
 // three dependent kernels.  A block per table row that looked through all ids took 639 and 3051 us.  Tried without
 // gain: fetching dY into L2 during the sort (the sums are not bound by HBM's latency), 16 rows in flight per
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const 
   const int64_t t = (int64_t)blockIdx.x * groups + group, begin = (int64_t)blockIdx.x * groups * a.tile;
   const int col = (blockIdx.y * cols + threadIdx.x % cols) * 8;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the sorted lists and the zeros are complete
-  ptx::launch_dependents();                      // the join kernel may look through the lists meanwhile
+  ptx::launch_dependents();                      // the join kernel's blocks take the places of those that are done
   for (int x = threadIdx.x; x < window; x += blockDim.x) {
     const int64_t p = begin + x;
     s_list[x] = p < a.n_round ? make_int2(__ldcg(a.key + p), __ldcg(a.pos + p)) : make_int2(INT_MAX, 0);
@@ -422,12 +422,14 @@ __global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const 
 // Runs over three tiles or more: the tile in which one begins left its part, every further tile its own.  A block
 // looks through its share of the tiles for the beginnings of such runs; 4 groups of 64 threads (4
 // columns each) add the parts of a run in 4 pieces, and the pieces in order.
+// (Looking through the lists before the wait on the sum kernel would hide 2 us, but only what follows the wait is
+// promised to see them.)
 constexpr int kJoinThreads = 256, kJoinGroups = 4, kJoinLanes = kJoinThreads / kJoinGroups, kJoinCols = kJoinLanes * 4;
 __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles) {
   __shared__ float4 sm[kJoinGroups][kJoinLanes];
   const int group = threadIdx.x / kJoinLanes, col = blockIdx.y * kJoinCols + (threadIdx.x % kJoinLanes) * 4;
-  // (the lists were complete before the sum kernel let this one start: looking through them needs no wait)
-  bool bad = false, waited = false;
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // the lists and the partial rows are complete and visible
+  bool bad = false;
   for (int64_t t0 = blockIdx.x; t0 < tiles; t0 += (int64_t)gridDim.x * kJoinThreads) {
     // thread x looks at tile t0 + x * blocks
     const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
@@ -456,8 +458,6 @@ __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const S
         more += here;
         if (here < kJoinThreads) break;
       }
-      if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // the partial rows are complete
-      waited = true;
       const int parts = more + 1, per = (parts + kJoinGroups - 1) / kJoinGroups;
       const int from = group * per, to = from + per < parts ? from + per : parts;
       float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -487,7 +487,6 @@ __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const S
     }
     __syncthreads();
   }
-  if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");     // no block is done before the sum kernel is
   if (bad && a.st) atomicOr(&a.st->h.found_inf, 1);
 }
 

@@ -36,3 +36,24 @@ def test_a_ratio_past_fp32_times_a_zero_factor_is_zero(mp, V):
             assert torch.isnan(tl[5]) and torch.isnan(dz[5]).all()                  # a NaN shows whatever the advantage is
     mp.mp_policy_loss(z, t, lp, adv, w, got, tl, dlogits16=dz, ref_logp=ref, kl_coef=0.1)    # a KL term that is meant
     assert (tl == math.inf).all()
+
+
+def test_calls_that_follow_one_another_in_one_workspace(mp):
+    """Batches whose long runs lie elsewhere, one after the other without a pause: no call may see the sorted
+    tokens or the partial rows of the call before it."""
+    V, D, n = 900, 200, 30000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    ws = torch.empty(mp.mp_embedding_bwd_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda")
+    cases = []
+    for k in range(8):                                    # exact sums: small whole numbers
+        ids = torch.randint(0, V, (n,), generator=g, device="cuda")
+        start = 3000 * k
+        ids[start:start + 9000] = (131 * k) % V
+        dY = torch.randint(-2, 3, (n, D), generator=g, device="cuda").half()
+        want = torch.zeros(V, D, dtype=torch.float64, device="cuda").index_add_(0, ids, dY.double())
+        cases.append((ids, dY, want.half()))
+    outs = [torch.full((V, D), 7.0, dtype=torch.float16, device="cuda") for _ in range(80)]
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        mp.mp_embedding_bwd(cases[i % 8][0], cases[i % 8][1], o, workspace=ws)
+    assert all(torch.equal(o, cases[i % 8][2]) for i, o in enumerate(outs))
