@@ -337,12 +337,14 @@ __device__ __forceinline__ bool store_row(const SumArgs& a, int key, int col, co
 }
 
 constexpr int kSumThreads = 256, kMostGroups = 32;
-__global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const SumArgs a, int cols, int groups, int tiles) {
-  // cols: vectors of 8 columns that a group of threads covers; blockIdx.y picks them
+__global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const SumArgs a, int cols, int groups, int tiles, unsigned across) {
+  // cols: vectors of 8 columns that a group of threads covers; across: blocks over the tiles.  The blocks over the columns
+  // are numbered after them in x, since a grid's y ends at 65535 and a row may need more
   extern __shared__ int2 s_list[];               // (key, position) of the groups' tiles and of the tile after them
   const int group = threadIdx.x / cols, window = (groups + 1) * a.tile;
-  const int64_t t = (int64_t)blockIdx.x * groups + group, begin = (int64_t)blockIdx.x * groups * a.tile;
-  const int col = (blockIdx.y * cols + threadIdx.x % cols) * 8;
+  const unsigned down = blockIdx.x / across, along = blockIdx.x - down * across;
+  const int64_t t = (int64_t)along * groups + group, begin = (int64_t)along * groups * a.tile;
+  const int col = (down * cols + threadIdx.x % cols) * 8;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the sorted lists and the zeros are complete
   ptx::launch_dependents();                      // the join kernel's blocks take the places of those that are done
   for (int x = threadIdx.x; x < window; x += blockDim.x) {
@@ -425,14 +427,15 @@ __global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const 
 // (Looking through the lists before the wait on the sum kernel would hide 2 us, but only what follows the wait is
 // promised to see them.)
 constexpr int kJoinThreads = 256, kJoinGroups = 4, kJoinLanes = kJoinThreads / kJoinGroups, kJoinCols = kJoinLanes * 4;
-__global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles) {
+__global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles, unsigned across) {
   __shared__ float4 sm[kJoinGroups][kJoinLanes];
-  const int group = threadIdx.x / kJoinLanes, col = blockIdx.y * kJoinCols + (threadIdx.x % kJoinLanes) * 4;
+  const unsigned down = blockIdx.x / across, along = blockIdx.x - down * across;
+  const int group = threadIdx.x / kJoinLanes, col = down * kJoinCols + (threadIdx.x % kJoinLanes) * 4;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the lists and the partial rows are complete and visible
   bool bad = false;
-  for (int64_t t0 = blockIdx.x; t0 < tiles; t0 += (int64_t)gridDim.x * kJoinThreads) {
+  for (int64_t t0 = along; t0 < tiles; t0 += (int64_t)across * kJoinThreads) {
     // thread x looks at tile t0 + x * blocks
-    const int64_t t = t0 + (int64_t)threadIdx.x * gridDim.x;
+    const int64_t t = t0 + (int64_t)threadIdx.x * across;
     bool begins = false;
     if (t < tiles) {
       const int64_t p0 = t * a.tile, p1 = p0 + a.tile;
@@ -449,7 +452,7 @@ __global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const S
         if (found[x >> 5] >> (x & 31) == 0) x |= 31;   // none in the rest of this word
         continue;
       }
-      const int64_t b = t0 + (int64_t)x * gridDim.x;
+      const int64_t b = t0 + (int64_t)x * across;
       const int key = key_of(a, (b + 1) * a.tile - 1);
       // further tiles whose first token is of this id
       int more = 0;
@@ -639,7 +642,8 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   int groups = kSumThreads / cols;
   if (groups > kMostGroups) groups = kMostGroups;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((tiles + groups - 1) / groups), (unsigned)((vecs + cols - 1) / cols), 1);
+  unsigned across = (unsigned)((tiles + groups - 1) / groups);
+  cfg.gridDim = dim3(across * (unsigned)((vecs + cols - 1) / cols), 1, 1);
   cfg.blockDim = dim3((unsigned)round_up(cols * groups, 32), 1, 1);
   cfg.dynamicSmemBytes = (size_t)(groups + 1) * m.tile * sizeof(int2);      // 33 KiB at most
   cfg.stream = st;
@@ -648,13 +652,14 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, groups, tiles));
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, groups, tiles, across));
   mp::count_launch();
   if (tiles < 3) return MP_OK;         // no run over three tiles
-  cfg.gridDim = dim3((unsigned)(tiles < 148 ? tiles : 148), (unsigned)((m.D4 + kJoinCols - 1) / kJoinCols), 1);
+  across = (unsigned)(tiles < 148 ? tiles : 148);
+  cfg.gridDim = dim3(across * (unsigned)(((int64_t)m.D4 + kJoinCols - 1) / kJoinCols), 1, 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
-  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles));
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles, across));
   mp::count_launch();
   return MP_OK;
 }

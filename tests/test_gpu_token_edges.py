@@ -57,3 +57,22 @@ def test_calls_that_follow_one_another_in_one_workspace(mp):
     for i, o in enumerate(outs):
         mp.mp_embedding_bwd(cases[i % 8][0], cases[i % 8][1], o, workspace=ws)
     assert all(torch.equal(o, cases[i % 8][2]) for i, o in enumerate(outs))
+
+
+def test_embedding_gradient_of_rows_wider_than_a_grid_is_high(mp):
+    """17 million columns: more blocks over the columns than a grid's second dimension holds.  Whole numbers, so exact."""
+    n, V, D = 300, 2, 17_000_008
+    dY = torch.empty(n, D, dtype=torch.float16, device="cuda")
+    col = torch.arange(D, device="cuda", dtype=torch.int32)
+    ids = torch.zeros(n, dtype=torch.int64, device="cuda")
+    ids[::3] = 1                                          # runs of 100 and 200 tokens: over one tile, over three
+    ids = 1 - ids
+    want = torch.zeros(V, D, dtype=torch.float32, device="cuda")
+    rows = ids.tolist()
+    for i in range(n):
+        dY[i] = ((col + 7 * i) % 5 - 2).half()
+        want[rows[i]] += dY[i].float()
+    dW = torch.full((V, D), 7.0, dtype=torch.float16, device="cuda")
+    ws = torch.empty(mp.mp_embedding_bwd_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda")
+    mp.mp_embedding_bwd(ids, dY, dW, workspace=ws)
+    assert torch.equal(dW, want.half())
