@@ -16,11 +16,7 @@
 #include <math.h>
 #include <string.h>
 
-#include <map>
-#include <mutex>
 #include <new>
-#include <type_traits>
-#include <utility>
 #include <vector>
 
 #include "rows.cuh"
@@ -396,21 +392,18 @@ mp_adamw_update_kernel(const Tensor* tensors, int n_tensors, int64_t n_blocks, i
   }
 }
 
-// Blocks of `kernel` that are resident at once on the current device, asked once per device and kernel.
-int resident_blocks(const void* kernel, int* out) {
-  static std::mutex mu;
-  static std::map<std::pair<int, const void*>, int> cache;
+// Blocks of `kernel` that are resident at once on the current device; `known` is the kernel's own.
+int resident_blocks(const void* kernel, mp::PerDevice& known, int* out) {
   int dev = 0;
   MP_CUDA_TRY(cudaGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  int& have = cache[{dev, kernel}];
-  if (have == 0) {
+  *out = known.get(dev);
+  if (*out == 0) {
     int sms = 0, per = 0;
     MP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     MP_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, kThreads, 0));
-    have = sms * (per < 1 ? 1 : per);
+    *out = sms * (per < 1 ? 1 : per);
+    known.set(dev, *out);
   }
-  *out = have;
   return MP_OK;
 }
 
@@ -498,8 +491,9 @@ int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config*
   int* gemm_status = nullptr;
   if (int rc = mp::gemm_status_device_ptr(&gemm_status)) return rc;
   // One resident round of blocks; units as large as leaves every warp four.
-  auto shape = [&](const void* kernel, int most_unit, int* grid, int* unit) {
-    if (int rc = resident_blocks(kernel, grid)) return rc;
+  static mp::PerDevice known[3];
+  auto shape = [&](const void* kernel, mp::PerDevice& of_kernel, int most_unit, int* grid, int* unit) {
+    if (int rc = resident_blocks(kernel, of_kernel, grid)) return rc;
     const int64_t warps = (int64_t)*grid * (kThreads / 32);
     *unit = most_unit;
     while (*unit > 1 && plan->n_blocks < 4 * warps * *unit) *unit /= 2;
@@ -509,12 +503,12 @@ int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config*
   };
   int grid = 0, unit = 0;
   if (check_mode == 1) {
-    if (int rc = shape((const void*)mp_adamw_check_kernel, 1, &grid, &unit)) return rc;
+    if (int rc = shape((const void*)mp_adamw_check_kernel, known[0], 1, &grid, &unit)) return rc;
     mp_adamw_check_kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, unit, state->dev);
     mp::count_launch();
   }
   auto kernel = plan->bits == 32 ? mp_adamw_update_kernel<32> : mp_adamw_update_kernel<8>;
-  if (int rc = shape((const void*)kernel, plan->bits == 32 ? 1 : kMostUnit, &grid, &unit)) return rc;
+  if (int rc = shape((const void*)kernel, known[plan->bits == 32 ? 1 : 2], plan->bits == 32 ? 1 : kMostUnit, &grid, &unit)) return rc;
   kernel<<<grid, kThreads, 0, st>>>(plan->d_tensors, plan->n_tensors, plan->n_blocks, unit, state->dev, *opt, gemm_status);
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());

@@ -6,6 +6,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <atomic>
+
 #include "mp.h"
 
 // Device-resident state.  Its head has the exact layout of mp_state_host so that a read is
@@ -32,6 +34,20 @@ int check_device();  // MP_OK if the current device is compute capability 10.x
 // Device address (on the current device) of the status word that the GEMM kernels set when a
 // bounded wait expires; defined beside those kernels.
 int gemm_status_device_ptr(int** out);
+
+// What a first call asks of the runtime, remembered for each device (0: not asked yet).  A fixed table without a lock:
+// an allocation may throw, and no exception may leave a C entry point.  Threads that both find 0 both ask.
+class PerDevice {
+ public:
+  int get(int dev) const { return dev >= 0 && dev < kMost ? value_[dev].load(std::memory_order_acquire) : 0; }
+  void set(int dev, int value) {
+    if (dev >= 0 && dev < kMost) value_[dev].store(value, std::memory_order_release);
+  }
+
+ private:
+  static constexpr int kMost = 64;     // devices past these are asked in every call
+  std::atomic<int> value_[kMost] = {};
+};
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

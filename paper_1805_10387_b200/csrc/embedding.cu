@@ -1,8 +1,6 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 
 #include <climits>
-#include <map>
-#include <mutex>
 
 #include "ptx.cuh"
 #include "rows.cuh"
@@ -510,8 +508,7 @@ int check(const char* name, const void* ids, int id_bytes, const void* a16, int6
 // have left, and the zeros would take twice as long.)
 template <int CL>
 int sort_launch(const SortArgs& s, cudaStream_t st) {
-  static std::mutex mu;
-  static std::map<int, int> resident;
+  static mp::PerDevice resident;
   auto kernel = mp_embedding_sort_kernel<CL>;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(144, 1, 1);
@@ -525,15 +522,12 @@ int sort_launch(const SortArgs& s, cudaStream_t st) {
   cfg.numAttrs = 1;
   int dev = 0, clusters = 0;
   MP_CUDA_TRY(cudaGetDevice(&dev));
-  {
-    std::lock_guard<std::mutex> lock(mu);
-    int& have = resident[dev];
-    if (have == 0) {
-      MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-      MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&have, kernel, &cfg));
-      if (have < 2) have = 2;                    // the sort's and one that writes zeros
-    }
-    clusters = have;
+  clusters = resident.get(dev);
+  if (clusters == 0) {
+    MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+    if (clusters < 2) clusters = 2;              // the sort's and one that writes zeros
+    resident.set(dev, clusters);
   }
   cfg.gridDim = dim3((unsigned)(clusters * CL), 1, 1);
   MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, s));

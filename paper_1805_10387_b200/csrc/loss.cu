@@ -7,10 +7,6 @@
 
 #include <math.h>
 
-#include <map>
-#include <mutex>
-#include <utility>
-
 #include "ptx.cuh"
 #include "rows.cuh"
 
@@ -443,8 +439,7 @@ void group_launch(const LossArgs& a, cudaStream_t st) {
 // size of a block's part of a row).
 template <int CL>
 int row_launch(const LossArgs& a, cudaStream_t st) {
-  static std::mutex mu;
-  static std::map<std::pair<int, int>, int> resident;
+  static mp::PerDevice resident[MP_POLICY_MAX_V / 8 / (CL * kRowThreads) + 1];     // by layers
   const int64_t vecs = (a.V + 7) / 8, layers = (vecs + CL * kRowThreads - 1) / (CL * kRowThreads);
   const int smem = (int)layers * kRowThreads * 16;
   auto kernel = mp_policy_loss_row_kernel<CL>;
@@ -460,17 +455,13 @@ int row_launch(const LossArgs& a, cudaStream_t st) {
   cfg.numAttrs = 1;
   int dev = 0, clusters = 0;
   MP_CUDA_TRY(cudaGetDevice(&dev));
-  {
-    std::lock_guard<std::mutex> lock(mu);
-    int& have = resident[{dev, smem}];
-    if (have == 0) {
-      MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       MP_POLICY_MAX_V / 8 * 2));
-      cfg.gridDim = dim3(CL * 148 * 16, 1, 1);
-      MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&have, kernel, &cfg));
-      if (have < 1) have = 1;
-    }
-    clusters = have;
+  clusters = resident[layers].get(dev);
+  if (clusters == 0) {
+    MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MP_POLICY_MAX_V / 8 * 2));
+    cfg.gridDim = dim3(CL * 148 * 16, 1, 1);
+    MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+    if (clusters < 1) clusters = 1;
+    resident[layers].set(dev, clusters);
   }
   if (a.N < clusters) clusters = (int)a.N;
   cfg.gridDim = dim3((unsigned)(clusters * CL), 1, 1);

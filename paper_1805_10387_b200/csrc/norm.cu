@@ -1,9 +1,5 @@
 // Norms before and after a block, with the block's gate and the residual scale, forward and backward.
 
-#include <map>
-#include <mutex>
-#include <utility>
-
 #include "rows.cuh"
 
 namespace {
@@ -679,23 +675,18 @@ int64_t blocks_for(int64_t M, int64_t D) {
   return blocks < 1 ? 1 : blocks < kSms ? blocks : kSms;
 }
 
-// Lets a kernel use `bytes` of dynamic shared memory; asked of the runtime once per device and kernel.
-int allow_smem(const void* kernel, size_t bytes) {
-  static std::mutex mu;
-  static std::map<std::pair<int, const void*>, size_t> allowed;
-  int dev = 0;
-  MP_CUDA_TRY(cudaGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  size_t& have = allowed[{dev, kernel}];
-  if (have >= bytes) return MP_OK;
-  MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
-  have = bytes;
-  return MP_OK;
-}
-
 // Stages of `slots` 16-byte slots per thread that fit the shared memory, 2 to 4 (the slots of a stage are 14 at
 // most, 112 KiB, so two always fit).
 constexpr size_t kMostSmem = 224 << 10;
+// Lets a kernel use that much dynamic shared memory; `allowed` is the kernel's own.
+int allow_smem(const void* kernel, mp::PerDevice& allowed) {
+  int dev = 0;
+  MP_CUDA_TRY(cudaGetDevice(&dev));
+  if (allowed.get(dev)) return MP_OK;
+  MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem));
+  allowed.set(dev, 1);
+  return MP_OK;
+}
 size_t stages_for(int slots, int* stages) {
   const size_t stage = (size_t)slots * kRowThreads * 16;
   const int fit = (int)(kMostSmem / stage);
@@ -705,11 +696,12 @@ size_t stages_for(int slots, int* stages) {
 
 template <class XT, int TPR>
 int fwd_launch(FwdArgs a, bool layer, int blocks, cudaStream_t st) {
+  static mp::PerDevice allowed[2];
   const int xs = sizeof(XT) / 2;
   a.slots = kC * (xs + (a.g_post ? 1 : 0) + (a.gate && a.ldgate ? 1 : 0));
   const size_t smem = stages_for(a.slots, &a.stages);
   auto kernel = layer ? mp_block_norm_fwd_kernel<XT, TPR, true> : mp_block_norm_fwd_kernel<XT, TPR, false>;
-  if (int rc = allow_smem((const void*)kernel, kMostSmem)) return rc;
+  if (int rc = allow_smem((const void*)kernel, allowed[layer])) return rc;
   kernel<<<blocks, kRowThreads, smem, st>>>(a);
   return MP_OK;
 }
@@ -732,6 +724,7 @@ int fwd_dispatch(const FwdArgs& a, bool layer, int blocks, cudaStream_t st) {
 
 template <class XT, int TPR>
 int bwd_launch(BwdArgs a, int blocks, cudaStream_t st) {
+  static mp::PerDevice allowed[4];
   const bool matrix = a.gate != nullptr && a.ldgate != 0, layer = a.kind == MP_NORM_LAYER;
   const int xs = sizeof(XT) / 2;
   a.slots = kC * (xs + (a.dx_out ? xs : 0) + 1 + (a.g_post ? 1 : 0) + (matrix ? 1 : 0));
@@ -740,15 +733,16 @@ int bwd_launch(BwdArgs a, int blocks, cudaStream_t st) {
   if (smem < sums) smem = sums;
   auto kernel = layer ? matrix ? mp_block_norm_bwd_kernel<XT, TPR, true, true> : mp_block_norm_bwd_kernel<XT, TPR, true, false>
                       : matrix ? mp_block_norm_bwd_kernel<XT, TPR, false, true> : mp_block_norm_bwd_kernel<XT, TPR, false, false>;
-  if (int rc = allow_smem((const void*)kernel, kMostSmem)) return rc;
+  if (int rc = allow_smem((const void*)kernel, allowed[2 * layer + matrix])) return rc;
   kernel<<<blocks, kRowThreads, smem, st>>>(a);
   return MP_OK;
 }
 template <class XT>
 int bwd_dispatch(const BwdArgs& a, int blocks, cudaStream_t st) {
   if (a.D > kWide) {
+    static mp::PerDevice allowed;
     const size_t smem = (size_t)2 * a.D * sizeof(float);
-    if (int rc = allow_smem((const void*)mp_block_norm_bwd_wide_kernel<XT>, smem)) return rc;
+    if (int rc = allow_smem((const void*)mp_block_norm_bwd_wide_kernel<XT>, allowed)) return rc;
     mp_block_norm_bwd_wide_kernel<XT><<<blocks, kRowThreads, smem, st>>>(a);
     return MP_OK;
   }

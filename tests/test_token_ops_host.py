@@ -127,3 +127,32 @@ def test_the_embedding_gradient_of_very_wide_rows_fits_the_grid(child):
             lines = record()
             assert sum(l.startswith("launch") for l in lines) in (2, 3), lines
     """)
+
+
+def test_no_exception_leaves_a_call_on_a_host_without_memory(child):
+    """A first call of every kind while the host can allocate nothing: it returns (an error or not), it does not end the process."""
+    child("""
+    p32, p8 = plan(1000)[1], plan(1000, 8)[1]
+    fake.fake_no_memory(1)
+    results = [embed_bwd(100, 50, 64, 64), embed_bwd(20000, 50, 64, 64), update(p32), update(p8)]
+    results += [norm_fwd(4, D, xb) for D in (64, 512, 1024, 2048, 4096, 8192, 16384) for xb in (2, 4)]
+    results += [norm_bwd(4, D, xb) for D in (64, 512, 1024, 2048, 4096, 8192, 16384) for xb in (2, 4)]
+    results += [loss(4, V) for V in (29, 600, 20000, 50000, 131072)]
+    rc, _ = plan(1000)
+    fake.fake_no_memory(0)
+    assert results == [0] * len(results), results
+    assert rc == mp.MP_ERR_NOMEM
+    """)
+
+
+def test_attributes_and_occupancies_are_asked_once(child):
+    child("""
+    def asked(call):
+        assert call() == 0
+        return record().count("attribute")
+    for call in (lambda: embed_bwd(100, 50, 64, 64), lambda: norm_fwd(4, 512), lambda: norm_bwd(4, 512), lambda: norm_bwd(4, 16384),
+                 lambda: loss(4, 600), lambda: loss(4, 131072)):
+        assert asked(call) > 0 and asked(call) == 0
+    assert asked(lambda: norm_fwd(4, 1024)) > 0           # another kernel
+    assert asked(lambda: norm_fwd(4, 512, 4)) > 0
+    """)
