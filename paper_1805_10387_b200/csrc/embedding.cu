@@ -69,8 +69,8 @@ mp_embedding_fwd_kernel(const void* ids, int id_bytes, const uint16_t* W, int64_
 //    one FP32 partial row in each tile.
 // 3. The partial rows of such runs are added in order.
 // dY is read once and dW written once (rows with tokens twice).  No floating-point atomics: the order of
-// every sum follows from the ids alone.  Measured on a B200: 8192 x 1024 into 32768 rows 33 us (sort 11 with the zeros
-// beside it, sums 8, join 7, and the gaps), 25600 x 1600 into 29 rows 37 us; HBM alone would need 13 each.  What
+// every sum follows from the ids alone.  Measured on a B200: 8192 x 1024 into 32768 rows 31 us (sort 11 with the zeros
+// beside it, sums 8, join 5, and the gaps), 25600 x 1600 into 29 rows 37 us; HBM alone would need 13 each.  What
 // is left is the latency of the sort's passes (about 5 us each: ids, counts, scan over the cluster, placement) and of
 // three dependent kernels.  A block per table row that looked through all ids took 639 and 3051 us.  Tried without
 // gain: fetching dY into L2 during the sort (the sums are not bound by HBM's latency), 16 rows in flight per
@@ -422,12 +422,12 @@ __global__ void __launch_bounds__(kSumThreads, 3) mp_embedding_sum_kernel(const 
 // Runs over three tiles or more: the tile in which one begins left its part, every further tile its own.  A block
 // looks through its share of the tiles for the beginnings of such runs; 4 groups of 64 threads (4
 // columns each) add the parts of a run in 4 pieces, and the pieces in order.
-// (Looking through the lists before the wait on the sum kernel would hide 2 us, but only what follows the wait is
+// (Looking through the lists before the wait on the sum kernel would hide up to 2 us, but only what follows the wait is
 // promised to see them.)
 constexpr int kJoinThreads = 256, kJoinGroups = 4, kJoinLanes = kJoinThreads / kJoinGroups, kJoinCols = kJoinLanes * 4;
-__global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles, unsigned across) {
+__global__ void __launch_bounds__(kJoinThreads) mp_embedding_join_kernel(const SumArgs a, int tiles) {
   __shared__ float4 sm[kJoinGroups][kJoinLanes];
-  const unsigned down = blockIdx.x / across, along = blockIdx.x - down * across;
+  const unsigned down = blockIdx.x, along = blockIdx.y, across = gridDim.y;     // a row may need more blocks than y holds
   const int group = threadIdx.x / kJoinLanes, col = down * kJoinCols + (threadIdx.x % kJoinLanes) * 4;
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the lists and the partial rows are complete and visible
   bool bad = false;
@@ -636,7 +636,7 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   int groups = kSumThreads / cols;
   if (groups > kMostGroups) groups = kMostGroups;
   cudaLaunchConfig_t cfg = {};
-  unsigned across = (unsigned)((tiles + groups - 1) / groups);
+  const unsigned across = (unsigned)((tiles + groups - 1) / groups);
   cfg.gridDim = dim3(across * (unsigned)((vecs + cols - 1) / cols), 1, 1);
   cfg.blockDim = dim3((unsigned)round_up(cols * groups, 32), 1, 1);
   cfg.dynamicSmemBytes = (size_t)(groups + 1) * m.tile * sizeof(int2);      // 33 KiB at most
@@ -649,11 +649,10 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
   MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_sum_kernel, m, cols, groups, tiles, across));
   mp::count_launch();
   if (tiles < 3) return MP_OK;         // no run over three tiles
-  across = (unsigned)(tiles < 148 ? tiles : 148);
-  cfg.gridDim = dim3(across * (unsigned)(((int64_t)m.D4 + kJoinCols - 1) / kJoinCols), 1, 1);
+  cfg.gridDim = dim3((unsigned)(((int64_t)m.D4 + kJoinCols - 1) / kJoinCols), (unsigned)(tiles < 148 ? tiles : 148), 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.dynamicSmemBytes = 0;
-  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles, across));
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_embedding_join_kernel, m, tiles));
   mp::count_launch();
   return MP_OK;
 }
