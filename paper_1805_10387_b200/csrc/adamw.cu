@@ -461,7 +461,8 @@ int mp_adamw_plan_create(int n, void* const* g16, void* const* w32, void* const*
       mp_adamw_plan_destroy(p);
       return mp::set_error(MP_ERR_NOMEM, "%s: device allocation failed", name);
     }
-    const cudaError_t e = bytes ? cudaMemcpy(p->d_tensors, ts.data(), bytes, cudaMemcpyHostToDevice) : cudaSuccess;
+    cudaError_t e = bytes ? cudaMemcpy(p->d_tensors, ts.data(), bytes, cudaMemcpyHostToDevice) : cudaSuccess;
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);     // a pageable copy may return before it has arrived
     if (e != cudaSuccess) {
       mp_adamw_plan_destroy(p);
       return mp::set_error(MP_ERR_CUDA, "%s: %s", name, cudaGetErrorString(e));

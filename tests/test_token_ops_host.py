@@ -156,3 +156,13 @@ def test_attributes_and_occupancies_are_asked_once(child):
     assert asked(lambda: norm_fwd(4, 1024)) > 0           # another kernel
     assert asked(lambda: norm_fwd(4, 512, 4)) > 0
     """)
+
+
+def test_a_plan_waits_for_its_table(child):
+    """A copy from pageable memory returns when the bytes are staged; a stream that does not wait for the default
+    one may read the table at once, so the plan's call waits for the copy itself."""
+    child("""
+    for bits in (32, 8):
+        assert plan(1000, bits)[0] == 0
+        assert record() == ["copy", "wait"]
+    """)
