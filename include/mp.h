@@ -330,7 +330,7 @@ int mp_block_norm_fwd(int kind, float eps, float res_scale, const void* x, int x
  *   dg_pre = sum_rows dn * xhat,   dg_post = sum_rows gx * gate * yhat,
  *   dgate = gx * h, summed over the rows for a gate vector, [M,D] (lddgate >= D) for a gate matrix.
  * With g_post16 NULL: dx = gx, and y16, dy16, gate16, dg_post16, dgate16 must be NULL; dgate16 is
- * NULL exactly when gate16 is.  dx may be dx_out itself, dy16 may be dn16 or y16 itself, a gate
+ * NULL exactly when gate16 is.  dx may be dx_out or x_out itself, dy16 may be dn16 or y16 itself, a gate
  * matrix's dgate16 may be gate16 itself (same pitch).  The gradients of the gains and of a gate
  * vector are FP32 sums over the rows in a fixed order.  workspace: at least
  * mp_block_norm_bwd_workspace_bytes(M,D) bytes, 16-byte aligned. */

@@ -827,7 +827,7 @@ int mp_block_norm_bwd(int kind, float res_scale, const void* dn16, int64_t lddn,
       bad_ptr16(stats) || bad_ptr16(dx) || bad_ptr16(dy16) || bad_ptr16(dg_post16) || bad_ptr16(dgate16) ||
       bad_ptr16(dg_pre16) || bad_ptr16(workspace))
     return mp::set_error(MP_ERR_ALIGNMENT, "%s: buffers must be 16-byte aligned, rows start on 16-byte boundaries", name);
-  if ((dx && dx == dx_out && lddx != lddxo) || (dy16 && ((dy16 == dn16 && lddy != lddn) || (dy16 == y16 && lddy != ldy))) ||
+  if ((dx && ((dx == dx_out && lddx != lddxo) || (dx == x_out && lddx != ldxo))) || (dy16 && ((dy16 == dn16 && lddy != lddn) || (dy16 == y16 && lddy != ldy))) ||
       (dgate16 && dgate16 == gate16 && lddgate != ldgate))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: a result in an input's place needs its pitch", name);
   const size_t need = mp_block_norm_bwd_workspace_bytes(M, D);

@@ -166,3 +166,16 @@ def test_a_plan_waits_for_its_table(child):
         assert plan(1000, bits)[0] == 0
         assert record() == ["copy", "wait"]
     """)
+
+
+def test_a_gradient_in_the_place_of_the_norms_input_needs_its_pitch(child):
+    """With another pitch a row's gradient would lie over rows that other threads have yet to read."""
+    child("""
+    def call(dx, ld, M=40, D=64, x_bytes=2):
+        return L.mp_block_norm_bwd(0, 1.0, P, 64, None, 0, P + 8192, x_bytes, 64, None, 0, None, None, 0, P, P, dx, ld, None, 0, None,
+                                   None, 0, P, M, D, None, P, 1 << 40, None)
+    for xb in (2, 4):
+        assert call(P + 8192, 64, x_bytes=xb) == 0 and call(P + 16384, 72, x_bytes=xb) == 0
+        assert call(P + 8192, 72, x_bytes=xb) == mp.MP_ERR_INVALID_ARG
+        assert b"place" in L.mp_last_error()
+    """)
