@@ -298,7 +298,7 @@ int mp_embedding_fwd(const void* ids, int id_bytes, const void* W16, int64_t ldw
  * by id, in ascending i for each id, and the sums follow that order in FP32 (a long run of one id
  * as the sums of its pieces, in order).  An id out of range adds to nothing and sets state->status as above.
  * workspace: at least mp_embedding_bwd_workspace_bytes(n,V,D) bytes of device scratch, 16-byte
- * aligned.  n and V below 2^31 - 1. */
+ * aligned.  n below 2^31 - 129, V below 2^31 - 1. */
 int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t lddy, void* dW16, int64_t ldw,
                      int64_t n, int64_t V, int64_t D, int64_t pad_id, float scale, mp_state* state,
                      void* workspace, size_t workspace_bytes, void* stream);

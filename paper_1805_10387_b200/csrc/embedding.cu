@@ -584,7 +584,7 @@ int mp_embedding_bwd(const void* ids, int id_bytes, const void* dY16, int64_t ld
     return mp::set_error(MP_ERR_INVALID_ARG, "mp_embedding_bwd: null pointer");
   if (int rc = check("mp_embedding_bwd", ids, id_bytes, dY16, lddy, dW16, ldw, n, V, D)) return rc;
   if (n >= INT_MAX - kTileRound || V >= INT_MAX)
-    return mp::set_error(MP_ERR_TOO_LARGE, "mp_embedding_bwd: n and V must be below 2^31 - %d", kTileRound + 1);
+    return mp::set_error(MP_ERR_TOO_LARGE, "mp_embedding_bwd: n must be below 2^31 - %d and V below 2^31 - 1", kTileRound + 1);
   if (workspace && !mp::aligned16(workspace))
     return mp::set_error(MP_ERR_ALIGNMENT, "mp_embedding_bwd: workspace must be 16-byte aligned");
   const size_t need = mp_embedding_bwd_workspace_bytes(n, V, D);

@@ -179,3 +179,22 @@ def test_a_gradient_in_the_place_of_the_norms_input_needs_its_pitch(child):
         assert call(P + 8192, 72, x_bytes=xb) == mp.MP_ERR_INVALID_ARG
         assert b"place" in L.mp_last_error()
     """)
+
+
+def test_the_bounds_of_the_embedding_gradient_are_the_documented_ones(child):
+    child("""
+    def call(n, V):
+        rc = L.mp_embedding_bwd(P, 8, P, 8, P, 8, n, V, 8, -1, 1.0, None, P, 16, None)
+        return rc, L.mp_last_error().decode()
+    last = 2 ** 31 - 130
+    assert call(last, 5)[0] == mp.MP_ERR_NOMEM and mp.mp_embedding_bwd_workspace_bytes(last, 5, 8) > 16 * last
+    rc, text = call(last + 1, 5)
+    assert rc == mp.MP_ERR_TOO_LARGE and "n must be below 2^31 - 129" in text, text
+    assert mp.mp_embedding_bwd_workspace_bytes(last + 1, 5, 8) == 0
+    last = 2 ** 31 - 2
+    assert call(5, last)[0] == mp.MP_ERR_NOMEM
+    rc, text = call(5, last + 1)
+    assert rc == mp.MP_ERR_TOO_LARGE and "V below 2^31 - 1" in text, text
+    header = " ".join(open({root!r} + "/include/mp.h").read().replace(" * ", " ").split())
+    assert "n below 2^31 - 129, V below 2^31 - 1" in header
+    """.replace("{root!r}", repr(os.path.dirname(os.path.dirname(os.path.abspath(__file__))))))
