@@ -279,7 +279,8 @@ int mp_lstm_cell_bwd(const void* G16, int64_t ldg, const void* c_prev16, const v
  * gradient enters its top layer, and an AdamW update.  (The paper's models have an embedding and
  * train with Adam; it gives no arithmetic for these.)  Matrices are FP16 with row pitches that
  * are multiples of 8 and may have any width: what lies between the width and the pitch is not
- * written, and its values do not matter.  Sums, norms and softmax statistics are FP32; each
+ * written, and its values do not matter.  Rows and vectors of gains or gates are read in whole units
+ * of 16 bytes: what follows the last element inside its unit is read too, and dropped.  Sums, norms and softmax statistics are FP32; each
  * stored value is rounded once.  No call uses floating-point atomics: the same inputs give the
  * same bits.  Gradients arrive and leave multiplied by the loss scale; a call that is given a
  * state sets state->found_inf when a parameter gradient or logit gradient that it stores is inf

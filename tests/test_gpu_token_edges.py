@@ -76,3 +76,36 @@ def test_embedding_gradient_of_rows_wider_than_a_grid_is_high(mp):
     ws = torch.empty(mp.mp_embedding_bwd_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda")
     mp.mp_embedding_bwd(ids, dY, dW, workspace=ws)
     assert torch.equal(dW, want.half())
+
+
+@pytest.mark.parametrize("M,D,wide", [(5, 1, 0), (9, 33, 1), (3, 1001, 0), (2, 2501, 1), (2, 9001, 0)])
+@pytest.mark.parametrize("kind", [0, 1])
+def test_what_follows_gains_and_gates_does_not_matter(mp, M, D, wide, kind):
+    """Vectors whose length is no multiple of 8, with NaN behind them and with zeros: the same bits, and none of it written."""
+    g = torch.Generator(device="cuda").manual_seed(D)
+    wide_d = -(-D // 8) * 8
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").half()  # noqa: E731
+    mats = {k: rnd(M, wide_d)[:, :D] for k in ("y", "dn")}
+    xt = torch.float32 if wide else torch.float16
+    x, up = (torch.randn(M, wide_d, generator=g, device="cuda").to(xt)[:, :D] for _ in range(2))
+    vecs = [rnd(D) for _ in range(3)]
+    results = []
+    for fill in (float("nan"), 0.0):
+        def vec(v=None):
+            b = torch.full((wide_d + 8,), fill, dtype=torch.float16, device="cuda")
+            if v is not None:
+                b[:D] = v
+            return b
+        bufs = [vec(v) for v in vecs]
+        gp, gq, gt = (b[:D] for b in bufs)
+        outs = [vec() for _ in range(3)]
+        new = lambda t: torch.zeros(M, wide_d, dtype=t, device="cuda")[:, :D]  # noqa: E731
+        xo, n, dx, dy, stats = new(xt), new(torch.float16), new(xt), new(torch.float16), torch.zeros(M, 4, device="cuda")
+        ws = torch.empty(mp.mp_block_norm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device="cuda")
+        mp.mp_block_norm_fwd(x, gq, n, stats, y16=mats["y"], g_post16=gp, gate16=gt, x_out=xo, kind=kind)
+        mp.mp_block_norm_bwd(mats["dn"], xo, gq, stats, dx, outs[0][:D], dx_out=up, y16=mats["y"], g_post16=gp, gate16=gt, dy16=dy,
+                             dg_post16=outs[1][:D], dgate16=outs[2][:D], kind=kind, workspace=ws)
+        for b in bufs + outs:
+            assert torch.isnan(b[D:]).all() if fill != fill else not b[D:].any()
+        results.append([t.clone() for t in (xo, n, dx, dy, stats, *(o[:D] for o in outs))])
+    assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(*results))
