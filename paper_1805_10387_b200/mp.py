@@ -152,10 +152,16 @@ def _check(rc: int):
         raise MpError(rc, lib().mp_last_error().decode())
 
 
+# Not part of torch's public interface: without them the public call answers.
+_raw_stream, _device = (getattr(torch._C, k, None) for k in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+
+
 def _stream():
     """The current torch stream of the current device (read without building a Stream object: the small calls
     are bound by the host, and that alone took 3 us of them)."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if _raw_stream is None or _device is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_device())
 
 
 def _dev(t: torch.Tensor, dtype) -> int:

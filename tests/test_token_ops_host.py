@@ -198,3 +198,17 @@ def test_the_bounds_of_the_embedding_gradient_are_the_documented_ones(child):
     header = " ".join(open({root!r} + "/include/mp.h").read().replace(" * ", " ").split())
     assert "n below 2^31 - 129, V below 2^31 - 1" in header
     """.replace("{root!r}", repr(os.path.dirname(os.path.dirname(os.path.abspath(__file__))))))
+
+
+def test_the_stream_is_found_without_the_private_functions_of_torch(monkeypatch):
+    import importlib.util
+    import types
+    import torch
+    for gone in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        with monkeypatch.context() as m:
+            m.delattr(torch._C, gone, raising=False)
+            m.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=1234))
+            spec = importlib.util.find_spec("paper_1805_10387_b200.mp")
+            fresh = importlib.util.module_from_spec(spec)          # a second copy: the first one keeps its functions
+            spec.loader.exec_module(fresh)
+            assert fresh._stream() == 1234, gone
