@@ -240,12 +240,12 @@ __device__ __forceinline__ uint4 live8(uint4 q, int nv) {
 }
 __device__ __forceinline__ uint4 no_words() { return make_uint4(kNegInf2, kNegInf2, kNegInf2, kNegInf2); }
 
-// ---- rows of up to 512 words: a group of TPR threads per row, the row in registers ----
+// ---- rows of up to 512 words: a group of TPR threads of a warp per row, the row in registers ----
 constexpr int kGroupThreads = 256;
 template <int TPR, int C>
 __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(const LossArgs a) {
-  constexpr int G = kGroupThreads / TPR, W = TPR / 32;
-  __shared__ Sum2 s_part[G][W > 1 ? W : 1];
+  static_assert(TPR <= 32, "a row's sums are joined inside a warp");
+  constexpr int G = kGroupThreads / TPR;
   const int group = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const int64_t i = (int64_t)blockIdx.x * G + group;
   const bool inside = i < a.N;
@@ -263,14 +263,8 @@ __global__ void __launch_bounds__(kGroupThreads) mp_policy_loss_group_kernel(con
       z[c] = live8(__ldcs(reinterpret_cast<const uint4*>(a.z + i * a.ldl + (c * TPR + t) * 8)), nv[c]);
   }
   const float S = a.st ? a.st->h.scale : 1.0f;
-  Sum2 v = join_lanes<(TPR < 32 ? TPR : 32)>(thread_sum<C>(z));
-  if constexpr (W > 1) {
-    if ((threadIdx.x & 31) == 0) s_part[group][t >> 5] = v;
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
-    v = join_lanes<W>(s_part[group][threadIdx.x & (W - 1)]);
-  } else {
-    __syncwarp();                                  // every lane has read its token's logit before dz may take its place
-  }
+  const Sum2 v = join_lanes<TPR>(thread_sum<C>(z));
+  __syncwarp();                                    // every lane has read its token's logit before dz may take its place
   bool bad = false;
   if (live) {
     const RowGrad g = finish_row(a, i, v, tok, S, t == 0);

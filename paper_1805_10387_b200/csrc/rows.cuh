@@ -18,11 +18,6 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  return v;
-}
 
 // Sum over a block of WARPS full warps, the same value in every thread.  `sm` holds WARPS floats;
 // the warps' sums are added in the order of the warps, so the result does not depend on timing.
@@ -35,17 +30,6 @@ __device__ __forceinline__ float block_sum(float v, float* sm) {
 #pragma unroll
   for (int w = 0; w < WARPS; ++w) t += sm[w];
   __syncthreads();                       // sm may be written again
-  return t;
-}
-template <int WARPS>
-__device__ __forceinline__ float block_max(float v, float* sm) {
-  v = warp_max(v);
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float t = sm[0];
-#pragma unroll
-  for (int w = 1; w < WARPS; ++w) t = fmaxf(t, sm[w]);
-  __syncthreads();
   return t;
 }
 
