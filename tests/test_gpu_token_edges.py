@@ -109,3 +109,31 @@ def test_what_follows_gains_and_gates_does_not_matter(mp, M, D, wide, kind):
             assert torch.isnan(b[D:]).all() if fill != fill else not b[D:].any()
         results.append([t.clone() for t in (xo, n, dx, dy, stats, *(o[:D] for o in outs))])
     assert all(torch.equal(a, b) and torch.isfinite(a).all() for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_step_of_masked_tokens_alone_decays_the_matrices(mp, bits):
+    """No gradient and first moments of zero: the matrices shrink by 1 - lr weight_decay, gains and gates keep their bits."""
+    from paper_1805_10387_b200.token_model import TokenModel
+    n, V, lr, decay = 64, 50, 1e-2, 0.25
+    model = TokenModel(V, 64, 64, 1, n, init_scale=1024.0, state_bits=bits, lr=lr, weight_decay=decay)
+    ids = torch.arange(n, device="cuda") % V
+    one, lp = torch.ones(n, device="cuda"), torch.empty(n, device="cuda")
+    model.log_probs(ids, ids, lp)
+    for _ in range(2):
+        model.step(ids, ids, lp, one, one / n)
+    for t in model.flat["m"] + model.flat["ms"]:
+        t.view(torch.uint8).zero_()
+    before = {k: v.clone() for k, v in model.w32.items()}
+    model.step(ids, ids, lp, one, 0 * one)
+    h = model.state.read()
+    assert h.t == 3 and h.skipped == 0 and model.loss.item() == 0
+    for k, w in model.w32.items():
+        assert not model.dw[k].any(), k
+        if w.dim() == 1:
+            assert torch.equal(w, before[k]), k
+        else:                                             # the factor, its product and the difference are rounded
+            want = before[k].double() * (1 - lr * decay)
+            assert ((w.double() - want).abs() <= U * want.abs() + 2 * U * lr * decay * before[k].double().abs() + 1e-45).all(), k
+            assert not torch.equal(w, before[k])
+    model.close()
