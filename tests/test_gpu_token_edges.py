@@ -137,3 +137,20 @@ def test_a_step_of_masked_tokens_alone_decays_the_matrices(mp, bits):
             assert ((w.double() - want).abs() <= U * want.abs() + 2 * U * lr * decay * before[k].double().abs() + 1e-45).all(), k
             assert not torch.equal(w, before[k])
     model.close()
+
+
+@pytest.mark.parametrize("n,V", [(700, 2 ** 21 - 1), (700, 2 ** 21), (1024, 20_000_000), (5, 2 ** 24 + 1), (3000, 2 ** 24)])
+def test_embedding_gradient_of_few_tokens_in_a_huge_table(mp, n, V):
+    """Id and position of a token fit one word up to 2^21 rows; from there on, and past 2^24, the sort takes three and four passes."""
+    D = 8
+    g = torch.Generator(device="cuda").manual_seed(n)
+    ids = torch.randint(0, V, (n,), generator=g, device="cuda")
+    ids[:2], ids[n // 2:n // 2 + 2], ids[-1] = V - 1, 0, V - 1
+    dY = torch.randint(-3, 4, (n, D), generator=g, device="cuda").half()
+    want = torch.zeros(V, D, dtype=torch.float16, device="cuda")
+    some, where = torch.unique(ids, return_inverse=True)
+    want[some] = torch.zeros(len(some), D, dtype=torch.float64, device="cuda").index_add_(0, where, dY.double()).half()
+    dW = torch.full((V, D), 7.0, dtype=torch.float16, device="cuda")
+    ws = torch.empty(mp.mp_embedding_bwd_workspace_bytes(n, V, D), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    mp.mp_embedding_bwd(ids, dY, dW, workspace=ws)
+    assert torch.equal(dW, want)
