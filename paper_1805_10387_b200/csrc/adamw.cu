@@ -3,12 +3,13 @@
 // As in the Adam update beside it every operation is one individually rounded FP32 operation, so the
 // result does not depend on what the compiler would contract.  With 8-bit states, where the kernel moves
 // 16 B a parameter and instructions weigh as much as memory, that holds for the moments alone: an E4M3 code
-// may turn on their last bit.  The quotient of the step is taken from the hardware's approximation (off by
-// about 2^-22 of a step, far below the last bit of the weight).
+// may turn on their last bit.  The quotient of the step is taken from the hardware's approximation: off by about 2^-22
+// of the step, so by a few units in the last place of the weight where the step is most of it (a weight at zero), and
+// by less than half a unit where the step is a quarter of the weight or less.
 //
 // 28 B a parameter with 32-bit states, 16 B and two scales for each 256 parameters with 8-bit ones: HBM bounds both.
-// Measured on a B200, 1e8 parameters: 32 bits 457 - 463 us (6.1 TB/s), 8 bits 329 us in one tensor or 500 (4.9 TB/s;
-// leaving out the root, the quotient and the codes changes that by 2 %).  What was tried: asynchronous copies into
+// Measured on B200s, 1e8 parameters: 32 bits 457 - 468 us (6.0 - 6.1 TB/s), 8 bits 324 - 350 us in one tensor or 500 (4.6 -
+// 5.0 TB/s; leaving out the root, the quotient and the codes changes that by 2 %).  What was tried: asynchronous copies into
 // shared memory two or three blocks ahead (32 bits 530, 8 bits 420 us), four blocks of threads an SM instead of
 // three (8 bits 409), two (401).
 

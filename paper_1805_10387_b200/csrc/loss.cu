@@ -2,8 +2,10 @@
 //
 // The gradient needs the row's sum, so a row is read, held on the chip, and its gradient written: N V FP16 in, N V
 // FP16 out, whatever lies between.  Two exponentials a word (16 results a clock and SM) and some 14 instructions stay
-// below that: HBM bounds it.  Measured on a B200: 8192 x 32768, a tenth of the rows masked, 190 us (5.4 TB/s; a copy
-// runs at 6.5); 1021 x 131071 99 us (4.6 TB/s).  Three passes over each row took 678 and 416 us.
+// below that: HBM bounds it from some 5000 words on.  Measured on B200s: 8192 x 32768, a tenth of the rows masked, 190 - 201 us
+// (5.1 - 5.4 TB/s; a copy runs at 6.5); 1021 x 131071 98 - 101 us (4.5 - 4.6 TB/s).  Three passes over each row took 678 and
+// 416 us.  Shorter rows are far from it: 40000 x 600 76 us where HBM would need 14, 20000 x 2000 56 (23), 20000 x 5000 86 (58).
+// A block works on one row there, with two barriers and two joins a row, and nothing covers that.
 
 #include <math.h>
 

@@ -12,9 +12,10 @@ namespace {
 // that everything is read once and written once.  What depends on the column alone (the gains, the
 // gate vector) stays in the thread's registers over all rows.
 // An element costs 8 B of HBM traffic forward and 12 B backward (FP16, shared gate), and some 20 and 50
-// instructions.  Measured on a B200: forward 8192 x 1024 16.4 us (4.1 TB/s), backward 25600 x 1600 112 us (4.4 TB/s):
-// backward the instructions weigh as much as HBM (half of the issue slots; a fifth of the lanes idle at a width of
-// 1600).  One row per block without prefetch took 70 and 2184 us, rows in registers of groups that come and
+// instructions.  Measured on B200s: forward 8192 x 1024 16.4 - 16.6 us (4.1 TB/s), 32768 x 1024 51 us (5.3 TB/s), backward
+// 25600 x 1600 112 - 113 us (4.4 TB/s).  Backward fills neither HBM (two thirds) nor the issue slots (56 %): with 128 registers
+// a thread an SM holds 16 warps, too few to cover the latency of the row's sums; a fifth of the lanes idle at a width of
+// 1600.  Widths just above a power of two leave half idle (1032: 24 us forward, 1024: 16.5).  One row per block without prefetch took 70 and 2184 us, rows in registers of groups that come and
 // go 22.6 us forward.  Tried for the backward pass and slower: 1024 threads with one vector each (150 us, spilled
 // registers), 384 threads (125 us), the rows' addresses recomputed instead of kept (122 us).
 constexpr int kRowThreads = 512, kC = 2;
@@ -511,7 +512,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_kernel(const
 
 // Rows of more than 8192 elements: the sums over the rows no longer fit the registers of a block
 // and take its shared memory instead; every row is read three times, the second and third time
-// from L2.
+// from L2.  2000 x 16384 takes 319 us (floor 60); the forward pass, a row in registers with nothing fetched ahead, 87 (40).
 constexpr int kWide = 8192;
 template <class XT>
 __global__ void __launch_bounds__(kRowThreads, 1) mp_block_norm_bwd_wide_kernel(const BwdArgs a) {
