@@ -397,6 +397,28 @@ int mp_adamw_plan_destroy(mp_adamw_plan* plan); /* NULL is accepted */
 int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config* opt, int check_mode,
                     void* stream);
 
+/* Attention over packed sequences, for each of `heads` heads of D elements (a multiple of 8, at most
+ * MP_ATTENTION_MAX_D):
+ *   s_ij = scale q_i . k_j,   p_ij = exp(s_ij - lse_i),   lse_i = log sum_j exp(s_ij),   o_i = sum_j p_ij v_j
+ * over the keys j of the query's own sequence that it sees: all of them; with causal 1 those with
+ * j <= i; with a window (causal only; 0: none) those of them with i - j < window.  Head h of a row
+ * is its elements h D .. (h + 1) D - 1; query head h reads key head h kv_heads / heads (kv_heads
+ * divides heads).  q16, o16 [T, heads D], k16, v16 [T, kv_heads D] with pitches of their own, so they may be
+ * columns of one product.  lse [heads, T] FP32.  offsets: n_seq + 1 integers of id_bytes (4 or 8)
+ * bytes in device memory, ascending within 0 .. T: sequence b is rows offsets[b] .. offsets[b + 1] - 1
+ * (none when they are equal); rows of no sequence are not read, and their outputs stay as they were.
+ * Offsets out of order or range give status MP_ERR_INVALID_ARG in the state, and which sequences are worked
+ * on is then not specified (nothing outside the matrices is touched).  Scores, sums and outputs
+ * are FP32 until one rounding; the weights p enter their product in FP16.  Values of other sequences never matter;
+ * inf or NaN in a key or value may reach all queries of its own sequence, those that do not see it
+ * too.  o16 may not be an input.  T = 0 or n_seq = 0 is legal.  scale > 0. */
+#define MP_ATTENTION_MAX_D 128
+#define MP_ATTENTION_MAX_ROWS (1 << 30)
+int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk, const void* v16, int64_t ldv,
+                     void* o16, int64_t ldo, float* lse, const void* offsets, int id_bytes, int64_t n_seq,
+                     int64_t T, int64_t heads, int64_t kv_heads, int64_t D, float scale, int causal,
+                     int64_t window, mp_state* state, void* stream);
+
 /* ---- auxiliaries --------------------------------------------------------------------- */
 
 enum { MP_OP_FWD = 0, MP_OP_DGRAD = 1, MP_OP_WGRAD = 2 };

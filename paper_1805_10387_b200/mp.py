@@ -121,6 +121,8 @@ SIGNATURES = {
                                     C.POINTER(_p)]),
     "mp_adamw_plan_destroy": (_i32, [_p]),
     "mp_adamw_update": (_i32, [_p, _p, C.POINTER(AdamWConfig), _i32, _p]),
+    "mp_attention_fwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p, _i32, _i64, _i64, _i64, _i64, _i64, _f32,
+                                _i32, _i64, _p, _p]),
     "mp_last_error": (C.c_char_p, []),
     "mp_kernel_launch_count": (_i64, []),
 }
@@ -458,6 +460,15 @@ def _stats(t, M):
     return _dev(t, torch.float32)
 
 
+def _f32_rows(t, shape):
+    """Pointer of a contiguous FP32 matrix of the given shape (None stays None)."""
+    if t is None:
+        return None
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {shape} matrix, got {tuple(t.shape)}")
+    return _dev(t, torch.float32)
+
+
 def _same(a, b, what):
     if a.dtype is not b.dtype:
         raise TypeError(f"{what} must have one type, got {a.dtype} and {b.dtype}")
@@ -535,6 +546,26 @@ def mp_token_logp(logits16, targets, logp, weight=None, state=None):
     t, nb = _ids(targets, N)
     _check(lib().mp_token_logp(z, ldl, t, nb, _vec(weight, N, torch.float32), N, V, _vec(logp, N, torch.float32),
                                _handle(state), _stream()))
+
+
+def _attention_sizes(q16, k16, v16, heads, kv_heads):
+    """Rows and head size of an attention call."""
+    T, width = q16.shape
+    if heads <= 0 or kv_heads <= 0 or width % heads:
+        raise ValueError(f"{width} columns are not {heads} heads")
+    return T, width // heads
+
+
+def mp_attention_fwd(q16, k16, v16, o16, lse, offsets, heads, kv_heads, scale=None, causal=True, window=0, state=None):
+    """o16 = softmax(scale q k^T) v for each head over packed sequences (rows offsets[b] .. offsets[b + 1] - 1), lse
+    [heads, T] = the rows' log-sums.  q16, o16 [T, heads D], k16, v16 [T, kv_heads D]; scale None: 1 / sqrt(D)."""
+    T, D = _attention_sizes(q16, k16, v16, heads, kv_heads)
+    (q, ldq), (o, ldo) = _rows(q16, (T, heads * D), _F16), _rows(o16, (T, heads * D), _F16)
+    (k, ldk), (v, ldv) = _rows(k16, (T, kv_heads * D), _F16), _rows(v16, (T, kv_heads * D), _F16)
+    p, nb = _ids(offsets)
+    _check(lib().mp_attention_fwd(q, ldq, k, ldk, v, ldv, o, ldo, _f32_rows(lse, (heads, T)), p, nb, offsets.shape[0] - 1,
+                                  T, heads, kv_heads, D, D ** -0.5 if scale is None else scale, int(causal), window,
+                                  _handle(state), _stream()))
 
 
 def mp_adamw_update(plan, state, opt: AdamWConfig, check_mode: int = 0):
