@@ -419,6 +419,23 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
                      int64_t T, int64_t heads, int64_t kv_heads, int64_t D, float scale, int causal,
                      int64_t window, mp_state* state, void* stream);
 
+/* Backward of the call above, from its inputs, o16 and lse; do16 [T, heads D]: gradient at o.  With
+ * delta_i = do_i . o_i and ds_ij = p_ij (do_i . v_j - delta_i):
+ *   dv_j = sum_i p_ij do_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i
+ * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16,
+ * p times 2^12 and ds times a power of two that fits the largest rows of do and v, so neither the loss scale nor
+ * long rows cost bits.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
+ * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs.  inf or NaN in a
+ * row of do16 may reach all gradients of its sequence.  workspace: at least mp_attention_bwd_workspace_bytes(..)
+ * bytes of device scratch, 16-byte aligned. */
+int mp_attention_bwd(const void* do16, int64_t lddo, const void* q16, int64_t ldq, const void* k16, int64_t ldk,
+                     const void* v16, int64_t ldv, const void* o16, int64_t ldo, const float* lse, void* dq16,
+                     int64_t lddq, void* dk16, int64_t lddk, void* dv16, int64_t lddv, const void* offsets,
+                     int id_bytes, int64_t n_seq, int64_t T, int64_t heads, int64_t kv_heads, int64_t D, float scale,
+                     int causal, int64_t window, mp_state* state, void* workspace, size_t workspace_bytes,
+                     void* stream);
+size_t mp_attention_bwd_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t D);
+
 /* ---- auxiliaries --------------------------------------------------------------------- */
 
 enum { MP_OP_FWD = 0, MP_OP_DGRAD = 1, MP_OP_WGRAD = 2 };

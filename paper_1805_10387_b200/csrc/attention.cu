@@ -329,7 +329,7 @@ int check_call(const char* name, Shape& s, const void* offsets, int id_bytes, in
   if (!(scale > 0.0f) || !isfinite(scale) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: the scale must be positive and finite, causal 0 or 1, and a window "
                          "needs causal", name);
-  if (D > MP_ATTENTION_MAX_D || heads > 65535 || T > MP_ATTENTION_MAX_ROWS || n_seq > MP_ATTENTION_MAX_ROWS ||
+  if (D > MP_ATTENTION_MAX_D || heads > 32767 || T > MP_ATTENTION_MAX_ROWS || n_seq > MP_ATTENTION_MAX_ROWS ||
       (T / kTile + n_seq) * heads > 0x3FFFFFFF)
     return mp::set_error(MP_ERR_TOO_LARGE, "%s: a head of more than %d elements, more than %d rows, or too many tiles",
                          name, MP_ATTENTION_MAX_D, MP_ATTENTION_MAX_ROWS);
@@ -346,7 +346,7 @@ int check_call(const char* name, Shape& s, const void* offsets, int id_bytes, in
   s.scale = scale;
   s.scale_log2 = scale * kLog2e;
   s.causal = causal;
-  s.window = window;
+  s.window = window < T ? window : 0;              // one that no query reaches past is none
   s.st = state ? state->dev : nullptr;
   s.status = nullptr;
   return MP_OK;

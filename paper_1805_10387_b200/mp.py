@@ -123,6 +123,9 @@ SIGNATURES = {
     "mp_adamw_update": (_i32, [_p, _p, C.POINTER(AdamWConfig), _i32, _p]),
     "mp_attention_fwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p, _i32, _i64, _i64, _i64, _i64, _i64, _f32,
                                 _i32, _i64, _p, _p]),
+    "mp_attention_bwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p, _i64, _p, _i64, _p, _i64, _p, _i32,
+                                _i64, _i64, _i64, _i64, _i64, _f32, _i32, _i64, _p, _p, _sz, _p]),
+    "mp_attention_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "mp_last_error": (C.c_char_p, []),
     "mp_kernel_launch_count": (_i64, []),
 }
@@ -566,6 +569,25 @@ def mp_attention_fwd(q16, k16, v16, o16, lse, offsets, heads, kv_heads, scale=No
     _check(lib().mp_attention_fwd(q, ldq, k, ldk, v, ldv, o, ldo, _f32_rows(lse, (heads, T)), p, nb, offsets.shape[0] - 1,
                                   T, heads, kv_heads, D, D ** -0.5 if scale is None else scale, int(causal), window,
                                   _handle(state), _stream()))
+
+
+def mp_attention_bwd_workspace_bytes(T: int, heads: int, kv_heads: int, D: int) -> int:
+    return int(lib().mp_attention_bwd_workspace_bytes(T, heads, kv_heads, D))
+
+
+def mp_attention_bwd(do16, q16, k16, v16, o16, lse, dq16, dk16, dv16, offsets, heads, kv_heads, scale=None, causal=True,
+                     window=0, state=None, workspace=None):
+    """Backward of mp_attention_fwd from its inputs, o16 and lse: do16 -> dq16, dk16, dv16."""
+    T, D = _attention_sizes(q16, k16, v16, heads, kv_heads)
+    wide, narrow = (T, heads * D), (T, kv_heads * D)
+    (do, lddo), (q, ldq), (o, ldo), (dq, lddq) = (_rows(t, wide, _F16) for t in (do16, q16, o16, dq16))
+    (k, ldk), (v, ldv), (dk, lddk), (dv, lddv) = (_rows(t, narrow, _F16) for t in (k16, v16, dk16, dv16))
+    p, nb = _ids(offsets)
+    ws, size = _ws(workspace)
+    _check(lib().mp_attention_bwd(do, lddo, q, ldq, k, ldk, v, ldv, o, ldo, _f32_rows(lse, (heads, T)), dq, lddq, dk, lddk,
+                                  dv, lddv, p, nb, offsets.shape[0] - 1, T, heads, kv_heads, D,
+                                  D ** -0.5 if scale is None else scale, int(causal), window, _handle(state), ws, size,
+                                  _stream()))
 
 
 def mp_adamw_update(plan, state, opt: AdamWConfig, check_mode: int = 0):
