@@ -397,6 +397,33 @@ int mp_adamw_plan_destroy(mp_adamw_plan* plan); /* NULL is accepted */
 int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config* opt, int check_mode,
                     void* stream);
 
+/* Norms of queries and keys for each head, and the position rotation, in one pass.  A row of x16 holds q_heads
+ * query heads and then k_heads key heads of D elements each (D a multiple of 8, at most MP_HEAD_MAX_D; what
+ * follows in the row, values for instance, is left alone).  Each head u becomes
+ *   n = u / sqrt(mean(u^2) + eps) * g,   y = R n
+ * with g = gq16 for query heads, gk16 for key heads (D elements each; both NULL: 1).  R turns the first rot
+ * elements (a multiple of 16, 0: none) pair by pair: for pair i with angle t = positions[row] freqs[i]
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t)
+ * pairs are elements (i, i + rot / 2) with pairs 0, (2 i, 2 i + 1) with pairs 1.  positions: T integers of
+ * pos_bytes (4 or 8) bytes, of any size; freqs: rot / 2 FP64 values in radians, finite.  The angle is formed in 64-bit fixed
+ * point turns, so far positions keep their precision.  y16 may be x16 itself (same pitch).  T = 0 is legal. */
+#define MP_HEAD_MAX_D 256
+int mp_head_norm_rope_fwd(const void* x16, int64_t ldx, const void* gq16, const void* gk16, const void* positions,
+                          int pos_bytes, const double* freqs, int64_t rot, int pairs, float eps, void* y16,
+                          int64_t ldy, int64_t T, int64_t q_heads, int64_t k_heads, int64_t D, void* stream);
+
+/* Backward of the call above, from its input x16: with u = R^-1 dy and xhat the normed head before the gain,
+ *   dx = (u g - xhat mean(u g xhat)) / sqrt(mean(x^2) + eps),   dg = sum over rows and heads of u xhat
+ * dx16 may be dy16 or x16 itself (same pitch).  dgq16, dgk16: D elements each, NULL exactly when the gains are;
+ * FP32 sums in a fixed order, rounded once.  workspace: at least mp_head_norm_rope_bwd_workspace_bytes(..) bytes,
+ * 16-byte aligned (none needed without gains). */
+int mp_head_norm_rope_bwd(const void* dy16, int64_t lddy, const void* x16, int64_t ldx, const void* gq16,
+                          const void* gk16, const void* positions, int pos_bytes, const double* freqs, int64_t rot,
+                          int pairs, float eps, void* dx16, int64_t lddx, void* dgq16, void* dgk16, int64_t T,
+                          int64_t q_heads, int64_t k_heads, int64_t D, mp_state* state, void* workspace,
+                          size_t workspace_bytes, void* stream);
+size_t mp_head_norm_rope_bwd_workspace_bytes(int64_t T, int64_t q_heads, int64_t k_heads, int64_t D);
+
 /* Attention over packed sequences, for each of `heads` heads of D elements (a multiple of 8, at most
  * MP_ATTENTION_MAX_D):
  *   s_ij = scale q_i . k_j,   p_ij = exp(s_ij - lse_i),   lse_i = log sum_j exp(s_ij),   o_i = sum_j p_ij v_j

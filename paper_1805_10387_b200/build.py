@@ -8,7 +8,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libmp_b200.so")
-SOURCES = ["update.cu", "gemm.cu", "lstm.cu", "embedding.cu", "norm.cu", "loss.cu", "adamw.cu", "attention.cu", "attention_bwd.cu"]
+SOURCES = ["update.cu", "gemm.cu", "lstm.cu", "embedding.cu", "norm.cu", "loss.cu", "adamw.cu", "headnorm.cu", "attention.cu",
+           "attention_bwd.cu"]
 HEADERS = ["common.h", "ptx.cuh", "rows.cuh", "attention.cuh", os.path.join(_ROOT, "include", "mp.h")]
 
 

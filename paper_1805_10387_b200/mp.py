@@ -121,6 +121,10 @@ SIGNATURES = {
                                     C.POINTER(_p)]),
     "mp_adamw_plan_destroy": (_i32, [_p]),
     "mp_adamw_update": (_i32, [_p, _p, C.POINTER(AdamWConfig), _i32, _p]),
+    "mp_head_norm_rope_fwd": (_i32, [_p, _i64, _p, _p, _p, _i32, _p, _i64, _i32, _f32, _p, _i64, _i64, _i64, _i64, _i64, _p]),
+    "mp_head_norm_rope_bwd": (_i32, [_p, _i64, _p, _i64, _p, _p, _p, _i32, _p, _i64, _i32, _f32, _p, _i64, _p, _p, _i64, _i64,
+                                     _i64, _i64, _p, _p, _sz, _p]),
+    "mp_head_norm_rope_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64]),
     "mp_attention_fwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p, _i32, _i64, _i64, _i64, _i64, _i64, _f32,
                                 _i32, _i64, _p, _p]),
     "mp_attention_bwd": (_i32, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _p, _i64, _p, _i64, _p, _i64, _p, _i32,
@@ -549,6 +553,49 @@ def mp_token_logp(logits16, targets, logp, weight=None, state=None):
     t, nb = _ids(targets, N)
     _check(lib().mp_token_logp(z, ldl, t, nb, _vec(weight, N, torch.float32), N, V, _vec(logp, N, torch.float32),
                                _handle(state), _stream()))
+
+
+def _head_size(x16, q_heads, k_heads):
+    T, width = x16.shape
+    if q_heads < 0 or k_heads < 0 or q_heads + k_heads <= 0 or width % (q_heads + k_heads):
+        raise ValueError(f"{width} columns are not {q_heads} + {k_heads} heads")
+    return T, width // (q_heads + k_heads)
+
+
+def _rotation(positions, freqs, T):
+    """(positions, bytes each, frequencies, rotated elements); no frequencies: no rotation."""
+    if freqs is None:
+        return None, 4, None, 0
+    p, nb = _ids(positions, T)
+    return p, nb, _vec(freqs, freqs.shape[0], torch.float64), 2 * freqs.shape[0]
+
+
+def mp_head_norm_rope_fwd(x16, gq16, gk16, positions, freqs, y16, q_heads, k_heads, eps=1e-6, pairs=False):
+    """y16 = each head of x16 [T, (q_heads + k_heads) D] divided by its root mean square, times gq16 (queries) or gk16
+    (keys; both None: 1), its first 2 len(freqs) elements turned by positions * freqs (FP64 radians; None: not
+    turned).  pairs: neighbours turn together, else the halves of the turned part."""
+    T, D = _head_size(x16, q_heads, k_heads)
+    (x, ldx), (y, ldy) = _rows(x16, x16.shape, _F16), _rows(y16, x16.shape, _F16)
+    p, nb, f, rot = _rotation(positions, freqs, T)
+    _check(lib().mp_head_norm_rope_fwd(x, ldx, _vec(gq16, D, torch.float16), _vec(gk16, D, torch.float16), p, nb, f, rot,
+                                       int(pairs), eps, y, ldy, T, q_heads, k_heads, D, _stream()))
+
+
+def mp_head_norm_rope_bwd_workspace_bytes(T: int, q_heads: int, k_heads: int, D: int) -> int:
+    return int(lib().mp_head_norm_rope_bwd_workspace_bytes(T, q_heads, k_heads, D))
+
+
+def mp_head_norm_rope_bwd(dy16, x16, gq16, gk16, positions, freqs, dx16, dgq16, dgk16, q_heads, k_heads, eps=1e-6, pairs=False,
+                          state=None, workspace=None):
+    """Backward of mp_head_norm_rope_fwd from its input: dy16 -> dx16 and the gains' gradients."""
+    T, D = _head_size(x16, q_heads, k_heads)
+    (dy, lddy), (x, ldx), (dx, lddx) = (_rows(t, x16.shape, _F16) for t in (dy16, x16, dx16))
+    p, nb, f, rot = _rotation(positions, freqs, T)
+    ws, size = _ws(workspace)
+    h = torch.float16
+    _check(lib().mp_head_norm_rope_bwd(dy, lddy, x, ldx, _vec(gq16, D, h), _vec(gk16, D, h), p, nb, f, rot, int(pairs), eps,
+                                       dx, lddx, _vec(dgq16, D, h), _vec(dgk16, D, h), T, q_heads, k_heads, D, _handle(state),
+                                       ws, size, _stream()))
 
 
 def _attention_sizes(q16, k16, v16, heads, kv_heads):
