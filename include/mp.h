@@ -372,6 +372,43 @@ int mp_policy_loss(const void* logits16, int64_t ldl, const void* targets, int i
 int mp_token_logp(const void* logits16, int64_t ldl, const void* targets, int id_bytes, const float* weight,
                   int64_t N, int64_t V, float* logp, mp_state* state, void* stream);
 
+/* Token scores: for row i with logits z and x = z / temperature, lp_j = x_j - log sum_l exp(x_l),
+ *   logp[i] = lp at targets[i],   entropy[i] = -sum_j exp(lp_j) lp_j,
+ *   top_ids[i, 0 .. k-1], top_logp[i, ..] = the k largest logits' ids and lp, largest first; of equal logits the
+ *   lower id comes first.
+ * targets: N integers of id_bytes (4 or 8) bytes, or NULL (then logp must be NULL).  logp, entropy and weight may be
+ * NULL.  top_ids (int32) and top_logp [N, k] dense, 1 <= k <= min(V, MP_TOP_MAX_K).  A row of weight 0 is not
+ * read: its ids become -1, its values 0.  A target out of range gives NaN and a status, as in mp_policy_loss.
+ * A row with +inf or NaN among its logits has NaN for its values; its ids are then not specified (-1 or a
+ * token).  temperature: MP_MIN_TEMPERATURE .. MP_MAX_TEMPERATURE. */
+#define MP_TOP_MAX_K 128
+#define MP_MIN_TEMPERATURE 1e-3f
+#define MP_MAX_TEMPERATURE 1e3f
+int mp_token_top(const void* logits16, int64_t ldl, const void* targets, int id_bytes, const float* weight, int64_t N,
+                 int64_t V, int64_t k, float temperature, float* logp, float* entropy, int32_t* top_ids,
+                 float* top_logp, mp_state* state, void* stream);
+
+/* Distillation from a teacher's top entries, forward and backward in one call.  ids, teacher_logp [N, K] dense: the tokens
+ * that the teacher lists for a row and their log-probabilities a (as mp_token_top gives them, at the same
+ * temperature); an id of -1 is no entry.  With lq the student's log-probabilities at the temperature:
+ *   tail 1:  l = sum_e p_e (a_e - lq_e) + r (log r - log sum_{j not listed} exp(lq_j)),  p = exp(a), r = max(0, 1 - sum_e p_e)
+ *   tail 0:  l = sum_e p_e (log p_e - lq_e),  p = the softmax of a over the row's entries (top logits / temperature do as well)
+ *   token_loss[i] = w l,   loss[0] = sum_i token_loss[i] (fixed order; may be NULL)
+ *   dz_j = rn16( grad_scale * S * w * dl/dz_j )
+ * An entry of probability 0 adds nothing.  Without an unlisted token of finite logit r is 0.  A row of weight 0 is
+ * masked as in mp_policy_loss.  An id that is out of range, or that a row lists twice (and whose logit is
+ * not -inf), gives NaN for the row's outputs and sets state->status.  logits16, dlogits16, S, N = 0 and the limits of V as in
+ * mp_policy_loss; 1 <= K <= min(V, MP_DISTILL_MAX_K). */
+#define MP_DISTILL_MAX_K 128
+typedef struct {
+  float temperature;
+  int32_t tail;
+  float grad_scale;
+} mp_distill_config;
+int mp_distill_loss(const void* logits16, int64_t ldl, const void* ids, int id_bytes, const float* teacher_logp,
+                    int64_t K, const float* weight, int64_t N, int64_t V, const mp_distill_config* cfg,
+                    void* dlogits16, int64_t lddl, float* token_loss, float* loss, mp_state* state, void* stream);
+
 /* AdamW (weight decay apart from the gradient) over the tensors of a plan, on the FP32 master, with
  * the flag, S and t of `state` as in mp_master_update.  Per element, with g = float(g16) / S,
  * c1 = 1 - beta1^t, c2 = 1 - beta2^t:

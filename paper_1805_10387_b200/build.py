@@ -8,9 +8,9 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libmp_b200.so")
-SOURCES = ["update.cu", "gemm.cu", "lstm.cu", "embedding.cu", "norm.cu", "loss.cu", "adamw.cu", "headnorm.cu", "attention.cu",
-           "attention_bwd.cu"]
-HEADERS = ["common.h", "ptx.cuh", "rows.cuh", "attention.cuh", os.path.join(_ROOT, "include", "mp.h")]
+SOURCES = ["update.cu", "gemm.cu", "lstm.cu", "embedding.cu", "norm.cu", "loss.cu", "adamw.cu", "top.cu", "distill.cu", "headnorm.cu",
+           "attention.cu", "attention_bwd.cu"]
+HEADERS = ["common.h", "ptx.cuh", "rows.cuh", "softmax.cuh", "attention.cuh", os.path.join(_ROOT, "include", "mp.h")]
 
 
 def _stale() -> bool:

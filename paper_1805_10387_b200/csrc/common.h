@@ -34,6 +34,8 @@ int check_device();  // MP_OK if the current device is compute capability 10.x
 // Device address (on the current device) of the status word that the GEMM kernels set when a
 // bounded wait expires; defined beside those kernels.
 int gemm_status_device_ptr(int** out);
+// loss[0] = sum of N token losses in a fixed order; the kernel ahead on the stream may still be writing them.
+int sum_token_loss(const float* token_loss, int64_t N, float* loss, cudaStream_t st);
 
 // What a first call asks of the runtime, remembered for each device (0: not asked yet).  A fixed table without a lock:
 // an allocation may throw, and no exception may leave a C entry point.  Threads that both find 0 both ask.

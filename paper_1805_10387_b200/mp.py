@@ -55,6 +55,10 @@ class PolicyConfig(C.Structure):
     _fields_ = [("clip_lo", C.c_float), ("clip_hi", C.c_float), ("kl_coef", C.c_float), ("grad_scale", C.c_float)]
 
 
+class DistillConfig(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("tail", C.c_int32), ("grad_scale", C.c_float)]
+
+
 class AdamWConfig(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("weight_decay", C.c_double)]
@@ -116,6 +120,9 @@ SIGNATURES = {
     "mp_policy_loss": (_i32, [_p, _i64, _p, _i32, _p, _p, _p, _p, _i64, _i64, C.POINTER(PolicyConfig), _p, _i64, _p, _p,
                               _p, _p, _p]),
     "mp_token_logp": (_i32, [_p, _i64, _p, _i32, _p, _i64, _i64, _p, _p, _p]),
+    "mp_token_top": (_i32, [_p, _i64, _p, _i32, _p, _i64, _i64, _i64, _f32, _p, _p, _p, _p, _p, _p]),
+    "mp_distill_loss": (_i32, [_p, _i64, _p, _i32, _p, _i64, _p, _i64, _i64, C.POINTER(DistillConfig), _p, _i64, _p, _p, _p,
+                               _p]),
     "mp_adamw_plan_create": (_i32, [_i32, C.POINTER(_p), C.POINTER(_p), C.POINTER(_p), C.POINTER(_p), C.POINTER(_p),
                                     C.POINTER(_i64), C.POINTER(_f32), _i32, C.POINTER(_p), C.POINTER(_p),
                                     C.POINTER(_p)]),
@@ -553,6 +560,38 @@ def mp_token_logp(logits16, targets, logp, weight=None, state=None):
     t, nb = _ids(targets, N)
     _check(lib().mp_token_logp(z, ldl, t, nb, _vec(weight, N, torch.float32), N, V, _vec(logp, N, torch.float32),
                                _handle(state), _stream()))
+
+
+def mp_token_top(logits16, top_ids, top_logp, targets=None, logp=None, entropy=None, weight=None, temperature=1.0, state=None):
+    """top_ids (int32), top_logp [N, k]: the k likeliest tokens of each row and their log-probabilities at the temperature;
+    logp, entropy [N] (FP32, may be None): of targets[i], and of the row.  Rows of weight 0: ids -1, values 0."""
+    N, V = logits16.shape
+    z, ldl = _rows(logits16, (N, V), _F16)
+    if top_ids.dim() != 2 or top_ids.shape[0] != N or not top_ids.is_contiguous():
+        raise ValueError(f"expected a contiguous [{N}, k] matrix of ids, got {tuple(top_ids.shape)}")
+    k = top_ids.shape[1]
+    t, nb = (None, 4) if targets is None else _ids(targets, N)
+    f = torch.float32
+    _check(lib().mp_token_top(z, ldl, t, nb, _vec(weight, N, f), N, V, k, temperature, _vec(logp, N, f), _vec(entropy, N, f),
+                              _dev(top_ids, torch.int32), _f32_rows(top_logp, (N, k)), _handle(state), _stream()))
+
+
+def mp_distill_loss(logits16, ids, teacher_logp, weight, token_loss, loss=None, dlogits16=None, temperature=1.0, tail=True,
+                    grad_scale=1.0, state=None):
+    """KL divergence from a teacher's top entries (ids [N, K] int32 or int64, -1: none; teacher_logp [N, K]): token_loss [N],
+    loss [1] (FP32), and the gradient at the logits times grad_scale and the loss scale of `state` (dlogits16 None: forward
+    only).  tail: what the teacher does not list is one more outcome, else its entries are all there is."""
+    N, V = logits16.shape
+    z, ldl = _rows(logits16, (N, V), _F16)
+    nb = _ID_BYTES.get(ids.dtype)
+    if nb is None or not ids.is_cuda or ids.dim() != 2 or ids.shape[0] != N or not ids.is_contiguous():
+        raise TypeError(f"expected a contiguous CUDA [{N}, K] matrix of int32 or int64, got {ids.device} {ids.dtype} {tuple(ids.shape)}")
+    K = ids.shape[1]
+    dz, lddl = (None, 0) if dlogits16 is None else _rows(dlogits16, (N, V), _F16)
+    cfg = DistillConfig(temperature, int(tail), grad_scale)
+    f = torch.float32
+    _check(lib().mp_distill_loss(z, ldl, ids.data_ptr(), nb, _f32_rows(teacher_logp, (N, K)), K, _vec(weight, N, f), N, V,
+                                 C.byref(cfg), dz, lddl, _vec(token_loss, N, f), _vec(loss, 1, f), _handle(state), _stream()))
 
 
 def _head_size(x16, q_heads, k_heads):
