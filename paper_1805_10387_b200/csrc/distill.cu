@@ -113,17 +113,22 @@ __device__ __forceinline__ Grad finish(const DistillArgs& g, int64_t i, Entries&
     sum_p = any ? 1.0f : 0.0f;
     if (most != most || most == -INFINITY) sum_p = any ? NAN : 0.0f;
   }
-  // the whole row's sum 2^k (s), and the tail
+  // the whole row's sum 2^k (s), and the tail.  r = 1 - P and the student's 1 - Q lose bits where P and Q are small, and
+  // there log1p keeps them; where Q is large the tail's own sum does
   const int k = max(rest.k, top == -INFINITY ? kNothing : top == INFINITY ? 0 : (int)kt);
-  const float rest_up = ex2((float)(rest.k - k));
-  const float s = rest.s * rest_up + st * ex2(kt - (float)k);
+  const float rest_up = ex2((float)(rest.k - k)), listed_s = st * ex2(kt - (float)k);
+  const float s = rest.s * rest_up + listed_s;
   const float log2s = log2f(s);
-  float pr = 0.0f, mass = sum_p, lr = 0.0f;
+  float mass = sum_p, lr = 0.0f, over = mass * rest_up / s;  // over: of the unlisted words' softmax, what their gradient takes
   if (g.tail && rest.s != 0.0f) {
-    pr = fmaxf(1.0f - sum_p, 0.0f);
-    if (sum_p != sum_p) pr = sum_p;
-    mass = sum_p + pr;
-    if (pr > 0.0f) lr = pr * (logf(pr) - ((float)(rest.k - k) + log2f(rest.s / s)) * kLn2);
+    const float r = 1.0f - sum_p, Q = listed_s / s;
+    if (!(r <= 0.0f)) {                           // a NaN goes on
+      mass = sum_p + r;
+      const float log_r = sum_p < 0.5f ? log1pf(-sum_p) : logf(r);
+      const float log_q = Q < 0.5f ? log1pf(-Q) : ((float)(rest.k - k) + log2f(rest.s / s)) * kLn2;
+      lr = r * (log_r - log_q);
+      over = (Q < 0.5f ? sum_p - Q : rest.s * rest_up / s - r) / rest.s;
+    }
   }
   if (bad) mass = NAN;
   const float G = g.factor * S * w;
@@ -141,9 +146,9 @@ __device__ __forceinline__ Grad finish(const DistillArgs& g, int64_t i, Entries&
     if (bad) rows::record_bad_id(g.st);
     if (writer) g.token_loss[i] = w * loss;
   }
-  const float cold = G * (mass * rest_up / s - (pr > 0.0f ? pr / rest.s : 0.0f));
-  // every |dz_j| is at most |G| (mass + pr): unless that is near FP16's end nobody looks at what is stored
-  return Grad{(float)rest.k, cold, !(fabsf(G) * (mass + pr) < 65000.0f) || !(fabsf(cold) <= 3.0e38f)};
+  const float cold = bad ? NAN : G * over;
+  // every |dz_j| is at most 2 |G| mass: unless that is near FP16's end nobody looks at what is stored
+  return Grad{(float)rest.k, cold, !(2.0f * fabsf(G) * mass < 65000.0f) || !(fabsf(cold) <= 3.0e38f)};
 }
 
 __device__ __forceinline__ uint4 cold8(const uint4& z, const Grad& g, float scale) {
