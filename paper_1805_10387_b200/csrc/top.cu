@@ -15,7 +15,6 @@
 #include "softmax.cuh"
 
 namespace {
-
 using namespace softmax;
 
 struct TopArgs {
@@ -32,6 +31,23 @@ struct TopArgs {
   float* tlogp;
   mp_dev_state* st;
 };
+
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)),
+        "l"(reinterpret_cast<const unsigned long long&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
+  return d;
+}
 
 // s 2^k = sum 2^(z scale), u = sum 2^y y with y = z scale - k.
 struct Sums {
@@ -57,35 +73,27 @@ __device__ __forceinline__ Sums join(Sums v) {
   v.k = k;
   return v;
 }
-// A thread's sums.  k follows the largest word and lags by less than 2^8: the entropy is a difference of logarithms, and
-// a k far off would cost it bits.
-struct Stream {
-  float k = 0.0f, s = 0.0f, u = 0.0f;
-  bool begun = false, infinite = false;
-  __device__ __forceinline__ void add(const uint4& z, float top, float scale) {
-    if (!begun || fmaf(top, scale, -k) > 8.0f) {
-      const float up = top == -INFINITY ? (float)kNothing : rintf(top * scale);
-      if (begun) rebase(s, u, k - up, ex2(k - up));
-      k = up;
-      begun = true;
-      infinite |= top == INFINITY;
-    }
+// A thread's sums, with k near its largest word: the entropy is a difference of logarithms, and a k far off would cost it bits.
+struct Tally {
+  float k, s = 0.0f, u = 0.0f;
+  bool infinite;
+  __device__ __forceinline__ Tally(float top, float scale)
+      : k(top == -INFINITY ? (float)kNothing : rintf(top * scale)), infinite(top == INFINITY) {}
+  __device__ __forceinline__ void add(const uint4& z, float scale) {
     const uint32_t w[4] = {z.x, z.y, z.z, z.w};
-    float ss[2] = {0.0f, 0.0f}, uu[2] = {0.0f, 0.0f};
+    const float2 sc = make_float2(scale, scale), mk = make_float2(-k, -k);
+    float2 ss = make_float2(0.0f, 0.0f), uu = ss;  // of the vector: long sums of small ones lose bits
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-      const float a = fmaf(f.x, scale, -k), b = fmaf(f.y, scale, -k);
-      const float ea = ex2(a), eb = ex2(b);
-      ss[0] += ea;
-      ss[1] += eb;
-      uu[0] = fmaf(ea, fmaxf(a, -200.0f), uu[0]);            // 0 times -inf is no summand
-      uu[1] = fmaf(eb, fmaxf(b, -200.0f), uu[1]);
+      const float2 y = fma2(__half22float2(*reinterpret_cast<const __half2*>(&w[j])), sc, mk);
+      const float2 e = make_float2(ex2(y.x), ex2(y.y));
+      ss = add2(ss, e);
+      uu = fma2(e, make_float2(fmaxf(y.x, -200.0f), fmaxf(y.y, -200.0f)), uu);      // 0 times -inf is no summand
     }
-    s += ss[0] + ss[1];
-    u += uu[0] + uu[1];
+    s += ss.x + ss.y;
+    u += uu.x + uu.y;
   }
-  __device__ __forceinline__ Sums sums() const { return begun ? Sums{infinite ? 0 : (int)k, s, u} : Sums{kNothing, 0.0f, 0.0f}; }
+  __device__ __forceinline__ Sums sums() const { return Sums{infinite ? 0 : (int)k, s, u}; }
 };
 
 // ---- entries: 16 bits that order the values, then 20 that order the ids downwards ----
@@ -102,36 +110,81 @@ __device__ __forceinline__ float top8(const uint4& z) {
   const float2 m = __half22float2(max8(__half2half2(__ushort_as_half(0xFC00)), z));
   return fmaxf(m.x, m.y);
 }
-// Lists the words of a vector (its first at id `at`) that reach the bound.
-__device__ __forceinline__ void list8(const uint4& z, int at, float bound, Entry* list, int cap, int* count) {
+// Lists the first `left` words of a vector (its first at id `at`) that reach the bound.
+__device__ __forceinline__ void list8(const uint4& z, int at, int left, __half2 bound, Entry* list, int cap, int* count) {
   const uint32_t w[4] = {z.x, z.y, z.z, z.w};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint16_t h = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-    if (rows::h2f(h) >= bound) {
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t hit = __hge2_mask(*reinterpret_cast<const __half2*>(&w[j]), bound);
+    if (hit == 0) continue;
+    auto one = [&](int e) {
       const int n = atomicAdd(count, 1);
-      if (n < cap) list[n] = entry(h, at + j);
-    }
+      if (n < cap) list[n] = entry((uint16_t)(w[j] >> (16 * e)), at + 2 * j + e);
+    };
+    if ((hit & 1) && 2 * j < left) one(0);
+    if ((hit >> 16) && 2 * j + 1 < left) one(1);
   }
 }
-// By a whole warp: moves the k largest of `count` entries (all of them, if fewer) to `out`; returns how many.
-__device__ __forceinline__ int pick(const Entry* list, int count, int k, Entry* out) {
+// By a whole warp: moves the k largest of `count` entries (all of them, if fewer) to `out`; returns how many.  R * 32 entries
+// are held in registers, what is beyond is read again in every round.  At most MOST entries.
+template <int MOST>
+__device__ __noinline__ int pick(const Entry* list, int count, int k, Entry* out) {
   const int lane = threadIdx.x & 31;
-  constexpr int R = 8;                            // entries a lane holds in registers
+  constexpr int R = 4;
   Entry mine[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) mine[i] = i * 32 + lane < count ? list[i * 32 + lane] : 0;
   Entry t = 0;
   if (count > k) {
-    for (int bit = 35; bit >= 0; --bit) {
-      const Entry cand = t | (Entry)1 << bit;
-      int n = 0;
+    // The k-th value first, two bits a round (three bounds at once), from the first bit on in which the
+    // values differ; then among those that equal it the k-th id.  Done when a bound leaves just k.
+    uint32_t key[R], most = 0, least = ~0u;
 #pragma unroll
-      for (int i = 0; i < R; ++i) n += mine[i] >= cand;
-      for (int i = R * 32 + lane; i < count; i += 32) n += list[i] >= cand;
-      n = __reduce_add_sync(0xFFFFFFFFu, n);
-      if (n >= k) t = cand;
-      if (n == k) break;
+    for (int i = 0; i < R; ++i) {
+      key[i] = (uint32_t)(mine[i] >> 20);
+      most = max(most, key[i]);
+      least = i * 32 + lane < count ? min(least, key[i]) : least;
+    }
+    for (int i = R * 32 + lane; i < count; i += 32) {
+      const uint32_t x = (uint32_t)(list[i] >> 20);
+      most = max(most, x);
+      least = min(least, x);
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    int bit = (33 - __clz(most ^ least)) & ~1, n = count;    // even, all bits from here up are alike
+    uint32_t v = most >> bit << bit;
+    while (bit > 0 && n != k) {
+      bit -= 2;
+      const uint32_t c1 = v + (1u << bit), c2 = v + (2u << bit), c3 = v + (3u << bit);
+      uint32_t here = 0, high = 0;                // three counts in a word, if 10 bits are enough for the last
+      constexpr bool kOne = MOST <= 1023;
+      auto add = [&](uint32_t x) {
+        here += (x >= c1) + (x >= c2 ? 1u << 11 : 0);
+        if (kOne) here += x >= c3 ? 1u << 22 : 0;
+        else high += x >= c3;
+      };
+#pragma unroll
+      for (int i = 0; i < R; ++i) add(key[i]);
+      for (int i = R * 32 + lane; i < count; i += 32) add((uint32_t)(list[i] >> 20));
+      here = __reduce_add_sync(0xFFFFFFFFu, here);
+      const int n1 = here & 0x7FF, n2 = here >> 11 & 0x7FF, n3 = kOne ? here >> 22 : __reduce_add_sync(0xFFFFFFFFu, high);
+      if (n3 >= k) { v = c3; n = n3; }
+      else if (n2 >= k) { v = c2; n = n2; }
+      else if (n1 >= k) { v = c1; n = n1; }
+    }
+    t = (Entry)v << 20;
+    for (bit = 19; bit >= 0 && n != k; --bit) {
+      const Entry cand = t | (Entry)1 << bit;
+      int here = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) here += mine[i] >= cand;
+      for (int i = R * 32 + lane; i < count; i += 32) here += list[i] >= cand;
+      here = __reduce_add_sync(0xFFFFFFFFu, here);
+      if (here >= k) {
+        t = cand;
+        n = here;
+      }
     }
   }
   int have = 0;
@@ -150,22 +203,25 @@ __device__ __forceinline__ int pick(const Entry* list, int count, int k, Entry* 
   return have;
 }
 
-// By a whole warp: a row's outputs, from its sums and its `have` picked entries.
-__device__ __forceinline__ void put(const TopArgs& a, int64_t i, const Sums& v, const Entry* picked, int have) {
-  const int lane = threadIdx.x & 31;
+// Puts `count` (at most 128) entries in order, largest first, the k first of them.  By `team` threads of which this is number
+// `lane`; the caller sees to the barriers.
+__device__ __forceinline__ void order(const Entry* list, int count, int k, Entry* out, int lane, int team) {
+  for (int e = lane; e < count; e += team) {
+    const Entry mine = list[e];
+    int rank = 0;
+#pragma unroll 8
+    for (int o = 0; o < count; ++o) rank += list[o] > mine;
+    if (rank < k) out[rank] = mine;
+  }
+}
+// A row's outputs, from its sums and its `have` entries in order, by `team` threads of which this is number `lane`.
+__device__ __forceinline__ void put(const TopArgs& a, int64_t i, const Sums& v, const Entry* sorted, int have, int lane, int team) {
   const float log2s = log2f(v.s), k = (float)v.k;
   auto lp = [&](float z) { return (fmaf(z, a.scale, -k) - log2s) * kLn2; };
-  for (int e = lane; e < a.k; e += 32) {
-    if (e >= have) {                              // fewer numbers than k
-      a.ids[i * a.k + e] = -1;
-      a.tlogp[i * a.k + e] = NAN;
-      continue;
-    }
-    const Entry mine = picked[e];
-    int rank = 0;
-    for (int o = 0; o < have; ++o) rank += picked[o] > mine;
-    a.ids[i * a.k + rank] = id_of(mine);
-    a.tlogp[i * a.k + rank] = lp(logit_of(mine));
+  for (int e = lane; e < a.k; e += team) {
+    const bool is = e < have;                     // else the row has fewer numbers than k
+    a.ids[i * a.k + e] = is ? id_of(sorted[e]) : -1;
+    a.tlogp[i * a.k + e] = is ? lp(logit_of(sorted[e])) : NAN;
   }
   if (lane == 0) {
     if (a.entropy != nullptr) {
@@ -217,16 +273,19 @@ __global__ void __launch_bounds__(kWarpThreads) mp_token_top_warp_kernel(const T
     return;
   }
   uint4 z[C];
-  Stream sums;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int left = (int)a.V - (c * 32 + lane) * 8;
     z[c] = left > 0 ? live8(__ldcs(reinterpret_cast<const uint4*>(a.z + i * a.ldl + (c * 32 + lane) * 8)), left) : no_words();
   }
   if (lane == 0) counts[warp] = 0;
+  float top = -INFINITY;
 #pragma unroll
-  for (int c = 0; c < C; ++c) sums.add(z[c], top8(z[c]), a.scale);
-  const Sums v = join<32>(sums.sums());
+  for (int c = 0; c < C; ++c) top = fmaxf(top, top8(z[c]));
+  Tally tally(top, a.scale);
+#pragma unroll
+  for (int c = 0; c < C; ++c) tally.add(z[c], a.scale);
+  const Sums v = join<32>(tally.sums());
   const uint32_t t = key_reached(a.k, [&](float bound) {
     int n = 0;
 #pragma unroll
@@ -241,27 +300,26 @@ __global__ void __launch_bounds__(kWarpThreads) mp_token_top_warp_kernel(const T
     return __reduce_add_sync(0xFFFFFFFFu, n);
   });
   __syncwarp();
-  const float bound = __half2float(bound_of(t));
+  const __half2 bound = __half2half2(bound_of(t));
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int at = (c * 32 + lane) * 8, left = (int)a.V - at;
-    if (left >= 8) {
-      if (top8(z[c]) >= bound) list8(z[c], at, bound, lists[warp], C * 256, &counts[warp]);
-    } else if (left > 0) {                        // the words past the row are -inf and no entries
-      const uint32_t w[4] = {z[c].x, z[c].y, z[c].z, z[c].w};
-      for (int j = 0; j < left; ++j) {
-        const uint16_t h = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-        if (rows::h2f(h) >= bound) lists[warp][atomicAdd(&counts[warp], 1)] = entry(h, at + j);
-      }
-    }
+    const int at = (c * 32 + lane) * 8, left = (int)a.V - at;     // words past the row are no entries
+    if (left > 0) list8(z[c], at, left, bound, lists[warp], C * 256, &counts[warp]);
   }
   __syncwarp();
-  put(a, i, v, picks[warp], pick(lists[warp], counts[warp], a.k, picks[warp]));
+  const int have = pick<C * 256>(lists[warp], counts[warp], a.k, picks[warp]);
+  order(picks[warp], have, a.k, lists[warp], lane, 32);
+  __syncwarp();
+  put(a, i, v, lists[warp], have, lane, 32);
 }
 
-// ---- longer rows: a block, or CL blocks of a cluster when there are few rows ----
-constexpr int kThreads = 256, kWarps = kThreads / 32, kBatch = 4;       // vectors of a thread between two looks at the list
-constexpr int kCap = 2048, kFull = 1024;          // entries of the list; how many make the bound rise
+// ---- longer rows: a block for a row, or CL blocks of a cluster, the row in their shared memory ----
+//
+// Persistent blocks, whose threads bring their own vectors of the next row by asynchronous copies as soon as they are done with this
+// one's, so each thread reads what it copied itself, and what covers a block's waits are the others on the SM.
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kPartWords = 32768;                 // words of a row that a block takes if a cluster of 8 can
+constexpr int kCap = 1023;                        // entries of the list
 
 // The part of a row that a block has: vectors mine, mine + hop, ..
 struct Part {
@@ -283,21 +341,6 @@ __device__ __forceinline__ int reach8(const uint4& z, int left, float bound, boo
     n += j < left && (above ? f > bound : f >= bound);
   }
   return n;
-}
-__device__ __forceinline__ void list_part(const uint4& z, int vec, int V, float bound, Entry* list, int* count) {
-  if (top8(z) < bound) return;
-  if (V - vec * 8 >= 8) {
-    list8(z, vec * 8, bound, list, kCap, count);
-    return;
-  }
-  const uint32_t w[4] = {z.x, z.y, z.z, z.w};
-  for (int j = 0; j < V - vec * 8; ++j) {
-    const uint16_t h = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-    if (rows::h2f(h) >= bound) {
-      const int n = atomicAdd(count, 1);
-      if (n < kCap) list[n] = entry(h, vec * 8 + j);
-    }
-  }
 }
 // The part's k largest by counting: exact whatever the row, 16 reads of it.  By the whole block; `list` receives k entries or all.
 __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, int* count, int* scratch) {
@@ -366,130 +409,181 @@ __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, in
 }
 
 template <int CL>
-__global__ void __launch_bounds__(kThreads) mp_token_top_row_kernel(const TopArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) mp_token_top_row_kernel(const TopArgs a) {
+  extern __shared__ uint4 slots[];                // [vectors]
   __shared__ Entry list[kCap];
-  __shared__ Entry picks[CL * MP_TOP_MAX_K];      // of rank 0: CL > 1, what the blocks picked
-  __shared__ Entry final_picks[CL > 1 ? MP_TOP_MAX_K : 1];
-  __shared__ Sums part_sums[kWarps], block_sums[CL];
-  __shared__ int block_have[CL];
-  __shared__ int count, scratch[kWarps];
+  __shared__ Entry picks[MP_TOP_MAX_K], sorted[MP_TOP_MAX_K];
+  __shared__ Entry gathered[2][CL > 1 ? CL * MP_TOP_MAX_K : 1];           // rank 0: what each block sorted
+  __shared__ Sums part_sums[kWarps], block_sums[2][CL];
+  __shared__ int block_have[2][CL], count, scratch[kWarps];
   __shared__ float warp_bound[kWarps];
-  __shared__ uint32_t raised;
   const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t i = blockIdx.x / CL;
-  if (a.weight != nullptr && a.weight[i] == 0.0f) {          // the same for all blocks of a row
-    if (rank == 0 && warp == 0) put_masked(a, i);
-    return;
-  }
+  const int64_t step = gridDim.x / CL;
+  const int V = (int)a.V, vecs = (V + 7) / 8, mine = rank * kThreads + (int)threadIdx.x;     // vector c: mine + c CL threads
+  const int own = mine < vecs ? (vecs - mine + CL * kThreads - 1) / (CL * kThreads) : 0;
+  // every vector but perhaps the row's last is whole
+  const int whole = own > 0 && (mine + (own - 1) * CL * kThreads) * 8 + 8 > V ? own - 1 : own, tail = own > whole ? V % 8 : 0;
+  const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
+  uint4* z = slots + threadIdx.x;
+  // Each warp's share of k: what so many of its lanes' maxima reach, k words of the row reach in the lowest of the warps.  Warps
+  // without a whole layer of vectors have none.
+  const int first_layer = vecs - rank * kThreads, taking = first_layer >= kThreads ? kWarps : max(first_layer / 32, 1);
+  const int share = (a.k + taking - 1) / taking;
+  auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
+  auto fetch = [&](int64_t i) {
+    const uint16_t* from = a.z + i * a.ldl + (int64_t)mine * 8;
+    for (int c = 0; c < own; ++c)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + c * kThreads * 16), "l"(from + c * (CL * kThreads * 8)) : "memory");
+  };
   if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
-  const int V = (int)a.V, vecs = (V + 7) / 8;
-  const Part p{a.z + i * a.ldl, V, vecs, rank * kThreads + (int)threadIdx.x, CL * kThreads};
-  Stream sums;
-  float bound = 0.0f;
-  if (threadIdx.x == 0) count = 0;
-  bool overflow = false, looked = false;
-  for (int base = rank * kThreads; base < vecs; base += kBatch * p.hop) {
-    uint4 z[kBatch];
-    float top[kBatch];
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) {
-      const int vec = base + c * p.hop + threadIdx.x;
-      z[c] = vec < vecs ? p.load(vec) : no_words();
+  int half = 0;
+  float w = weight_of(blockIdx.x / CL);
+  if (w != 0.0f) fetch(blockIdx.x / CL);          // a masked row is not read
+  for (int64_t i = blockIdx.x / CL; i < a.N; i += step) {
+    const float w_next = weight_of(i + step);
+    if (w == 0.0f) {
+      if (rank == 0 && warp == 0) put_masked(a, i);
+      if (w_next != 0.0f) fetch(i + step);
+      w = w_next;
+      continue;
     }
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) top[c] = top8(z[c]);
-    if (!looked) {
-      // Each warp finds what its share of k vectors reaches: together at least k words reach the lowest of these.  Warps
-      // that have no whole first layer of vectors do not take part.
-      const int here = vecs - base, taking = here >= kThreads ? kWarps : here >= 32 ? here / 32 : 1;
-      if (warp < taking) {
-        const uint32_t t = key_reached((a.k + taking - 1) / taking, [&](float b) {
-          int n = 0;
-#pragma unroll
-          for (int c = 0; c < kBatch; ++c) n += top[c] >= b;
-          return __reduce_add_sync(0xFFFFFFFFu, n);
-        });
-        if (lane == 0) warp_bound[warp] = __half2float(bound_of(t));
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (tail > 0) z[whole * kThreads] = live8(z[whole * kThreads], tail);
+    __half2 m2 = __half2half2(__ushort_as_half(0xFC00));
+#pragma unroll 4
+    for (int c = 0; c < own; ++c) m2 = max8(m2, z[c * kThreads]);
+    const float top = fmaxf(__low2float(m2), __high2float(m2));
+    Tally tally(top, a.scale);
+#pragma unroll 4
+    for (int c = 0; c < own; ++c) tally.add(z[c * kThreads], a.scale);
+    const Sums part = join<32>(tally.sums());
+    int above = 0, reach = 0;
+#pragma unroll 8
+    for (int l = 0; l < 32; ++l) {
+      const float x = __shfl_sync(0xFFFFFFFFu, top, l);
+      above += x > top;
+      reach += x >= top;
+    }
+    const uint32_t at = __ballot_sync(0xFFFFFFFFu, above < share && reach >= share);
+    const float warps = share > 32 ? -INFINITY : __shfl_sync(0xFFFFFFFFu, top, at ? __ffs(at) - 1 : 0);
+    if (lane == 0) {
+      part_sums[warp] = part;
+      warp_bound[warp] = warps;
+    }
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    float bound = warp_bound[0];
+    for (int x = 1; x < taking; ++x) bound = fminf(bound, warp_bound[x]);
+    if (top >= bound) {                           // few threads
+      const __half2 two = __float2half2_rn(bound);           // an FP16 value
+      for (int c = 0; c < own; ++c) {
+        const uint4 q = z[c * kThreads];
+        const int vec = mine + c * CL * kThreads;
+        if (top8(q) >= bound) list8(q, vec * 8, V - vec * 8, two, list, kCap, &count);
       }
+    }
+    Sums v = join<kWarps>(part_sums[lane & (kWarps - 1)]);
+    if (w_next != 0.0f) fetch(i + step);          // the slots have been read
+    w = w_next;
+    __syncthreads();
+    if (count > kCap) {
+      const Part p{a.z + i * a.ldl, V, vecs, mine, CL * kThreads};
+      count_through(p, a.k, list, &count, scratch);
+    }
+    const int n = count;
+    int have = min(n, a.k);
+    if (CL == 1 && n <= 64) {                     // one warp's work, while the others begin the next row
+      if (warp == 0) {
+        order(list, n, a.k, sorted, lane, 32);
+        __syncwarp();
+        put(a, i, v, sorted, have, lane, 32);
+      }
+      continue;
+    }
+    const bool many = n > kThreads / 2;           // then the k largest alone are ordered
+    if (many) {
+      if (warp == 0) pick<kCap>(list, n, a.k, picks);
       __syncthreads();
-      bound = warp_bound[0];
-      for (int w = 1; w < taking; ++w) bound = fminf(bound, warp_bound[w]);
-      looked = true;
     }
-#pragma unroll
-    for (int c = 0; c < kBatch; ++c) {
-      const int vec = base + c * p.hop + threadIdx.x;
-      if (vec < vecs) {
-        sums.add(z[c], top[c], a.scale);
-        if (!overflow) list_part(z[c], vec, V, bound, list, &count);
-      }
-    }
-    if (base + kBatch * p.hop < vecs && !overflow) {
-      // The list is looked at by all together: too long, and the bound rises to its k-th entry.
-      if (__syncthreads_or(*(volatile int*)&count > kFull)) {
-        overflow = count > kCap;
-        __syncthreads();                          // everyone has read the count
-        if (!overflow) {
-          if (warp == 0) {
-            const int have = pick(list, count, a.k, picks);
-            Entry least = ~(Entry)0;
-            for (int e = lane; e < have; e += 32) {
-              least = picks[e] < least ? picks[e] : least;
-              list[e] = picks[e];
-            }
-            const uint32_t key = __reduce_min_sync(0xFFFFFFFFu, (uint32_t)(least >> 20));
-            if (lane == 0) {
-              count = have;
-              raised = key;
-            }
-          }
-          __syncthreads();
-          bound = __half2float(bound_of(raised));
-        }
-      }
-    }
-  }
-  const Sums w = join<32>(sums.sums());
-  if (lane == 0) part_sums[warp] = w;
-  __syncthreads();
-  if (overflow || count > kCap) count_through(p, a.k, list, &count, scratch);
-  if constexpr (CL > 1) {
-    if (warp == 0) {
-      const Sums v = join<kWarps>(part_sums[lane & (kWarps - 1)]);
-      Entry* mine = final_picks;                  // free until the blocks have met
-      const int have = pick(list, count, a.k, mine);
+    order(many ? picks : list, many ? have : n, a.k, sorted, threadIdx.x, kThreads);
+    __syncthreads();
+    if constexpr (CL > 1) {
       // hand them to rank 0
-      const uint32_t to = ptx::map_to_cta(ptx::smem_u32(picks + rank * MP_TOP_MAX_K), 0);
-      for (int e = lane; e < have; e += 32)
-        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to + e * 8), "l"(mine[e]) : "memory");
-      if (lane == 0) {
-        const uint32_t s = ptx::map_to_cta(ptx::smem_u32(&block_sums[rank]), 0), h = ptx::map_to_cta(ptx::smem_u32(&block_have[rank]), 0);
+      const uint32_t to = ptx::map_to_cta(ptx::smem_u32(gathered[half] + rank * MP_TOP_MAX_K), 0);
+      for (int e = threadIdx.x; e < have; e += kThreads)
+        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to + e * 8), "l"(sorted[e]) : "memory");
+      if (threadIdx.x == 0) {
+        const uint32_t s = ptx::map_to_cta(ptx::smem_u32(&block_sums[half][rank]), 0);
+        const uint32_t h = ptx::map_to_cta(ptx::smem_u32(&block_have[half][rank]), 0);
         asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(s), "r"(v.k) : "memory");
         asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(s + 4), "r"(__float_as_int(v.s)) : "memory");
         asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(s + 8), "r"(__float_as_int(v.u)) : "memory");
         asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(h), "r"(have) : "memory");
       }
-      __syncwarp();
-    }
-    ptx::cluster_sync();
-    if (rank == 0 && warp == 0) {
-      const Sums v = join<CL>(block_sums[lane & (CL - 1)]);
-      int all = 0;                                // one list of what the blocks picked
-      for (int r = 0; r < CL; ++r) {
-        for (int e = lane; e < block_have[r]; e += 32) list[all + e] = picks[r * MP_TOP_MAX_K + e];
-        all += block_have[r];
+      ptx::cluster_sync();
+      if (rank == 0) {
+        v = join<CL>(block_sums[half][lane & (CL - 1)]);
+        // an entry's place is its place in its own list and the number of larger ones in each of the others
+        const int* in = block_have[half];
+        have = 0;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) have += in[r];
+        have = min(have, a.k);
+        for (int x = threadIdx.x; x < CL * a.k; x += kThreads) {
+          const int r = x / a.k, e = x - r * a.k;
+          if (e >= in[r]) continue;
+          const Entry entry = gathered[half][r * MP_TOP_MAX_K + e];
+          int before[CL], place = 0;              // (own list: finds itself)
+#pragma unroll
+          for (int o = 0; o < CL; ++o) before[o] = 0;
+#pragma unroll
+          for (int hop = MP_TOP_MAX_K; hop > 0; hop >>= 1)
+#pragma unroll
+            for (int o = 0; o < CL; ++o)
+              if (before[o] + hop <= in[o] && gathered[half][o * MP_TOP_MAX_K + before[o] + hop - 1] > entry) before[o] += hop;
+#pragma unroll
+          for (int o = 0; o < CL; ++o) place += before[o];
+          if (place < a.k) sorted[place] = entry;
+        }
+        __syncthreads();
       }
-      __syncwarp();
-      const int have = pick(list, all, a.k, final_picks);
-      put(a, i, v, final_picks, have);
+      half ^= 1;
+      if (rank != 0) continue;
     }
-  } else {
-    if (warp == 0) {
-      const Sums v = join<kWarps>(part_sums[lane & (kWarps - 1)]);
-      const int have = pick(list, count, a.k, picks);
-      put(a, i, v, picks, have);
-    }
+    put(a, i, v, sorted, have, threadIdx.x, kThreads);
   }
+}
+
+// Persistent grid of whole clusters, as many as are resident at once (asked once per device, kernel and size of a part).
+template <int CL>
+int row_launch(const TopArgs& a, cudaStream_t st) {
+  static mp::PerDevice resident[MP_POLICY_MAX_V / 8 / (CL * kThreads) + 2];        // by layers
+  const int64_t vecs = (a.V + 7) / 8, layers = (vecs + CL * kThreads - 1) / (CL * kThreads);
+  auto kernel = mp_token_top_row_kernel<CL>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)layers * kThreads * 16;
+  cfg.stream = st;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = CL;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int dev = 0;
+  MP_CUDA_TRY(cudaGetDevice(&dev));
+  int clusters = resident[layers].get(dev);
+  if (clusters == 0) {
+    MP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MP_POLICY_MAX_V / 8 * 2));
+    cfg.gridDim = dim3(CL * 148 * 16, 1, 1);
+    MP_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg));
+    if (clusters < 1) clusters = 1;
+    resident[layers].set(dev, clusters);
+  }
+  if (a.N < clusters) clusters = (int)a.N;
+  cfg.gridDim = dim3((unsigned)(clusters * CL), 1, 1);
+  MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+  return MP_OK;
 }
 
 template <int C>
@@ -523,20 +617,13 @@ extern "C" int mp_token_top(const void* logits16, int64_t ldl, const void* targe
   if (V <= 256) warp_launch<1>(a, st);
   else if (V <= 512) warp_launch<2>(a, st);
   else if (V <= kWarpWords) warp_launch<4>(a, st);
-  else if (N > 148 || V <= 8 * kThreads * 8)
-    mp_token_top_row_kernel<1><<<(unsigned)N, kThreads, 0, st>>>(a);
-  else {                                          // fewer rows than SMs, each long enough for eight blocks
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(N * 8), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 8;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, mp_token_top_row_kernel<8>, a));
+  else {
+    // A block takes up to kPartWords of a row; more blocks share one where there are fewer rows than SMs and each block has a layer
+    // of vectors still.
+    const bool few = N <= 148 && V > 8 * kThreads * 8;
+    const int rc = few || V > 4 * kPartWords ? row_launch<8>(a, st)
+                   : V <= kPartWords ? row_launch<1>(a, st) : V <= 2 * kPartWords ? row_launch<2>(a, st) : row_launch<4>(a, st);
+    if (rc) return rc;
   }
   mp::count_launch();
   MP_CUDA_TRY(cudaGetLastError());
