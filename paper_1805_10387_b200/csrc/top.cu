@@ -15,6 +15,7 @@
 #include "softmax.cuh"
 
 namespace {
+
 using namespace softmax;
 
 struct TopArgs {
@@ -110,6 +111,17 @@ __device__ __forceinline__ float top8(const uint4& z) {
   const float2 m = __half22float2(max8(__half2half2(__ushort_as_half(0xFC00)), z));
   return fmaxf(m.x, m.y);
 }
+// Bits of the first `left` words of a vector that reach the bound.
+__device__ __forceinline__ uint32_t reach8(const uint4& z, __half2 bound, int left) {
+  const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t hit = __hge2_mask(*reinterpret_cast<const __half2*>(&w[j]), bound);
+    m |= ((hit & 1) | (hit >> 16 & 2)) << (2 * j);
+  }
+  return left >= 8 ? m : m & ((1u << left) - 1);
+}
 // Lists the first `left` words of a vector (its first at id `at`) that reach the bound.
 __device__ __forceinline__ void list8(const uint4& z, int at, int left, __half2 bound, Entry* list, int cap, int* count) {
   const uint32_t w[4] = {z.x, z.y, z.z, z.w};
@@ -203,37 +215,28 @@ __device__ __noinline__ int pick(const Entry* list, int count, int k, Entry* out
   return have;
 }
 
-// Puts `count` (at most 128) entries in order, largest first, the k first of them.  By `team` threads of which this is number
-// `lane`; the caller sees to the barriers.
-__device__ __forceinline__ void order(const Entry* list, int count, int k, Entry* out, int lane, int team) {
-  for (int e = lane; e < count; e += team) {
-    const Entry mine = list[e];
-    int rank = 0;
-#pragma unroll 8
-    for (int o = 0; o < count; ++o) rank += list[o] > mine;
-    if (rank < k) out[rank] = mine;
-  }
+// A row's outputs: one of its entries, a place that no number is left for, and what goes with the row.
+__device__ __forceinline__ float lp_of(const TopArgs& a, const Sums& v, float z) {
+  return (fmaf(z, a.scale, -(float)v.k) - log2f(v.s)) * kLn2;
 }
-// A row's outputs, from its sums and its `have` entries in order, by `team` threads of which this is number `lane`.
-__device__ __forceinline__ void put(const TopArgs& a, int64_t i, const Sums& v, const Entry* sorted, int have, int lane, int team) {
-  const float log2s = log2f(v.s), k = (float)v.k;
-  auto lp = [&](float z) { return (fmaf(z, a.scale, -k) - log2s) * kLn2; };
-  for (int e = lane; e < a.k; e += team) {
-    const bool is = e < have;                     // else the row has fewer numbers than k
-    a.ids[i * a.k + e] = is ? id_of(sorted[e]) : -1;
-    a.tlogp[i * a.k + e] = is ? lp(logit_of(sorted[e])) : NAN;
+__device__ __forceinline__ void put_one(const TopArgs& a, int64_t i, const Sums& v, int place, Entry e) {
+  a.ids[i * a.k + place] = id_of(e);
+  a.tlogp[i * a.k + place] = lp_of(a, v, logit_of(e));
+}
+__device__ __forceinline__ void put_none(const TopArgs& a, int64_t i, int place) {
+  a.ids[i * a.k + place] = -1;
+  a.tlogp[i * a.k + place] = NAN;
+}
+__device__ __forceinline__ void put_row(const TopArgs& a, int64_t i, const Sums& v) {
+  if (a.entropy != nullptr) {
+    const float h = (log2f(v.s) - v.u / v.s) * kLn2;
+    a.entropy[i] = h < 0.0f ? 0.0f : h;
   }
-  if (lane == 0) {
-    if (a.entropy != nullptr) {
-      const float h = (log2s - v.u / v.s) * kLn2;
-      a.entropy[i] = h < 0.0f ? 0.0f : h;
-    }
-    if (a.logp != nullptr) {
-      const int64_t t = a.id_bytes == 8 ? rows::load_id<int64_t>(a.targets, i) : rows::load_id<int32_t>(a.targets, i);
-      const bool good = t >= 0 && t < a.V;
-      a.logp[i] = good ? lp(rows::h2f(a.z[i * a.ldl + t])) : NAN;
-      if (!good) rows::record_bad_id(a.st);
-    }
+  if (a.logp != nullptr) {
+    const int64_t t = a.id_bytes == 8 ? rows::load_id<int64_t>(a.targets, i) : rows::load_id<int32_t>(a.targets, i);
+    const bool good = t >= 0 && t < a.V;
+    a.logp[i] = good ? lp_of(a, v, rows::h2f(a.z[i * a.ldl + t])) : NAN;
+    if (!good) rows::record_bad_id(a.st);
   }
 }
 __device__ __forceinline__ void put_masked(const TopArgs& a, int64_t i) {
@@ -308,18 +311,27 @@ __global__ void __launch_bounds__(kWarpThreads) mp_token_top_warp_kernel(const T
   }
   __syncwarp();
   const int have = pick<C * 256>(lists[warp], counts[warp], a.k, picks[warp]);
-  order(picks[warp], have, a.k, lists[warp], lane, 32);
-  __syncwarp();
-  put(a, i, v, lists[warp], have, lane, 32);
+  for (int e = lane; e < a.k; e += 32) {
+    if (e >= have) {
+      put_none(a, i, e);
+      continue;
+    }
+    const Entry mine = picks[warp][e];
+    int place = 0;
+#pragma unroll 8
+    for (int o = 0; o < have; ++o) place += picks[warp][o] > mine;
+    put_one(a, i, v, place, mine);
+  }
+  if (lane == 0) put_row(a, i, v);
 }
 
 // ---- longer rows: a block for a row, or CL blocks of a cluster, the row in their shared memory ----
 //
 // Persistent blocks, whose threads bring their own vectors of the next row by asynchronous copies as soon as they are done with this
 // one's, so each thread reads what it copied itself, and what covers a block's waits are the others on the SM.
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kPartWords = 32768;                 // words of a row that a block takes if a cluster of 8 can
-constexpr int kCap = 1023;                        // entries of the list
+constexpr int kCap = 1024;                        // entries of the list
+constexpr int kOrdered = 192;                     // so many are ordered by comparing all with all; of more the k largest are picked
 
 // The part of a row that a block has: vectors mine, mine + hop, ..
 struct Part {
@@ -332,7 +344,7 @@ struct Part {
   }
 };
 // Words of a vector that exist and reach the bound (a bound of -inf must not count what lies past the row).
-__device__ __forceinline__ int reach8(const uint4& z, int left, float bound, bool above) {
+__device__ __forceinline__ int count8(const uint4& z, int left, float bound, bool above) {
   const uint32_t w[4] = {z.x, z.y, z.z, z.w};
   int n = 0;
 #pragma unroll
@@ -343,7 +355,9 @@ __device__ __forceinline__ int reach8(const uint4& z, int left, float bound, boo
   return n;
 }
 // The part's k largest by counting: exact whatever the row, 16 reads of it.  By the whole block; `list` receives k entries or all.
+template <int kThreads>
 __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, int* count, int* scratch) {
+  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   auto block_sum = [&](int n) {
     n = __reduce_add_sync(0xFFFFFFFFu, n);
@@ -356,7 +370,7 @@ __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, in
   };
   const uint32_t t = key_reached(k, [&](float bound) {
     int n = 0;
-    for (int vec = p.mine; vec < p.vecs; vec += p.hop) n += reach8(p.load(vec), p.V - vec * 8, bound, false);
+    for (int vec = p.mine; vec < p.vecs; vec += p.hop) n += count8(p.load(vec), p.V - vec * 8, bound, false);
     return block_sum(n);
   });
   const float bound = __half2float(bound_of(t));
@@ -385,7 +399,7 @@ __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, in
     uint4 z = no_words();
     if (vec < p.vecs) {
       z = p.load(vec);
-      n = reach8(z, p.V - vec * 8, bound, false) - reach8(z, p.V - vec * 8, bound, true);
+      n = count8(z, p.V - vec * 8, bound, false) - count8(z, p.V - vec * 8, bound, true);
     }
     int before = n;                               // ties in the vectors of this round up to this one
 #pragma unroll
@@ -408,35 +422,37 @@ __device__ __noinline__ void count_through(const Part& p, int k, Entry* list, in
   __syncthreads();
 }
 
-template <int CL>
-__global__ void __launch_bounds__(kThreads, 3) mp_token_top_row_kernel(const TopArgs a) {
+template <int CL, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 8) mp_token_top_row_kernel(const TopArgs a) {
+  constexpr int kWarps = kThreads / 32;
   extern __shared__ uint4 slots[];                // [vectors]
   __shared__ Entry list[kCap];
-  __shared__ Entry picks[MP_TOP_MAX_K], sorted[MP_TOP_MAX_K];
   __shared__ Entry gathered[2][CL > 1 ? CL * MP_TOP_MAX_K : 1];           // rank 0: what each block sorted
-  __shared__ Sums part_sums[kWarps], block_sums[2][CL];
-  __shared__ int block_have[2][CL], count, scratch[kWarps];
-  __shared__ float warp_bound[kWarps];
+  __shared__ Sums part_sums[2][kWarps], block_sums[2][CL];
+  __shared__ int block_have[2][CL], count[2], scratch[kWarps];
+  __shared__ float bounds[CL * kWarps];           // of every warp of the row's blocks
   const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t step = gridDim.x / CL;
   const int V = (int)a.V, vecs = (V + 7) / 8, mine = rank * kThreads + (int)threadIdx.x;     // vector c: mine + c CL threads
   const int own = mine < vecs ? (vecs - mine + CL * kThreads - 1) / (CL * kThreads) : 0;
+  const int layers = (vecs - rank * kThreads + CL * kThreads - 1) / (CL * kThreads);
   // every vector but perhaps the row's last is whole
   const int whole = own > 0 && (mine + (own - 1) * CL * kThreads) * 8 + 8 > V ? own - 1 : own, tail = own > whole ? V % 8 : 0;
   const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
   uint4* z = slots + threadIdx.x;
-  // Each warp's share of k: what so many of its lanes' maxima reach, k words of the row reach in the lowest of the warps.  Warps
-  // without a whole layer of vectors have none.
-  const int first_layer = vecs - rank * kThreads, taking = first_layer >= kThreads ? kWarps : max(first_layer / 32, 1);
+  // Each warp's share of k: when every warp has a value that so many of its words reach, k words of the row reach the lowest
+  // of these values.  Warps without a whole layer of vectors (in a row of one block) have none.
+  const int taking = CL > 1 ? CL * kWarps : vecs >= kThreads ? kWarps : vecs / 32;
   const int share = (a.k + taking - 1) / taking;
   auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
   auto fetch = [&](int64_t i) {
     const uint16_t* from = a.z + i * a.ldl + (int64_t)mine * 8;
+#pragma unroll 4
     for (int c = 0; c < own; ++c)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(base + c * kThreads * 16), "l"(from + c * (CL * kThreads * 8)) : "memory");
   };
   if constexpr (CL > 1) ptx::cluster_sync();      // every block of the cluster has started
-  int half = 0;
+  int half = 0, turn = 0;
   float w = weight_of(blockIdx.x / CL);
   if (w != 0.0f) fetch(blockIdx.x / CL);          // a masked row is not read
   for (int64_t i = blockIdx.x / CL; i < a.N; i += step) {
@@ -449,69 +465,125 @@ __global__ void __launch_bounds__(kThreads, 3) mp_token_top_row_kernel(const Top
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (tail > 0) z[whole * kThreads] = live8(z[whole * kThreads], tail);
-    __half2 m2 = __half2half2(__ushort_as_half(0xFC00));
+    // the vectors with the largest and the second largest maxima, and the largest of the others'
+    float top = -INFINITY, second = -INFINITY, third = -INFINITY;
+    int in = 0, in2 = 0;
 #pragma unroll 4
-    for (int c = 0; c < own; ++c) m2 = max8(m2, z[c * kThreads]);
-    const float top = fmaxf(__low2float(m2), __high2float(m2));
+    for (int c = 0; c < own; ++c) {
+      const float x = top8(z[c * kThreads]);
+      const bool first = x > top;
+      third = fmaxf(third, fminf(second, x));
+      in2 = first ? in : x > second ? c : in2;
+      second = fmaxf(second, fminf(top, x));
+      in = first ? c : in;
+      top = fmaxf(top, x);
+    }
     Tally tally(top, a.scale);
 #pragma unroll 4
     for (int c = 0; c < own; ++c) tally.add(z[c * kThreads], a.scale);
     const Sums part = join<32>(tally.sums());
-    int above = 0, reach = 0;
-#pragma unroll 8
-    for (int l = 0; l < 32; ++l) {
-      const float x = __shfl_sync(0xFFFFFFFFu, top, l);
-      above += x > top;
-      reach += x >= top;
-    }
-    const uint32_t at = __ballot_sync(0xFFFFFFFFu, above < share && reach >= share);
-    const float warps = share > 32 ? -INFINITY : __shfl_sync(0xFFFFFFFFu, top, at ? __ffs(at) - 1 : 0);
-    if (lane == 0) {
-      part_sums[warp] = part;
-      warp_bound[warp] = warps;
-    }
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    float bound = warp_bound[0];
-    for (int x = 1; x < taking; ++x) bound = fminf(bound, warp_bound[x]);
-    if (top >= bound) {                           // few threads
-      const __half2 two = __float2half2_rn(bound);           // an FP16 value
-      for (int c = 0; c < own; ++c) {
-        const uint4 q = z[c * kThreads];
-        const int vec = mine + c * CL * kThreads;
-        if (top8(q) >= bound) list8(q, vec * 8, V - vec * 8, two, list, kCap, &count);
+    // the share-th largest of the lanes' maxima: a few by taking the largest away, more (and the second ones too) by comparing
+    // all with all
+    float mine_reaches;
+    if (share <= 4) {
+      const int bits = __float_as_int(top);
+      int key = bits ^ (bits >> 31 & 0x7FFFFFFF), best = 0;  // ordered as the values are
+      for (int s = 0; s < share; ++s) {
+        best = __reduce_max_sync(0xFFFFFFFFu, key);
+        const uint32_t has = __ballot_sync(0xFFFFFFFFu, key == best);
+        if (lane == __ffs(has) - 1) key = (int)0x80000000;
       }
+      mine_reaches = __int_as_float(best ^ (best >> 31 & 0x7FFFFFFF));
+    } else {
+      int above = 0, reach = 0, above2 = 0, reach2 = 0;
+#pragma unroll 8
+      for (int l = 0; l < 32; ++l) {
+        const float x = __shfl_sync(0xFFFFFFFFu, top, l), y = __shfl_sync(0xFFFFFFFFu, second, l);
+        above += (x > top) + (y > top);
+        reach += (x >= top) + (y >= top);
+        above2 += (x > second) + (y > second);
+        reach2 += (x >= second) + (y >= second);
+      }
+      const uint32_t at = __ballot_sync(0xFFFFFFFFu, above < share && reach >= share);
+      const uint32_t at2 = __ballot_sync(0xFFFFFFFFu, above2 < share && reach2 >= share);
+      const float x = __shfl_sync(0xFFFFFFFFu, top, at ? __ffs(at) - 1 : 0), y = __shfl_sync(0xFFFFFFFFu, second, at2 ? __ffs(at2) - 1 : 0);
+      mine_reaches = at ? x : y;
     }
-    Sums v = join<kWarps>(part_sums[lane & (kWarps - 1)]);
+    if (threadIdx.x == 0) count[turn] = 0;
+    if (lane == 0) part_sums[turn][warp] = part;
+    float bound;
+    if constexpr (CL > 1) {
+      if (lane < CL) {
+        const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&bounds[rank * kWarps + warp]), lane);
+        asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to), "r"(__float_as_int(mine_reaches)) : "memory");
+      }
+      __syncwarp();
+      ptx::cluster_sync();
+      bound = bounds[lane % (CL * kWarps)];
+      if (CL * kWarps > 32) bound = fminf(bound, bounds[lane + 32 < CL * kWarps ? lane + 32 : lane]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) bound = fminf(bound, __shfl_xor_sync(0xFFFFFFFFu, bound, o));
+    } else {
+      if (lane == 0) bounds[warp] = mine_reaches;
+      __syncthreads();
+      bound = bounds[0];
+      for (int x = 1; x < taking; ++x) bound = fminf(bound, bounds[x]);
+    }
+    // The few threads whose largest word reaches the bound list what does so in its vector; fewer have another such vector, and
+    // hardly one a third.
+    const __half2 two = __float2half2_rn(bound);             // an FP16 value
+    auto list_vector = [&](int c, bool on) {                 // by a whole warp
+      const int vec = mine + c * CL * kThreads;
+      uint32_t hits = on ? reach8(z[c * kThreads], two, V - vec * 8) : 0;
+      for (uint32_t any = __ballot_sync(0xFFFFFFFFu, hits); any; any = __ballot_sync(0xFFFFFFFFu, hits)) {
+        int to = 0;
+        if (lane == 0) to = atomicAdd(&count[turn], __popc(any));
+        to = __shfl_sync(0xFFFFFFFFu, to, 0) + __popc(any & ((1u << lane) - 1));
+        const int j = __ffs(hits) - 1;
+        if (hits && to < kCap) list[to] = entry(reinterpret_cast<const uint16_t*>(z + c * kThreads)[j], vec * 8 + j);
+        hits &= hits - 1;
+      }
+    };
+    if (__any_sync(0xFFFFFFFFu, top >= bound)) list_vector(in, top >= bound && own > 0);
+    if (__any_sync(0xFFFFFFFFu, second >= bound)) list_vector(in2, second >= bound && own > 1);
+    if (__any_sync(0xFFFFFFFFu, third >= bound))
+      for (int c = 0; c < layers; ++c) list_vector(c < own ? c : 0, c < own && c != in && c != in2 && third >= bound);
+    __syncthreads();
     if (w_next != 0.0f) fetch(i + step);          // the slots have been read
     w = w_next;
-    __syncthreads();
-    if (count > kCap) {
+    int n = count[turn];
+    if (n > kCap) {
       const Part p{a.z + i * a.ldl, V, vecs, mine, CL * kThreads};
-      count_through(p, a.k, list, &count, scratch);
-    }
-    const int n = count;
-    int have = min(n, a.k);
-    if (CL == 1 && n <= 64) {                     // one warp's work, while the others begin the next row
-      if (warp == 0) {
-        order(list, n, a.k, sorted, lane, 32);
-        __syncwarp();
-        put(a, i, v, sorted, have, lane, 32);
-      }
-      continue;
-    }
-    const bool many = n > kThreads / 2;           // then the k largest alone are ordered
-    if (many) {
-      if (warp == 0) pick<kCap>(list, n, a.k, picks);
+      count_through<kThreads>(p, a.k, list, &count[turn], scratch);
+      n = count[turn];
+    } else if (n > kOrdered) {
+      if (warp == 0) pick<kCap>(list, n, a.k, list);
       __syncthreads();
+      n = min(n, a.k);
     }
-    order(many ? picks : list, many ? have : n, a.k, sorted, threadIdx.x, kThreads);
-    __syncthreads();
+    const int have = min(n, a.k);
+    Sums v{0, 0.0f, 0.0f};
+    if (warp * 32 < max(n, 1)) v = join<kWarps>(part_sums[turn][lane & (kWarps - 1)]);
+    turn ^= 1;                                    // a warp may be a row ahead
+    for (int e = threadIdx.x; e - lane < n; e += kThreads) {
+      // an entry's place: how many are larger
+      const Entry mine_is = list[min(e, n - 1)];
+      int place = 0;
+#pragma unroll 8
+      for (int o = 0; o < n; ++o) place += list[o] > mine_is;
+      if (e >= n || place >= a.k) continue;
+      if constexpr (CL == 1) {
+        put_one(a, i, v, place, mine_is);
+      } else {                                    // rank 0 gets it
+        const uint32_t to = ptx::map_to_cta(ptx::smem_u32(gathered[half] + rank * MP_TOP_MAX_K + place), 0);
+        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(mine_is) : "memory");
+      }
+    }
+    if constexpr (CL == 1) {
+      if ((int)threadIdx.x >= have && (int)threadIdx.x < a.k) put_none(a, i, threadIdx.x);
+      if (threadIdx.x == 0) put_row(a, i, v);
+    }
     if constexpr (CL > 1) {
-      // hand them to rank 0
-      const uint32_t to = ptx::map_to_cta(ptx::smem_u32(gathered[half] + rank * MP_TOP_MAX_K), 0);
-      for (int e = threadIdx.x; e < have; e += kThreads)
-        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to + e * 8), "l"(sorted[e]) : "memory");
       if (threadIdx.x == 0) {
         const uint32_t s = ptx::map_to_cta(ptx::smem_u32(&block_sums[half][rank]), 0);
         const uint32_t h = ptx::map_to_cta(ptx::smem_u32(&block_have[half][rank]), 0);
@@ -525,15 +597,14 @@ __global__ void __launch_bounds__(kThreads, 3) mp_token_top_row_kernel(const Top
         v = join<CL>(block_sums[half][lane & (CL - 1)]);
         // an entry's place is its place in its own list and the number of larger ones in each of the others
         const int* in = block_have[half];
-        have = 0;
+        int all = 0;
 #pragma unroll
-        for (int r = 0; r < CL; ++r) have += in[r];
-        have = min(have, a.k);
+        for (int r = 0; r < CL; ++r) all += in[r];
         for (int x = threadIdx.x; x < CL * a.k; x += kThreads) {
           const int r = x / a.k, e = x - r * a.k;
           if (e >= in[r]) continue;
           const Entry entry = gathered[half][r * MP_TOP_MAX_K + e];
-          int before[CL], place = 0;              // (own list: finds itself)
+          int before[CL], to = 0;                 // (own list: finds itself)
 #pragma unroll
           for (int o = 0; o < CL; ++o) before[o] = 0;
 #pragma unroll
@@ -542,24 +613,23 @@ __global__ void __launch_bounds__(kThreads, 3) mp_token_top_row_kernel(const Top
             for (int o = 0; o < CL; ++o)
               if (before[o] + hop <= in[o] && gathered[half][o * MP_TOP_MAX_K + before[o] + hop - 1] > entry) before[o] += hop;
 #pragma unroll
-          for (int o = 0; o < CL; ++o) place += before[o];
-          if (place < a.k) sorted[place] = entry;
+          for (int o = 0; o < CL; ++o) to += before[o];
+          if (to < a.k) put_one(a, i, v, to, entry);
         }
-        __syncthreads();
+        if ((int)threadIdx.x >= all && (int)threadIdx.x < a.k) put_none(a, i, threadIdx.x);
+        if (threadIdx.x == 0) put_row(a, i, v);
       }
       half ^= 1;
-      if (rank != 0) continue;
     }
-    put(a, i, v, sorted, have, threadIdx.x, kThreads);
   }
 }
 
 // Persistent grid of whole clusters, as many as are resident at once (asked once per device, kernel and size of a part).
-template <int CL>
+template <int CL, int kThreads>
 int row_launch(const TopArgs& a, cudaStream_t st) {
   static mp::PerDevice resident[MP_POLICY_MAX_V / 8 / (CL * kThreads) + 2];        // by layers
   const int64_t vecs = (a.V + 7) / 8, layers = (vecs + CL * kThreads - 1) / (CL * kThreads);
-  auto kernel = mp_token_top_row_kernel<CL>;
+  auto kernel = mp_token_top_row_kernel<CL, kThreads>;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = (size_t)layers * kThreads * 16;
@@ -620,9 +690,10 @@ extern "C" int mp_token_top(const void* logits16, int64_t ldl, const void* targe
   else {
     // A block takes up to kPartWords of a row; more blocks share one where there are fewer rows than SMs and each block has a layer
     // of vectors still.
-    const bool few = N <= 148 && V > 8 * kThreads * 8;
-    const int rc = few || V > 4 * kPartWords ? row_launch<8>(a, st)
-                   : V <= kPartWords ? row_launch<1>(a, st) : V <= 2 * kPartWords ? row_launch<2>(a, st) : row_launch<4>(a, st);
+    const bool few = N <= 148 && V > 8 * 256 * 8;
+    const int rc = few || V > 4 * kPartWords ? row_launch<8, 256>(a, st)
+                   : V <= 16384 ? row_launch<1, 128>(a, st) : V <= kPartWords ? row_launch<1, 256>(a, st)
+                   : V <= 2 * kPartWords ? row_launch<2, 256>(a, st) : row_launch<4, 256>(a, st);
     if (rc) return rc;
   }
   mp::count_launch();
