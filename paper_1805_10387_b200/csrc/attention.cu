@@ -26,31 +26,75 @@ struct FwdArgs {
   float* lse;
 };
 
+// TILES query tiles a block.  Heads of more than 64 elements: two tiles share the keys and values, which would else ask L2
+// for 64 bytes a clock and SM; below that one tile a block and two blocks an SM, whose beginnings and ends cover one another.
 template <int DP>
 struct FwdLayout {
+  static constexpr int kTiles = DP == 64 ? 1 : 2, kBlocks = DP == 64 ? 2 : 1;      // tiles a block, blocks an SM
+  static constexpr int kThreads = kTiles * 256 + 64;         // eight warps a tile, half a row a thread; then products; copies
   static constexpr int kBoxes = DP / 64, kTileBytes = kBoxes * kBoxBytes;
-  static constexpr int kStages = DP == 64 ? 8 : 4;
-  static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+  static constexpr int kStages = DP == 64 ? 5 : 4;
+  static constexpr int kSmem = (kTiles + kStages) * kTileBytes + 1024;
+  static constexpr int kColumns = DP == 64 ? 256 : 512;      // of tensor memory: S, with P in its place, then O, for each tile
 };
-constexpr int kFwdThreads = 320;                  // warps 0-3 and 4-7: a row of each tile a thread; 8: products; 9: copies
 constexpr float kLag = 8.0f;
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 2^x for two values on the multiply-add pipe: whole and fractional part split by rounding, a polynomial of the fraction on
+// [-1/2, 1/2] (least largest relative error, 2.6e-6; fitted to 2^f by weighted least squares), the whole part added to the exponent.
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+  const float2 magic = make_float2(12582912.0f, 12582912.0f);            // 1.5 * 2^23: the sum's low bits are the whole part
+  x = make_float2(fmaxf(x.x, -126.0f), fmaxf(x.y, -126.0f));
+  const float2 t = add2(x, magic), whole = add2(t, make_float2(-12582912.0f, -12582912.0f));
+  const float2 f = fma2(whole, make_float2(-1.0f, -1.0f), x);
+  float2 p = make_float2(0.009570101276040077f, 0.009570101276040077f);
+  p = fma2(p, f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+  p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+  p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+  p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
+                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// Among the 256 threads of tile t: a barrier, and whether anyone says yes; a barrier alone.
+__device__ __forceinline__ bool any_of_tile(int t, bool yes) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 256, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)yes), "r"(1 + t)
+      : "memory");
+  return any != 0;
+}
+__device__ __forceinline__ void tile_sync(int t) { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + t) : "memory"); }
+
 template <int DP>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+__global__ void __launch_bounds__(FwdLayout<DP>::kThreads, FwdLayout<DP>::kBlocks)
 mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                         const __grid_constant__ CUtensorMap mv, const FwdArgs a) {
   using L = FwdLayout<DP>;
+  constexpr int kTiles = L::kTiles, kProducts = kTiles * 8, kCopies = kProducts + 1;      // these two warps' numbers
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  uint8_t* ring = smem + 2 * L::kTileBytes;
-  __shared__ uint64_t q_full, kv_full[L::kStages], kv_empty[L::kStages], tail_full, s_full[2], p_ready[2], o_done[2];
+  uint8_t* ring = smem + kTiles * L::kTileBytes;
+  // p_ready: the first and the second 64 columns of P; row_of, sum_of: what the threads of a row tell one another
+  __shared__ uint64_t q_full, kv_full[L::kStages], kv_empty[L::kStages], tail_full, s_full[kTiles], p_ready[kTiles][2], o_done[kTiles];
+  __shared__ float row_of[kTiles][2][kTile], sum_of[kTiles][2][kTile];
   __shared__ uint32_t s_tmem;
+  __shared__ volatile int failed[kTiles];
   const Shape& s = a.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
   const int head = blockIdx.x % s.heads;
-  const Place at = place_of<2 * kTile>(s, blockIdx.x / s.heads);
+  const Place at = place_of<kTiles * kTile>(s, blockIdx.x / s.heads);
   if (blockIdx.x == 0 && warp == 0) check_offsets(s);
   if (at.tile >= at.tiles) return;
   if (threadIdx.x == 0) {
@@ -60,37 +104,40 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
       ptx::mbar_init(&kv_full[i], 1);
       ptx::mbar_init(&kv_empty[i], 1);
     }
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < kTiles; ++t) {
       ptx::mbar_init(&s_full[t], 1);
-      ptx::mbar_init(&p_ready[t], kTile);
+      ptx::mbar_init(&p_ready[t][0], kTile);
+      ptx::mbar_init(&p_ready[t][1], kTile);
       ptx::mbar_init(&o_done[t], 1);
+      failed[t] = 0;
     }
     ptx::fence_mbar_init();
   }
-  if (warp == 8) {
-    ptx::tmem_alloc(&s_tmem, 512);
+  if (warp == kProducts) {
+    ptx::tmem_alloc(&s_tmem, L::kColumns);
     ptx::tmem_relinquish();
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = s_tmem;
+  constexpr uint32_t kO = kTiles * kTile;
   // the long ones first: a causal query sees all keys before it
-  const int q0 = (int)(at.tiles - 1 - at.tile) * 2 * kTile, len = (int)at.len;
+  const int q0 = (int)(at.tiles - 1 - at.tile) * kTiles * kTile, len = (int)at.len;
   // key blocks that a tile of queries sees
-  int b0[2], b1[2];
+  int b0[kTiles], b1[kTiles];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < kTiles; ++t) {
     const int first = q0 + t * kTile, last = min(first + kTile, len);     // queries
     b0[t] = s.window > 0 && first + 1 > s.window ? (int)(first + 1 - s.window) / kTile : 0;
     b1[t] = first >= len ? b0[t] : ((s.causal ? last : len) + kTile - 1) / kTile;
   }
-  const int j0 = b0[0], j1 = max(b1[0], b1[1]);
+  const int j0 = b0[0], j1 = max(b1[0], b1[kTiles - 1]);
   bool ok = true;
 
-  if (warp == 9) {
+  if (warp == kCopies) {
     const int kv = head / (s.heads / s.kv_heads), row0 = (int)at.start;
-    const int tiles = q0 + kTile < len ? 2 : 1;
+    const int tiles = kTiles == 2 && q0 + kTile < len ? 2 : 1;
     if (lane == 0) {
       ptx::mbar_arrive_expect_tx(&q_full, tiles * L::kTileBytes);
       for (int t = 0; t < tiles; ++t)
@@ -119,11 +166,9 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     }
     // no copy is in flight into a block that has ended
     wait(&q_full, 0);
-    for (int i = max(0, n - L::kStages); i < n; ++i)
-      wait(&kv_full[i % L::kStages], i / L::kStages & 1);
-  } else if (warp == 8) {
+    for (int i = max(0, n - L::kStages); i < n; ++i) wait(&kv_full[i % L::kStages], i / L::kStages & 1);
+  } else if (warp == kProducts) {
     const int ksteps = (s.D + 15) / 16;
-    const uint32_t idesc_s = ptx::idesc_f16_f32(kTile, kTile, false, false);
     const uint32_t idesc_o = ptx::idesc_f16_f32(kTile, ksteps * 16, false, true);
     ok = wait(&q_full, 0);
     for (int j = j0; j <= j1 && ok; ++j) {
@@ -132,81 +177,110 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
       if (ok && j > j0) ok = wait(&kv_full[nv % L::kStages], nv / L::kStages & 1);
       const uint32_t sk = ptx::smem_u32(ring + nk % L::kStages * L::kTileBytes);
       const uint32_t sv = ptx::smem_u32(ring + (nv < 0 ? 0 : nv % L::kStages) * L::kTileBytes);
+      // the last block of a sequence is as wide as it has keys
+      const int before = (min(kTile, len - (j - 1) * kTile) + 15) / 16, wide = (min(kTile, len - j * kTile) + 15) / 16 * 16;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (ok && j > b0[t] && j <= b1[t]) {      // O += P V of the block before
-          ok = wait(&p_ready[t], (j - 1 - b0[t]) & 1);
-          ptx::tc_fence_after_sync();
-          if (ok && lane == 0) {
-            for (int k = 0; k < kTile / 16; ++k)
-              mma_f16_ts(tmem + 256 + t * DP, tmem + t * kTile + k * 8, desc_mn(sv, k), idesc_o, j - 1 > b0[t] || k > 0);
-            ptx::mma_commit(&o_done[t]);
+      for (int t = 0; t < kTiles; ++t) {
+        if (ok && j > b0[t] && j <= b1[t]) {      // O += P V of the block before, in two halves
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            ok = ok && wait(&p_ready[t][h], (j - 1 - b0[t]) & 1);
+            ptx::tc_fence_after_sync();
+            if (ok && ptx::elect_one()) {
+              if (h == 0) {
+                product_ts<0, 4>(tmem + kO + t * DP, tmem + t * kTile, desc_mn(sv), idesc_o, before, j - 1 > b0[t]);
+              } else {
+                product_ts<4, 8>(tmem + kO + t * DP, tmem + t * kTile, desc_mn(sv), idesc_o, before, true);
+                ptx::mma_commit(&o_done[t]);
+              }
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
         if (ok && j >= b0[t] && j < b1[t]) {      // S of this one, in the place of that P
           ptx::tc_fence_after_sync();
-          if (lane == 0) {
-            const uint32_t sq = ptx::smem_u32(smem + t * L::kTileBytes);
-            for (int k = 0; k < ksteps; ++k)
-              ptx::mma_f16_ss(tmem + t * kTile, desc_k(sq, k), desc_k(sk, k), idesc_s, k > 0);
+          if (ptx::elect_one()) {
+            product_ss<DP / 16>(tmem + t * kTile, desc_k(ptx::smem_u32(smem + t * L::kTileBytes)), desc_k(sk),
+                                ptx::idesc_f16_f32(kTile, wide, false, false), ksteps);
             ptx::mma_commit(&s_full[t]);
           }
           __syncwarp();
         }
       }
-      if (ok && lane == 0) {
+      if (ok && ptx::elect_one()) {
         if (j > j0) ptx::mma_commit(&kv_empty[nv % L::kStages]);
         if (j < j1) ptx::mma_commit(&kv_empty[nk % L::kStages]);
       }
       __syncwarp();
     }
   } else {
-    const int t = warp >> 2, row = q0 + t * kTile + (warp & 3) * 32 + lane;      // of the sequence
+    // Two threads have a row, 64 columns each: a tile's scores pass through twice as many warps in half the time, and it is this
+    // time that the products of the tile wait for.
+    const int t = warp >> 3, half = warp >> 2 & 1, in_tile = (warp & 3) * 32 + lane, row = q0 + t * kTile + in_tile;   // of the sequence
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + t * kTile + lanes, to = tmem + 256 + t * DP + lanes;
-    const int lo = t ? b0[1] : b0[0], hi = t ? b1[1] : b1[0];
+    const uint32_t ts = tmem + t * kTile + half * 64 + lanes, to = tmem + kO + t * DP + half * (DP / 2) + lanes;
+    const int lo = t ? b0[kTiles - 1] : b0[0], hi = t ? b1[kTiles - 1] : b1[0];
     const float c = s.scale_log2;
+    const bool some = row - lane < len;           // the warp has rows that exist
     // the keys that this query sees
     const int key1 = s.causal ? min(row + 1, len) : len;
     const int key0 = s.window > 0 && row + 1 > s.window ? (int)(row + 1 - s.window) : 0;
-    const int first = q0 + t * kTile;             // blocks between these two are seen whole by every query of the tile
-    const int whole1 = s.causal ? min(first + 1, len) : len;
-    const int whole0 = s.window > 0 && first + kTile > s.window ? (int)(first + kTile - s.window) : 0;
+    // blocks between these two are seen whole by every query of the warp; no query of it sees a key from `end` on
+    const int first = row - lane;
+    const int whole1 = s.causal ? min(first + 1, len) : len, end = s.causal ? min(first + 32, len) : len;
+    const int whole0 = s.window > 0 && first + 32 > s.window ? (int)(first + 32 - s.window) : 0;
     float m = -INFINITY, sum = 0.0f;
-    for (int j = lo; j < hi && ok; ++j) {
-      ok = wait(&s_full[t], (j - lo) & 1);
-      if (!ok) break;
+    for (int j = lo; j < hi; ++j) {
+      ok = ok && wait(&s_full[t], (j - lo) & 1);
       ptx::tc_fence_after_sync();
-      uint32_t r[4][32];
+      const int k0 = j * kTile + half * 64;       // this thread's first key
+      // pieces of 32 columns with keys that are seen (rows of what comes behind the sequence: whatever P holds stays in them)
+      const int pieces = !ok || !some ? 0 : max(0, min(2, (end - k0 + 31) / 32));
+      const bool edge = k0 + 64 > whole1 || k0 < whole0;
+      const int stop = key1 - k0, begin = key0 - k0;
+      // The scores are read twice, for the maximum and for the weights: in registers all the while they would not leave room
+      // for enough warps.
+      uint32_t r[32];
+      auto load = [&](int i) {
+        ptx::tmem_ld_32x32(ts + i * 32, r);
+        ptx::tmem_ld_wait();
+        if (edge) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) ptx::tmem_ld_32x32(ts + i * 32, r[i]);
-      ptx::tmem_ld_wait();
-      const int k0 = j * kTile;
-      if (k0 + kTile > whole1 || k0 < whole0) {
-        const int end = key1 - k0, begin = key0 - k0;
+          for (int e = 0; e < 32; ++e)
+            if (i * 32 + e >= stop || i * 32 + e < begin) r[e] = 0xFF800000u;
+        }
+      };
+      float now = -INFINITY, other = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kTile; ++i)
-          if (i >= end || i < begin) r[i / 32][i % 32] = 0xFF800000u;
-      }
-      float top[4];
+      for (int i = 0; i < 2; ++i)
+        if (i < pieces) {
+          load(i);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        top[i] = __uint_as_float(r[i][0]);
-#pragma unroll
-        for (int e = 1; e < 32; ++e) top[i] = fmaxf(top[i], __uint_as_float(r[i][e]));
-      }
-      const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
-      const bool raise = now > m + kLag;          // from -inf on: at the first block with a key that is seen
-      if (__any_sync(0xFFFFFFFFu, raise)) {
+          for (int e = 0; e < 32; e += 4) {
+            now = max3(now, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
+            other = max3(other, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+          }
+        }
+      now = fmaxf(now, other) * c;
+      // from -inf on: at the first block with a key that is seen.  (A wait that ran out comes this way too, to end all warps.)
+      if (any_of_tile(t, now > m + kLag || !ok)) {
+        row_of[t][half][in_tile] = now;
+        if (!ok) failed[t] = 1;
+        tile_sync(t);
+        if (failed[t]) {
+          ok = false;
+          break;
+        }
+        now = fmaxf(now, row_of[t][half ^ 1][in_tile]);
+        const bool raise = now > m + kLag;
         const float f = raise ? ex2(m - now) : 1.0f;
         m = raise ? now : m;
         sum *= f;
-        if (j > lo) {                             // the products so far have this maximum's factor
+        if (j > lo && __any_sync(0xFFFFFFFFu, raise)) {      // the products so far have this maximum's factor
           ok = wait(&o_done[t], (j - 1 - lo) & 1);
           ptx::tc_fence_after_sync();
 #pragma unroll 1
-          for (int i = 0; i < DP; i += 32) {
+          for (int i = 0; i < DP / 2; i += 32) {
             uint32_t v[32];
             ptx::tmem_ld_32x32(to + i, v);
             ptx::tmem_ld_wait();
@@ -216,33 +290,47 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
           }
         }
       }
-      const float shift = m == -INFINITY ? 0.0f : m;
-      float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const float shift = m == -INFINITY ? 0.0f : -m;
+      const float2 c2 = make_float2(c, c), shift2 = make_float2(shift, shift);
+      float2 part = make_float2(0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        uint32_t p[32];
+        uint32_t p[16];
+        if (i < pieces) {
+          load(i);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float x = ex2(fmaf(__uint_as_float(r[2 * i + e / 16][2 * (e % 16)]), c, -shift));
-          const float y = ex2(fmaf(__uint_as_float(r[2 * i + e / 16][2 * (e % 16) + 1]), c, -shift));
-          part[2 * i] += x;
-          part[2 * i + 1] += y;
-          p[e] = rows::pack2(x, y);
+          for (int e = 0; e < 16; ++e) {
+            const float2 x = fma2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, shift2);
+            const float2 y = e % 8 == 7 ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
+            part = add2(part, y);
+            p[e] = rows::pack2(y.x, y.y);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = 0;
         }
-        tmem_st_32x32(ts + i * 32, p);
+        if (some) tmem_st_32x16(ts + i * 16, p);
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&p_ready[t]);
+      ptx::mbar_arrive(&p_ready[t][half]);
+      sum += part.x + part.y;
     }
-    if (ok && hi > lo) {
+    // (a warp whose wait ran out comes here as well: all of the tile's warps meet once more)
+    sum_of[t][half][in_tile] = sum;
+    if (!ok) failed[t] = 1;
+    tile_sync(t);
+    ok = ok && !failed[t];
+    if (ok && some && hi > lo) {
+      sum += sum_of[t][half ^ 1][in_tile];
       ok = wait(&o_done[t], (hi - 1 - lo) & 1);
       ptx::tc_fence_after_sync();
       const float inv = 1.0f / sum;
       uint16_t* o = a.o + (at.start + row) * a.ldo + (int64_t)head * s.D;
-#pragma unroll 1
-      for (int i = 0; i < s.D; i += 32) {
+#pragma unroll
+      for (int i = 0; i < DP / 2; i += 32) {
+        const int col = half * (DP / 2) + i;
+        if (col >= s.D) break;
         uint32_t v[32];
         ptx::tmem_ld_32x32(to + i, v);
         ptx::tmem_ld_wait();
@@ -252,19 +340,19 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             float f[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(v[e + x]) * inv;
-            if (i + e < s.D) *reinterpret_cast<uint4*>(o + i + e) = rows::pack8(f);
+            if (col + e < s.D) *reinterpret_cast<uint4*>(o + col + e) = rows::pack8(f);
           }
         }
       }
-      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (m + log2f(sum)) * kLn2;
+      if (ok && row < len && half == 0) a.lse[(int64_t)head * s.T + at.start + row] = (m + log2f(sum)) * kLn2;
     }
   }
   if (!ok && lane == 0) report_timeout(s);
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kProducts) {
     ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc(tmem, 512);
+    ptx::tmem_dealloc(tmem, L::kColumns);
   }
 }
 
@@ -281,7 +369,7 @@ int fwd_launch(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& 
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
-  cfg.blockDim = dim3(kFwdThreads, 1, 1);
+  cfg.blockDim = dim3(FwdLayout<DP>::kThreads, 1, 1);
   cfg.dynamicSmemBytes = FwdLayout<DP>::kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr;
@@ -385,7 +473,7 @@ extern "C" int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, i
   if (int rc = make_map(&mq, Operand{q16, ldq, (int)heads}, T, (int)D)) return rc;
   if (int rc = make_map(&mk, Operand{k16, ldk, (int)kv_heads}, T, (int)D)) return rc;
   if (int rc = make_map(&mv, Operand{v16, ldv, (int)kv_heads}, T, (int)D)) return rc;
-  const int64_t blocks = (T / (2 * kTile) + n_seq) * heads;
+  const int64_t blocks = (T / ((D <= 64 ? FwdLayout<64>::kTiles : FwdLayout<128>::kTiles) * kTile) + n_seq) * heads;
   return D <= 64 ? fwd_launch<64>(mq, mk, mv, a, blocks, (cudaStream_t)stream)
                  : fwd_launch<128>(mq, mk, mv, a, blocks, (cudaStream_t)stream);
 }

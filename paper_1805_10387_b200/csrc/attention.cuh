@@ -44,16 +44,20 @@ __device__ __forceinline__ int64_t offset_at(const Shape& s, int64_t b) {
 template <int ROWS>
 __device__ __forceinline__ Place place_of(const Shape& s, int64_t v) {
   const int lane = threadIdx.x & 31;
-  int64_t lo = 0, hi = s.n_seq;
-  while (hi - lo > 1) {
+  int64_t lo = 0, hi = s.n_seq, from = offset_at(s, 0), to = 0;
+  while (true) {
     const int64_t hop = (hi - lo + 31) / 32, b = lo + (lane + 1) * hop;
-    const bool before = b < hi && offset_at(s, b) / ROWS + b <= v;
-    const int n = __popc(__ballot_sync(0xFFFFFFFFu, before));
+    const int64_t x = b <= hi ? offset_at(s, b) : 0;         // (offset[n_seq] ends the last sequence)
+    const int n = __popc(__ballot_sync(0xFFFFFFFFu, b < hi && x / ROWS + b <= v));
+    if (n > 0) from = __shfl_sync(0xFFFFFFFFu, x, n - 1);
     const int64_t next = lo + (n + 1) * hop;
     lo += n * hop;
     hi = next < hi ? next : hi;
+    if (hop == 1) {                               // the next offset is the next lane's
+      to = __shfl_sync(0xFFFFFFFFu, x, n);
+      break;
+    }
   }
-  const int64_t from = offset_at(s, lo), to = offset_at(s, lo + 1);
   Place p{from, to - from, v - (from / ROWS + lo), 0};
   // an offset out of order or range gives no work (and is recorded by check_offsets)
   if (from >= 0 && to >= from && to <= s.T && p.tile >= 0) p.tiles = (p.len + ROWS - 1) / ROWS;
@@ -85,6 +89,23 @@ __device__ __forceinline__ float ex2(float x) {   // 2 units in the last place; 
   return y;
 }
 
+// Two FP32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)),
+        "l"(reinterpret_cast<const unsigned long long&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
+  return d;
+}
+
 // ---- copies: 3-D maps [token][head][element] ----
 __device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, uint64_t* bar, int col, int head, int row) {
   asm volatile(
@@ -113,14 +134,12 @@ __device__ __forceinline__ void clear_rows(uint8_t* tile, int valid) {
 }
 
 // ---- operands in shared memory: boxes of 128 rows of 128 bytes, 128-byte swizzle ----
-// Step ks of 16 along the columns (the tile's rows are the operand's M or N).
-__device__ __forceinline__ uint64_t desc_k(uint32_t tile, int ks) {
-  return ptx::smem_desc_sw128(tile + (ks >> 2) * kBoxBytes + (ks & 3) * 32, 16, 1024);
-}
-// Step ks of 16 along the rows (the tile's columns are the operand's N).
-__device__ __forceinline__ uint64_t desc_mn(uint32_t tile, int ks) {
-  return ptx::smem_desc_sw128(tile + ks * 2048, kBoxBytes, 1024);
-}
+// Along the columns (the tile's rows are the operand's M or N), and along the rows (its columns are the operand's N); step ks
+// of 16.  A descriptor is formed once for a tile; a step adds a constant to it, since its address is in units of 16 bytes.
+__device__ __forceinline__ uint64_t desc_k(uint32_t tile) { return ptx::smem_desc_sw128(tile, 16, 1024); }
+__device__ __forceinline__ uint64_t desc_mn(uint32_t tile) { return ptx::smem_desc_sw128(tile, kBoxBytes, 1024); }
+__host__ __device__ constexpr uint64_t step_k(int ks) { return (uint64_t)((ks >> 2) * kBoxBytes + (ks & 3) * 32) >> 4; }
+__host__ __device__ constexpr uint64_t step_mn(int ks) { return (uint64_t)(ks * 2048) >> 4; }
 
 // D[tmem] (+)= A[tmem] B[smem]; A: FP16 pairs in 32-bit columns, 8 columns a step of 16.
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
@@ -133,6 +152,24 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
       : "memory");
 }
 
+// Column of the step ks of 16 of a 128-column operand that two warps wrote: each half's 32 packed columns lie at its own start.
+__host__ __device__ constexpr uint32_t packed_at(int ks) { return (ks >> 2) * 64 + (ks & 3) * 8; }
+// A product of two tiles: D (+)= sum over `steps` of 16, at most STEPS.  By one thread; unrolled, so that what an instruction
+// needs is at hand when the tensor core is free: a loop that formed descriptors issued one in 130 cycles, and a step takes 64.
+template <int STEPS>
+__device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, int steps) {
+#pragma unroll
+  for (int k = 0; k < STEPS; ++k)
+    if (k < steps) ptx::mma_f16_ss(d, a + step_k(k), b + step_k(k), idesc, k > 0);
+}
+// Steps FROM .. TO - 1 of A in tensor memory and the rows of a tile.
+template <int FROM, int TO>
+__device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, int steps, bool accumulate) {
+#pragma unroll
+  for (int k = FROM; k < TO; ++k)
+    if (k < steps) mma_f16_ts(d, a + packed_at(k), b + step_mn(k), idesc, accumulate || k > 0);
+}
+
 // 32 lanes x 32 consecutive 32-bit columns from registers.
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
@@ -143,6 +180,14 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r
       "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
       "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
       "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }

@@ -126,9 +126,6 @@ __device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&a)[32], uint32
   ptx::tmem_ld_32x32(taddr + 32, b);
   ptx::tmem_ld_wait();
 }
-// Column of the step ks of 16 of a 128-column operand that two warps wrote: each half's 32 packed columns lie at its own start.
-__device__ __forceinline__ uint32_t packed_at(int ks) { return (ks >> 2) * 64 + (ks & 3) * 8; }
-
 // Rows `row` of a tile from tensor memory, times f, to the columns of a head.
 template <int COLS>
 __device__ __forceinline__ void store_rows(uint32_t taddr, float f, uint16_t* out, bool on, int col0, int D) {
@@ -221,17 +218,16 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
     const uint32_t sk = ptx::smem_u32(smem), sv = sk + L::kTileBytes;
     auto tile = [&](int x) { return ptx::smem_u32(ring + x % L::kStages * 2 * L::kTileBytes); };
     auto scores = [&](int x) {
-      for (int k = 0; k < ksteps; ++k) ptx::mma_f16_ss(tmem + kS, desc_k(sk, k), desc_k(tile(x), k), idesc_s, k > 0);
+      product_ss<DP / 16>(tmem + kS, desc_k(sk), desc_k(tile(x)), idesc_s, ksteps);
       ptx::mma_commit(&b.s_full[0]);
     };
     auto dprob = [&](int x) {
-      for (int k = 0; k < ksteps; ++k)
-        ptx::mma_f16_ss(tmem + kDP, desc_k(sv, k), desc_k(tile(x) + L::kTileBytes, k), idesc_s, k > 0);
+      product_ss<DP / 16>(tmem + kDP, desc_k(sv), desc_k(tile(x) + L::kTileBytes), idesc_s, ksteps);
       ptx::mma_commit(&b.dp_full);
     };
     ok = wait(&b.fixed_full, 0) && wait(&b.full[0], 0);
     ptx::tc_fence_after_sync();
-    if (ok && lane == 0) {
+    if (ok && ptx::elect_one()) {
       scores(0);
       dprob(0);
     }
@@ -241,18 +237,16 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
       if (ok && x + 1 < n) ok = wait(&b.full[(x + 1) % L::kStages], (x + 1) / L::kStages & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      if (lane == 0) {
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_f16_ts(tmem + kDV, tmem + kS + packed_at(k), desc_mn(tile(x) + L::kTileBytes, k), idesc_o, x > 0 || k > 0);
+      if (ptx::elect_one()) {
+        product_ts<0, 8>(tmem + kDV, tmem + kS, desc_mn(tile(x) + L::kTileBytes), idesc_o, 8, x > 0);
         if (x + 1 < n) scores(x + 1);             // in the place of that P
       }
       __syncwarp();
       ok = wait(&b.ds_ready, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      if (lane == 0) {
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_f16_ts(tmem + kDK, tmem + kDP + packed_at(k), desc_mn(tile(x), k), idesc_o, x > 0 || k > 0);
+      if (ptx::elect_one()) {
+        product_ts<0, 8>(tmem + kDK, tmem + kDP, desc_mn(tile(x)), idesc_o, 8, x > 0);
         ptx::mma_commit(&b.empty[x % L::kStages]);
         if (x + 1 < n) dprob(x + 1);
         else ptx::mma_commit(&b.done);
@@ -387,18 +381,16 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
     const uint32_t sq = ptx::smem_u32(smem), sdo = sq + L::kTileBytes;
     auto keys = [&](int x) { return ptx::smem_u32(ring + x % L::kStages * 2 * L::kTileBytes); };
     auto scores = [&](int x) {
-      for (int k = 0; k < ksteps; ++k)
-        ptx::mma_f16_ss(tmem + kS + (x & 1) * kTile, desc_k(sq, k), desc_k(keys(x), k), idesc_s, k > 0);
+      product_ss<DP / 16>(tmem + kS + (x & 1) * kTile, desc_k(sq), desc_k(keys(x)), idesc_s, ksteps);
       ptx::mma_commit(&b.s_full[x & 1]);
     };
     auto dprob = [&](int x) {
-      for (int k = 0; k < ksteps; ++k)
-        ptx::mma_f16_ss(tmem + kDP, desc_k(sdo, k), desc_k(keys(x) + L::kTileBytes, k), idesc_s, k > 0);
+      product_ss<DP / 16>(tmem + kDP, desc_k(sdo), desc_k(keys(x) + L::kTileBytes), idesc_s, ksteps);
       ptx::mma_commit(&b.dp_full);
     };
     ok = wait(&b.fixed_full, 0) && wait(&b.full[0], 0);
     ptx::tc_fence_after_sync();
-    if (ok && lane == 0) {
+    if (ok && ptx::elect_one()) {
       scores(0);
       dprob(0);
     }
@@ -408,15 +400,14 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
         ok = wait(&b.full[(x + 1) % L::kStages], (x + 1) / L::kStages & 1) && wait(&b.s_free[(x + 1) & 1], ((x + 1) / 2 & 1) ^ 1);
         if (!ok) break;
         ptx::tc_fence_after_sync();
-        if (lane == 0) scores(x + 1);
+        if (ptx::elect_one()) scores(x + 1);
         __syncwarp();
       }
       ok = wait(&b.ds_ready, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      if (lane == 0) {
-        for (int k = 0; k < kTile / 16; ++k)
-          mma_f16_ts(tmem + kDQ, tmem + kDP + packed_at(k), desc_mn(keys(x), k), idesc_o, x > 0 || k > 0);
+      if (ptx::elect_one()) {
+        product_ts<0, 8>(tmem + kDQ, tmem + kDP, desc_mn(keys(x)), idesc_o, 8, x > 0);
         ptx::mma_commit(&b.empty[x % L::kStages]);
         if (x + 1 < n) dprob(x + 1);
         else ptx::mma_commit(&b.done);
