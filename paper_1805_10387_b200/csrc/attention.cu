@@ -1,11 +1,13 @@
 // Attention over packed sequences, forward: O = softmax(scale Q K^T) V for each head, with the rows' log-sums.
 //
-// One pass over the keys with a running maximum and sum.  A block has two tiles of 128 queries of a head, whose two
-// products S = Q K^T and O += P V alternate on the tensor core: while one tile's scores go through the exponential, the
-// other's products run.  S and O stay in tensor memory, P takes the place of its S there as FP16 (rounded once, 2^-12 of
-// the value; the sum is taken from the unrounded FP32 values), keys and values pass through a ring in shared memory.
+// One pass over the keys with a running maximum and sum.  A tile of 128 queries meets 64 keys at a time: S = Q K^T (64 columns of
+// tensor memory), the exponentials, O += P V with P in the place of its S as FP16 (rounded once, 2^-12 of the value; the
+// sum is taken from the unrounded FP32 values).  There are two places for S, so the tensor core forms the next scores while
+// these go through the exponential, and what a tile waits for is the special-function unit: 16 results a clock and SM, as long as
+// the products of a head of 128 elements take.  Scores of 128 keys at a time, whose next ones could not be formed before this
+// P was used up, took 1.6 times as long.  Keys and values pass through a ring in shared memory.
 // The running maximum may lag: it is raised, and O multiplied, only where a row's maximum has passed it by 2^8, so that
-// almost no tile pays for it; P stays below 2^8 and its FP16 rounding is relative.
+// almost no step pays for it; P stays below 2^8 and its FP16 rounding is relative.
 
 #include <math.h>
 
@@ -31,12 +33,15 @@ struct FwdArgs {
 template <int DP>
 struct FwdLayout {
   static constexpr int kTiles = DP == 64 ? 1 : 2, kBlocks = DP == 64 ? 2 : 1;      // tiles a block, blocks an SM
-  static constexpr int kThreads = kTiles * 256 + 64;         // eight warps a tile, half a row a thread; then products; copies
+  // Four warps a tile, a row a thread; then one a tile that issues its products (with one for both, the tensor core waited while
+  // that warp waited for the other tile, four tenths of the time); then one for the copies.
+  static constexpr int kThreads = kTiles * 160 + 32;
   static constexpr int kBoxes = DP / 64, kTileBytes = kBoxes * kBoxBytes;
   static constexpr int kStages = DP == 64 ? 5 : 4;
   static constexpr int kSmem = (kTiles + kStages) * kTileBytes + 1024;
   static constexpr int kColumns = DP == 64 ? 256 : 512;      // of tensor memory: S, with P in its place, then O, for each tile
 };
+constexpr int kStep = 64;                         // keys that a tile meets at once
 constexpr float kLag = 8.0f;
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -44,51 +49,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// 2^x for two values on the multiply-add pipe: whole and fractional part split by rounding, a polynomial of the fraction on
-// [-1/2, 1/2] (least largest relative error, 2.6e-6; fitted to 2^f by weighted least squares), the whole part added to the exponent.
-__device__ __forceinline__ float2 ex2_poly(float2 x) {
-  const float2 magic = make_float2(12582912.0f, 12582912.0f);            // 1.5 * 2^23: the sum's low bits are the whole part
-  x = make_float2(fmaxf(x.x, -126.0f), fmaxf(x.y, -126.0f));
-  const float2 t = add2(x, magic), whole = add2(t, make_float2(-12582912.0f, -12582912.0f));
-  const float2 f = fma2(whole, make_float2(-1.0f, -1.0f), x);
-  float2 p = make_float2(0.009570101276040077f, 0.009570101276040077f);
-  p = fma2(p, f, make_float2(0.05591785907745361f, 0.05591785907745361f));
-  p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
-  p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-  p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
-}
-
-// Among the 256 threads of tile t: a barrier, and whether anyone says yes; a barrier alone.
-__device__ __forceinline__ bool any_of_tile(int t, bool yes) {
-  uint32_t any;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, %2, 256, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"((uint32_t)yes), "r"(1 + t)
-      : "memory");
-  return any != 0;
-}
-__device__ __forceinline__ void tile_sync(int t) { asm volatile("barrier.cta.sync %0, 256;" ::"r"(1 + t) : "memory"); }
-
 template <int DP>
 __global__ void __launch_bounds__(FwdLayout<DP>::kThreads, FwdLayout<DP>::kBlocks)
 mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                         const __grid_constant__ CUtensorMap mv, const FwdArgs a) {
   using L = FwdLayout<DP>;
-  constexpr int kTiles = L::kTiles, kProducts = kTiles * 8, kCopies = kProducts + 1;      // these two warps' numbers
+  constexpr int kTiles = L::kTiles, kProducts = kTiles * 4, kCopies = kProducts + kTiles;     // these warps' numbers
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* ring = smem + kTiles * L::kTileBytes;
-  // p_ready: the first and the second 64 columns of P; row_of, sum_of: what the threads of a row tell one another
-  __shared__ uint64_t q_full, kv_full[L::kStages], kv_empty[L::kStages], tail_full, s_full[kTiles], p_ready[kTiles][2], o_done[kTiles];
-  __shared__ float row_of[kTiles][2][kTile], sum_of[kTiles][2][kTile];
+  // of each place for S apart: a waiter is then never two phases from a barrier
+  __shared__ uint64_t q_full, kv_full[L::kStages], kv_empty[L::kStages], tail_full, s_full[kTiles][2], p_ready[kTiles][2], o_done[kTiles][2];
   __shared__ uint32_t s_tmem;
-  __shared__ volatile int failed[kTiles];
   const Shape& s = a.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   ptx::launch_dependents();
@@ -102,14 +74,14 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     ptx::mbar_init(&tail_full, 1);
     for (int i = 0; i < L::kStages; ++i) {
       ptx::mbar_init(&kv_full[i], 1);
-      ptx::mbar_init(&kv_empty[i], 1);
+      ptx::mbar_init(&kv_empty[i], kTiles);
     }
     for (int t = 0; t < kTiles; ++t) {
-      ptx::mbar_init(&s_full[t], 1);
-      ptx::mbar_init(&p_ready[t][0], kTile);
-      ptx::mbar_init(&p_ready[t][1], kTile);
-      ptx::mbar_init(&o_done[t], 1);
-      failed[t] = 0;
+      for (int i = 0; i < 2; ++i) {
+        ptx::mbar_init(&s_full[t][i], 1);
+        ptx::mbar_init(&p_ready[t][i], 4);            // warps
+        ptx::mbar_init(&o_done[t][i], 1);
+      }
     }
     ptx::fence_mbar_init();
   }
@@ -124,15 +96,15 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   constexpr uint32_t kO = kTiles * kTile;
   // the long ones first: a causal query sees all keys before it
   const int q0 = (int)(at.tiles - 1 - at.tile) * kTiles * kTile, len = (int)at.len;
-  // key blocks that a tile of queries sees
-  int b0[kTiles], b1[kTiles];
+  // the steps of kStep keys that a tile of queries sees
+  int u0[kTiles], u1[kTiles];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
     const int first = q0 + t * kTile, last = min(first + kTile, len);     // queries
-    b0[t] = s.window > 0 && first + 1 > s.window ? (int)(first + 1 - s.window) / kTile : 0;
-    b1[t] = first >= len ? b0[t] : ((s.causal ? last : len) + kTile - 1) / kTile;
+    u0[t] = s.window > 0 && first + 1 > s.window ? (int)(first + 1 - s.window) / kStep : 0;
+    u1[t] = first >= len ? u0[t] : ((s.causal ? last : len) + kStep - 1) / kStep;
   }
-  const int j0 = b0[0], j1 = max(b1[0], b1[kTiles - 1]);
+  const int from = u0[0], to = max(u1[0], u1[kTiles - 1]), j0 = from / 2, j1 = (to + 1) / 2;      // steps, and blocks of 128 keys
   bool ok = true;
 
   if (warp == kCopies) {
@@ -167,172 +139,150 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     // no copy is in flight into a block that has ended
     wait(&q_full, 0);
     for (int i = max(0, n - L::kStages); i < n; ++i) wait(&kv_full[i % L::kStages], i / L::kStages & 1);
-  } else if (warp == kProducts) {
+  } else if (warp >= kProducts) {
+    const int t = warp - kProducts, lo = t ? u0[kTiles - 1] : u0[0], hi = t ? u1[kTiles - 1] : u1[0];
     const int ksteps = (s.D + 15) / 16;
     const uint32_t idesc_o = ptx::idesc_f16_f32(kTile, ksteps * 16, false, true);
+    const uint32_t d_s = tmem + t * kTile, d_o = tmem + kO + t * DP;
+    const uint64_t dq = desc_k(ptx::smem_u32(smem + t * L::kTileBytes));
     ok = wait(&q_full, 0);
-    for (int j = j0; j <= j1 && ok; ++j) {
-      const int nk = 2 * (j - j0), nv = nk - 1;   // their places in the order of copies
-      if (j < j1) ok = wait(&kv_full[nk % L::kStages], nk / L::kStages & 1);
-      if (ok && j > j0) ok = wait(&kv_full[nv % L::kStages], nv / L::kStages & 1);
-      const uint32_t sk = ptx::smem_u32(ring + nk % L::kStages * L::kTileBytes);
-      const uint32_t sv = ptx::smem_u32(ring + (nv < 0 ? 0 : nv % L::kStages) * L::kTileBytes);
-      // the last block of a sequence is as wide as it has keys
-      const int before = (min(kTile, len - (j - 1) * kTile) + 15) / 16, wide = (min(kTile, len - j * kTile) + 15) / 16 * 16;
-#pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        if (ok && j > b0[t] && j <= b1[t]) {      // O += P V of the block before, in two halves
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            ok = ok && wait(&p_ready[t][h], (j - 1 - b0[t]) & 1);
-            ptx::tc_fence_after_sync();
-            if (ok && ptx::elect_one()) {
-              if (h == 0) {
-                product_ts<0, 4>(tmem + kO + t * DP, tmem + t * kTile, desc_mn(sv), idesc_o, before, j - 1 > b0[t]);
-              } else {
-                product_ts<4, 8>(tmem + kO + t * DP, tmem + t * kTile, desc_mn(sv), idesc_o, before, true);
-                ptx::mma_commit(&o_done[t]);
-              }
-            }
-            __syncwarp();
-          }
+    // Step u: O += P V of step u - 2, and S of step u in the place of that P.  A block of keys or values has two steps; the warp
+    // lets go of those that only the other tile sees as well.
+    for (int u = from; u < to + 2 && ok; ++u) {
+      const int nk = 2 * ((u >> 1) - j0), nv = 2 * ((u - 2 >> 1) - j0) + 1;      // places in the order of copies
+      const bool scores = u < to, values = u - 2 >= from;
+      if (scores && (u == from || !(u & 1))) ok = wait(&kv_full[nk % L::kStages], nk / L::kStages & 1);
+      if (ok && values && (u - 2 == from || !(u & 1))) ok = wait(&kv_full[nv % L::kStages], nv / L::kStages & 1);
+      const int v = u - 2 - lo, place = (u - lo) & 1;
+      if (ok && v >= 0 && u - 2 < hi) {
+        ok = wait(&p_ready[t][place], v >> 1 & 1);
+        ptx::tc_fence_after_sync();
+        if (ok && ptx::elect_one()) {
+          // the last step of a sequence is as wide as it has keys
+          const int steps = (min(kStep, len - (u - 2) * kStep) + 15) / 16;
+          const uint64_t dv = desc_mn(ptx::smem_u32(ring + nv % L::kStages * L::kTileBytes) + (u & 1) * kStep * 128);
+          product_ts<0, kStep / 16>(d_o, d_s + place * kStep, dv, idesc_o, steps, v > 0);
+          ptx::mma_commit(&o_done[t][place]);
         }
-        if (ok && j >= b0[t] && j < b1[t]) {      // S of this one, in the place of that P
-          ptx::tc_fence_after_sync();
-          if (ptx::elect_one()) {
-            product_ss<DP / 16>(tmem + t * kTile, desc_k(ptx::smem_u32(smem + t * L::kTileBytes)), desc_k(sk),
-                                ptx::idesc_f16_f32(kTile, wide, false, false), ksteps);
-            ptx::mma_commit(&s_full[t]);
-          }
-          __syncwarp();
+        __syncwarp();
+      }
+      if (ok && u >= lo && u < hi) {
+        ptx::tc_fence_after_sync();
+        if (ptx::elect_one()) {
+          const int wide = (min(kStep, len - u * kStep) + 15) / 16 * 16;
+          const uint64_t dk = desc_k(ptx::smem_u32(ring + nk % L::kStages * L::kTileBytes) + (u & 1) * kStep * 128);
+          product_ss<DP / 16>(d_s + place * kStep, dq, dk, ptx::idesc_f16_f32(kTile, wide, false, false), ksteps);
+          ptx::mma_commit(&s_full[t][place]);
         }
+        __syncwarp();
       }
       if (ok && ptx::elect_one()) {
-        if (j > j0) ptx::mma_commit(&kv_empty[nv % L::kStages]);
-        if (j < j1) ptx::mma_commit(&kv_empty[nk % L::kStages]);
+        if (values && ((u & 1) || u - 1 == to)) ptx::mma_commit(&kv_empty[nv % L::kStages]);
+        if (scores && ((u & 1) || u + 1 == to)) ptx::mma_commit(&kv_empty[nk % L::kStages]);
       }
       __syncwarp();
     }
   } else {
-    // Two threads have a row, 64 columns each: a tile's scores pass through twice as many warps in half the time, and it is this
-    // time that the products of the tile wait for.
-    const int t = warp >> 3, half = warp >> 2 & 1, in_tile = (warp & 3) * 32 + lane, row = q0 + t * kTile + in_tile;   // of the sequence
+    const int t = warp >> 2, row = q0 + t * kTile + (warp & 3) * 32 + lane;      // of the sequence
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + t * kTile + half * 64 + lanes, to = tmem + kO + t * DP + half * (DP / 2) + lanes;
-    const int lo = t ? b0[kTiles - 1] : b0[0], hi = t ? b1[kTiles - 1] : b1[0];
+    const uint32_t ts = tmem + t * kTile + lanes, to_o = tmem + kO + t * DP + lanes;
+    const int lo = t ? u0[kTiles - 1] : u0[0], hi = t ? u1[kTiles - 1] : u1[0];
     const float c = s.scale_log2;
     const bool some = row - lane < len;           // the warp has rows that exist
     // the keys that this query sees
     const int key1 = s.causal ? min(row + 1, len) : len;
     const int key0 = s.window > 0 && row + 1 > s.window ? (int)(row + 1 - s.window) : 0;
-    // blocks between these two are seen whole by every query of the warp; no query of it sees a key from `end` on
+    // steps between these two are seen whole by every query of the warp; no query of it sees a key from `end` on
     const int first = row - lane;
     const int whole1 = s.causal ? min(first + 1, len) : len, end = s.causal ? min(first + 32, len) : len;
     const int whole0 = s.window > 0 && first + 32 > s.window ? (int)(first + 32 - s.window) : 0;
     float m = -INFINITY, sum = 0.0f;
-    for (int j = lo; j < hi; ++j) {
-      ok = ok && wait(&s_full[t], (j - lo) & 1);
+    for (int u = lo; u < hi && ok; ++u) {
+      const int n = u - lo, k0 = u * kStep;
+      const uint32_t at_s = ts + (n & 1) * kStep;
+      ok = wait(&s_full[t][n & 1], n >> 1 & 1);
+      if (!ok) break;
+      if (!some) {                                // rows of what comes behind the sequence: whatever P holds stays in them
+        arrive(&p_ready[t][n & 1]);
+        continue;
+      }
       ptx::tc_fence_after_sync();
-      const int k0 = j * kTile + half * 64;       // this thread's first key
-      // pieces of 32 columns with keys that are seen (rows of what comes behind the sequence: whatever P holds stays in them)
-      const int pieces = !ok || !some ? 0 : max(0, min(2, (end - k0 + 31) / 32));
-      const bool edge = k0 + 64 > whole1 || k0 < whole0;
-      const int stop = key1 - k0, begin = key0 - k0;
-      // The scores are read twice, for the maximum and for the weights: in registers all the while they would not leave room
-      // for enough warps.
-      uint32_t r[32];
-      auto load = [&](int i) {
-        ptx::tmem_ld_32x32(ts + i * 32, r);
-        ptx::tmem_ld_wait();
-        if (edge) {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (i * 32 + e >= stop || i * 32 + e < begin) r[e] = 0xFF800000u;
-        }
-      };
-      float now = -INFINITY, other = -INFINITY;
+      // pieces of 32 columns with keys that are seen
+      const int pieces = max(0, min(2, (end - k0 + 31) / 32));
+      uint32_t r[2][32];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        if (i < pieces) {
-          load(i);
+        if (i < pieces) ptx::tmem_ld_32x32(at_s + i * 32, r[i]);
+      ptx::tmem_ld_wait();
+      if (k0 + kStep > whole1 || k0 < whole0) {
+        const int stop = key1 - k0, begin = key0 - k0;
+#pragma unroll
+        for (int e = 0; e < kStep; ++e)
+          if (e >= stop || e < begin) r[e / 32][e % 32] = 0xFF800000u;
+      }
+      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (i < pieces)
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
-            now = max3(now, __uint_as_float(r[e]), __uint_as_float(r[e + 1]));
-            other = max3(other, __uint_as_float(r[e + 2]), __uint_as_float(r[e + 3]));
+            top[2 * i] = max3(top[2 * i], __uint_as_float(r[i][e]), __uint_as_float(r[i][e + 1]));
+            top[2 * i + 1] = max3(top[2 * i + 1], __uint_as_float(r[i][e + 2]), __uint_as_float(r[i][e + 3]));
           }
-        }
-      now = fmaxf(now, other) * c;
-      // from -inf on: at the first block with a key that is seen.  (A wait that ran out comes this way too, to end all warps.)
-      if (any_of_tile(t, now > m + kLag || !ok)) {
-        row_of[t][half][in_tile] = now;
-        if (!ok) failed[t] = 1;
-        tile_sync(t);
-        if (failed[t]) {
-          ok = false;
-          break;
-        }
-        now = fmaxf(now, row_of[t][half ^ 1][in_tile]);
-        const bool raise = now > m + kLag;
+      const float now = max3(fmaxf(top[0], top[1]), top[2], top[3]) * c;
+      const bool raise = now > m + kLag;          // from -inf on: at the first step with a key that is seen
+      if (__any_sync(0xFFFFFFFFu, raise)) {
         const float f = raise ? ex2(m - now) : 1.0f;
         m = raise ? now : m;
         sum *= f;
-        if (j > lo && __any_sync(0xFFFFFFFFu, raise)) {      // the products so far have this maximum's factor
-          ok = wait(&o_done[t], (j - 1 - lo) & 1);
+        if (n > 0) {                              // the products so far have this maximum's factor
+          ok = wait(&o_done[t][(n - 1) & 1], n - 1 >> 1 & 1);
           ptx::tc_fence_after_sync();
 #pragma unroll 1
-          for (int i = 0; i < DP / 2; i += 32) {
+          for (int i = 0; i < DP; i += 32) {
             uint32_t v[32];
-            ptx::tmem_ld_32x32(to + i, v);
+            ptx::tmem_ld_32x32(to_o + i, v);
             ptx::tmem_ld_wait();
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-            tmem_st_32x32(to + i, v);
+            tmem_st_32x32(to_o + i, v);
           }
         }
       }
       const float shift = m == -INFINITY ? 0.0f : -m;
       const float2 c2 = make_float2(c, c), shift2 = make_float2(shift, shift);
-      float2 part = make_float2(0.0f, 0.0f);
+      float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         uint32_t p[16];
         if (i < pieces) {
-          load(i);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float2 x = fma2(make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])), c2, shift2);
-            const float2 y = e % 8 == 7 ? ex2_poly(x) : make_float2(ex2(x.x), ex2(x.y));
-            part = add2(part, y);
+            const float2 x = fma2(make_float2(__uint_as_float(r[i][2 * e]), __uint_as_float(r[i][2 * e + 1])), c2, shift2);
+            const float2 y = make_float2(ex2(x.x), ex2(x.y));
+            part[e & 1] = add2(part[e & 1], y);
             p[e] = rows::pack2(y.x, y.y);
           }
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) p[e] = 0;
         }
-        if (some) tmem_st_32x16(ts + i * 16, p);
+        tmem_st_32x16(at_s + i * 16, p);
       }
       tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&p_ready[t][half]);
-      sum += part.x + part.y;
+      arrive(&p_ready[t][n & 1]);
+      sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
     }
-    // (a warp whose wait ran out comes here as well: all of the tile's warps meet once more)
-    sum_of[t][half][in_tile] = sum;
-    if (!ok) failed[t] = 1;
-    tile_sync(t);
-    ok = ok && !failed[t];
     if (ok && some && hi > lo) {
-      sum += sum_of[t][half ^ 1][in_tile];
-      ok = wait(&o_done[t], (hi - 1 - lo) & 1);
+      ok = wait(&o_done[t][(hi - 1 - lo) & 1], hi - 1 - lo >> 1 & 1);
       ptx::tc_fence_after_sync();
       const float inv = 1.0f / sum;
       uint16_t* o = a.o + (at.start + row) * a.ldo + (int64_t)head * s.D;
-#pragma unroll
-      for (int i = 0; i < DP / 2; i += 32) {
-        const int col = half * (DP / 2) + i;
-        if (col >= s.D) break;
+#pragma unroll 1
+      for (int i = 0; i < s.D; i += 32) {
         uint32_t v[32];
-        ptx::tmem_ld_32x32(to + i, v);
+        ptx::tmem_ld_32x32(to_o + i, v);
         ptx::tmem_ld_wait();
         if (ok && row < len) {
 #pragma unroll
@@ -340,11 +290,11 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
             float f[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) f[x] = __uint_as_float(v[e + x]) * inv;
-            if (col + e < s.D) *reinterpret_cast<uint4*>(o + col + e) = rows::pack8(f);
+            if (i + e < s.D) *reinterpret_cast<uint4*>(o + i + e) = rows::pack8(f);
           }
         }
       }
-      if (ok && row < len && half == 0) a.lse[(int64_t)head * s.T + at.start + row] = (m + log2f(sum)) * kLn2;
+      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (m + log2f(sum)) * kLn2;
     }
   }
   if (!ok && lane == 0) report_timeout(s);

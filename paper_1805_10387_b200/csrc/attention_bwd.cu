@@ -209,7 +209,7 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
         dst[e + lane] = on ? fmaf(a.lse[base + q], kLog2e, -kUp) : INFINITY;
         dst[kTile + e + lane] = on ? a.delta[base + q] * f : 0.0f;
       }
-      ptx::mbar_arrive(&b.stat_full[stage]);
+      arrive(&b.stat_full[stage]);
     }
   } else if (warp == 8) {
     const int ksteps = (s.D + 15) / 16;
@@ -291,7 +291,7 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
       pack_store(ts, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&b.p_ready);
+      arrive(&b.p_ready);
       ok = wait(&b.dp_full, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
@@ -314,8 +314,8 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
       pack_store(td, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&b.ds_ready);
-      ptx::mbar_arrive(&b.stat_empty[stage]);
+      arrive(&b.ds_ready);
+      arrive(&b.stat_empty[stage]);
     }
     if (ok) ok = wait(&b.done, 0);
     if (ok) {
@@ -433,7 +433,7 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
       uint32_t r0[32], r1[32];
       load64(tmem + kS + (x & 1) * kTile + lanes + half * 64, r0, r1);
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&b.s_free[x & 1]);
+      arrive(&b.s_free[x & 1]);
       const int k0 = (j0 + x) * kTile;
       const bool edge = k0 + kTile > whole1 || k0 < whole0;
       const int end = key1 - k0 - half * 64, begin = key0 - k0 - half * 64;
@@ -456,7 +456,7 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
       pack_store(td, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
-      ptx::mbar_arrive(&b.ds_ready);
+      arrive(&b.ds_ready);
     }
     if (ok) ok = wait(&b.done, 0);
     if (ok) {
@@ -492,16 +492,16 @@ mp_attention_bwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     for (int i = 0; i < L::kStages; ++i) {
       ptx::mbar_init(&b.full[i], 1);
       ptx::mbar_init(&b.empty[i], 1);
-      ptx::mbar_init(&b.stat_full[i], 32);
-      ptx::mbar_init(&b.stat_empty[i], 256);
+      ptx::mbar_init(&b.stat_full[i], 1);
+      ptx::mbar_init(&b.stat_empty[i], 8);          // warps, as below
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(&b.s_full[i], 1);
-      ptx::mbar_init(&b.s_free[i], 256);
+      ptx::mbar_init(&b.s_free[i], 8);
     }
     ptx::mbar_init(&b.dp_full, 1);
-    ptx::mbar_init(&b.p_ready, 256);
-    ptx::mbar_init(&b.ds_ready, 256);
+    ptx::mbar_init(&b.p_ready, 8);
+    ptx::mbar_init(&b.ds_ready, 8);
     ptx::mbar_init(&b.done, 1);
     ptx::fence_mbar_init();
   }
