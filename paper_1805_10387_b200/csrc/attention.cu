@@ -161,7 +161,7 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
           // the last step of a sequence is as wide as it has keys
           const int steps = (min(kStep, len - (u - 2) * kStep) + 15) / 16;
           const uint64_t dv = desc_mn(ptx::smem_u32(ring + nv % L::kStages * L::kTileBytes) + (u & 1) * kStep * 128);
-          product_ts<0, kStep / 16>(d_o, d_s + place * kStep, dv, idesc_o, steps, v > 0);
+          product_ts<kStep / 16, false>(d_o, d_s + place * kStep, dv, idesc_o, steps, v > 0);
           ptx::mma_commit(&o_done[t][place]);
         }
         __syncwarp();

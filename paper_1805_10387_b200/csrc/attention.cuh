@@ -111,6 +111,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
+  return d;
+}
+
 // ---- copies: 3-D maps [token][head][element] ----
 __device__ __forceinline__ void load_box(void* dst, const CUtensorMap* map, uint64_t* bar, int col, int head, int row) {
   asm volatile(
@@ -157,8 +165,6 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
       : "memory");
 }
 
-// Column of the step ks of 16 of a 128-column operand that two warps wrote: each half's 32 packed columns lie at its own start.
-__host__ __device__ constexpr uint32_t packed_at(int ks) { return (ks >> 2) * 64 + (ks & 3) * 8; }
 // A product of two tiles: D (+)= sum over `steps` of 16, at most STEPS.  By one thread; unrolled, so that what an instruction
 // needs is at hand when the tensor core is free: a loop that formed descriptors issued one in 130 cycles, and a step takes 64.
 template <int STEPS>
@@ -167,12 +173,13 @@ __device__ __forceinline__ void product_ss(uint32_t d, uint64_t a, uint64_t b, u
   for (int k = 0; k < STEPS; ++k)
     if (k < steps) ptx::mma_f16_ss(d, a + step_k(k), b + step_k(k), idesc, k > 0);
 }
-// Steps FROM .. TO - 1 of A in tensor memory and the rows of a tile.
-template <int FROM, int TO>
+// The same with A in tensor memory, along the rows of a tile.  QUARTERS: each 32 columns were written in the place of their
+// scores by a warp of their own, so their 16 packed columns begin where the scores did; else all follow one another.
+template <int STEPS, bool QUARTERS>
 __device__ __forceinline__ void product_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, int steps, bool accumulate) {
 #pragma unroll
-  for (int k = FROM; k < TO; ++k)
-    if (k < steps) mma_f16_ts(d, a + packed_at(k), b + step_mn(k), idesc, accumulate || k > 0);
+  for (int k = 0; k < STEPS; ++k)
+    if (k < steps) mma_f16_ts(d, a + (QUARTERS ? (k >> 1) * 32 + (k & 1) * 8 : 8 * k), b + step_mn(k), idesc, accumulate || k > 0);
 }
 
 // 32 lanes x 32 consecutive 32-bit columns from registers.

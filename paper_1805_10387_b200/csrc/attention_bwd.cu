@@ -99,133 +99,172 @@ __device__ __forceinline__ float ds_exponent(const BwdArgs& a, int kv) {
   return 15.0f - ceilf(log2f(bound) + 0.01f);
 }
 
+// Shared memory: two tiles that stay, rings of the tiles that pass (A: queries, or keys; B: gradients, or values), the queries'
+// statistics, the barriers.  Nothing is declared apart, so that seven tiles of a head of 128 elements fit: a third place
+// for A is what lets the next scores be formed while these are worked on.
 template <int DP>
 struct BwdLayout {
   static constexpr int kBoxes = DP / 64, kTileBytes = kBoxes * kBoxBytes;
-  static constexpr int kStages = DP == 64 ? 4 : 2;           // of two tiles each
-  static constexpr int kSmem = (2 + 2 * kStages) * kTileBytes + kStages * 2 * kTile * 4 + 1024;
+  static constexpr int kA = DP == 64 ? 4 : 3, kB = DP == 64 ? 4 : 2, kStats = 2;
+  static constexpr int kStatBytes = 2 * kTile * 4, kBarBytes = 512;
+  static constexpr int kSmem = (2 + kA + kB) * kTileBytes + kStats * kStatBytes + kBarBytes;
 };
-constexpr int kBwdThreads = 352;                  // warps 0-7: a row and half of the columns a thread; 8: products; 9: copies; 10: row statistics
+static_assert(BwdLayout<128>::kSmem <= 232448, "of a block");
+// Sixteen warps that compute (four a quarter of the columns, a row a thread), then one each for products, copies, row statistics.
+constexpr int kCompute = 16, kProducts = 16, kCopies = 17, kStatistics = 18, kBwdThreads = 19 * 32;
 
-template <int STAGES>
 struct BwdBars {
-  uint64_t fixed_full, full[STAGES], empty[STAGES], tail_full, stat_full[STAGES], stat_empty[STAGES];
+  uint64_t fixed_full, full_a[4], empty_a[4], full_b[4], empty_b[4], tail_full, stat_full[2], stat_empty[2];
   uint64_t s_full[2], s_free[2], dp_full, p_ready, ds_ready, done;
   uint32_t tmem;
 };
+static_assert(sizeof(BwdBars) <= BwdLayout<64>::kBarBytes, "room of the barriers");
 
-// One half (64 columns) of a row of scores and its place: P 2^kUp in FP32.  `shift` is added in the exponent.
-__device__ __forceinline__ void pack_store(uint32_t taddr, const float (&p)[64]) {
-  uint32_t h[32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) h[i] = rows::pack2(p[2 * i], p[2 * i + 1]);
-  tmem_st_32x32(taddr, h);
-}
-__device__ __forceinline__ void load64(uint32_t taddr, uint32_t (&a)[32], uint32_t (&b)[32]) {
-  ptx::tmem_ld_32x32(taddr, a);
-  ptx::tmem_ld_32x32(taddr + 32, b);
-  ptx::tmem_ld_wait();
-}
-// Rows `row` of a tile from tensor memory, times f, to the columns of a head.
-template <int COLS>
-__device__ __forceinline__ void store_rows(uint32_t taddr, float f, uint16_t* out, bool on, int col0, int D) {
-#pragma unroll 1
-  for (int i = 0; i < COLS; i += 32) {
-    if (col0 + i >= D) break;                     // warp-uniform
-    uint32_t v[32];
-    ptx::tmem_ld_32x32(taddr + i, v);
-    ptx::tmem_ld_wait();
-    if (on) {
-#pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(v[e + k]) * f;
-        if (col0 + i + e < D) *reinterpret_cast<uint4*>(out + col0 + i + e) = rows::pack8(x);
-      }
+template <int DP>
+struct BwdSmem {
+  using L = BwdLayout<DP>;
+  uint8_t* base;
+  __device__ __forceinline__ uint8_t* fixed(int i) const { return base + i * L::kTileBytes; }
+  __device__ __forceinline__ uint8_t* a(int x) const { return base + (2 + x % L::kA) * L::kTileBytes; }
+  __device__ __forceinline__ uint8_t* b(int x) const { return base + (2 + L::kA + x % L::kB) * L::kTileBytes; }
+  __device__ __forceinline__ float* stats(int x) const {
+    return reinterpret_cast<float*>(base + (2 + L::kA + L::kB) * L::kTileBytes + x % L::kStats * L::kStatBytes);
+  }
+  __device__ __forceinline__ BwdBars& bars() const {
+    return *reinterpret_cast<BwdBars*>(base + (2 + L::kA + L::kB) * L::kTileBytes + L::kStats * L::kStatBytes);
+  }
+};
+
+// The copies of n pairs of tiles; `tail(x)`: rows of pair x that exist.  A's rows that do not are cleared, B's if `clear_b`.
+template <int DP, class Tail, class LoadA, class LoadB>
+__device__ __forceinline__ bool copy_pairs(const BwdSmem<DP>& m, BwdBars& b, int n, bool clear_b, Tail tail, LoadA load_a, LoadB load_b) {
+  using L = BwdLayout<DP>;
+  const int lane = threadIdx.x & 31;
+  bool ok = true;
+  int x = 0, y = 0, tails = 0;
+  auto one = [&](uint8_t* dst, uint64_t* full, bool cut, int valid, auto load) {
+    uint64_t* bar = cut ? &b.tail_full : full;
+    if (lane == 0) {
+      ptx::mbar_arrive_expect_tx(bar, L::kTileBytes);
+      load(dst, bar);
     }
+    __syncwarp();
+    if (cut) {
+      ok = wait(&b.tail_full, tails++ & 1);
+      clear_rows<L::kBoxes>(dst, valid);
+      if (lane == 0) ptx::mbar_arrive(full);
+    }
+  };
+  for (; x < n && ok; ++x) {
+    const int valid = tail(x);
+    ok = wait(&b.empty_a[x % L::kA], (x / L::kA & 1) ^ 1);
+    if (!ok) break;
+    one(m.a(x), &b.full_a[x % L::kA], valid < kTile, valid, [&](uint8_t* d, uint64_t* bar) { load_a(x, d, bar); });
+    ok = ok && wait(&b.empty_b[x % L::kB], (x / L::kB & 1) ^ 1);
+    if (!ok) break;
+    one(m.b(x), &b.full_b[x % L::kB], clear_b && valid < kTile, valid, [&](uint8_t* d, uint64_t* bar) { load_b(x, d, bar); });
+    y = x + 1;
+  }
+  // no copy is in flight into a block that has ended
+  wait(&b.fixed_full, 0);
+  for (int i = max(0, x - L::kA); i < x; ++i) wait(&b.full_a[i % L::kA], i / L::kA & 1);
+  for (int i = max(0, y - L::kB); i < y; ++i) wait(&b.full_b[i % L::kB], i / L::kB & 1);
+  return ok;
+}
+
+// 32 scores of a row to their place as FP16.
+__device__ __forceinline__ void pack_store(uint32_t taddr, const float2 (&p)[16]) {
+  uint32_t h[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) h[i] = rows::pack2(p[i].x, p[i].y);
+  tmem_st_32x16(taddr, h);
+}
+// 32 columns of rows from tensor memory, times f, to the columns of a head from col0 on.
+__device__ __forceinline__ void store_rows(uint32_t taddr, float f, uint16_t* out, bool on, int col0, int D) {
+  uint32_t v[32];
+  ptx::tmem_ld_32x32(taddr, v);
+  ptx::tmem_ld_wait();
+  if (!on) return;
+#pragma unroll
+  for (int e = 0; e < 32; e += 8) {
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(v[e + k]) * f;
+    if (col0 + e < D) *reinterpret_cast<uint4*>(out + col0 + e) = rows::pack8(x);
+  }
+}
+__device__ __forceinline__ float2 pair_of(const uint32_t (&r)[32], int i) {
+  return make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+}
+// Zeros in place of the columns outside begin .. end - 1.
+__device__ __forceinline__ void mask32(float2 (&p)[16], int begin, int end) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (2 * i < begin || 2 * i >= end) p[i].x = 0.0f;
+    if (2 * i + 1 < begin || 2 * i + 1 >= end) p[i].y = 0.0f;
   }
 }
 
 template <int DP>
 __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
-                                           const CUtensorMap& mdo, const BwdArgs& a, const Place& at, int kv,
-                                           uint8_t* smem, BwdBars<BwdLayout<DP>::kStages>& b) {
+                                           const CUtensorMap& mdo, const BwdArgs& a, const Place& at, int kv, const BwdSmem<DP>& m) {
   using L = BwdLayout<DP>;
   const Shape& s = a.s;
+  BwdBars& b = m.bars();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = s.heads / s.kv_heads;
   const int k0 = (int)at.tile * kTile, len = (int)at.len, row0 = (int)at.start, nq = (len + kTile - 1) / kTile;
   const int i0 = s.causal ? (int)at.tile : 0;     // query tiles that see these keys
   const int64_t reach = k0 + kTile - 1 + (s.window > 0 ? s.window : (int64_t)len);   // first query past all their windows
   const int i1 = s.window > 0 && reach < len ? (int)((reach + kTile - 1) / kTile) : nq;
   const int per = i1 - i0, n = per * group;
-  uint8_t* ring = smem + 2 * L::kTileBytes;
-  float* stats = reinterpret_cast<float*>(ring + 2 * L::kStages * L::kTileBytes);
   const uint32_t tmem = b.tmem;
-  constexpr uint32_t kS = 0, kDP = 128, kDV = 256, kDK = 256 + DP;
+  constexpr uint32_t kS = 0, kDP = 128, kSums = 256;         // then dV and dK
   bool ok = true;
 
-  if (warp == 9) {
+  if (warp == kCopies) {
     if (lane == 0) {
       ptx::mbar_arrive_expect_tx(&b.fixed_full, 2 * L::kTileBytes);
-      load_tile<L::kBoxes>(smem, &mk, &b.fixed_full, kv, row0 + k0);
-      load_tile<L::kBoxes>(smem + L::kTileBytes, &mv, &b.fixed_full, kv, row0 + k0);
+      load_tile<L::kBoxes>(m.fixed(0), &mk, &b.fixed_full, kv, row0 + k0);
+      load_tile<L::kBoxes>(m.fixed(1), &mv, &b.fixed_full, kv, row0 + k0);
     }
-    int x = 0, tails = 0;
-    for (; x < n && ok; ++x) {
-      const int stage = x % L::kStages, head = kv * group + x / per, i = i0 + x % per, valid = len - i * kTile;
-      ok = wait(&b.empty[stage], (x / L::kStages & 1) ^ 1);
-      if (!ok) break;
-      uint8_t* dst = ring + stage * 2 * L::kTileBytes;
-      const bool tail = valid < kTile;
-      uint64_t* bar = tail ? &b.tail_full : &b.full[stage];
-      if (lane == 0) {
-        ptx::mbar_arrive_expect_tx(bar, 2 * L::kTileBytes);
-        load_tile<L::kBoxes>(dst, &mq, bar, head, row0 + i * kTile);
-        load_tile<L::kBoxes>(dst + L::kTileBytes, &mdo, bar, head, row0 + i * kTile);
-      }
-      __syncwarp();
-      if (tail) {                                 // queries and gradients of the next sequence: operands of both sums
-        ok = wait(&b.tail_full, tails++ & 1);
-        clear_rows<L::kBoxes>(dst, valid);
-        clear_rows<L::kBoxes>(dst + L::kTileBytes, valid);
-        if (lane == 0) ptx::mbar_arrive(&b.full[stage]);
-      }
-    }
-    wait(&b.fixed_full, 0);
-    for (int i = max(0, x - L::kStages); i < x; ++i) wait(&b.full[i % L::kStages], i / L::kStages & 1);
-  } else if (warp == 10) {
-    const float f = ex2(ds_exponent(a, kv) - kUp);    // P holds 2^kUp of it
+    // queries and gradients of the next sequence would be operands of both sums: cleared
+    auto load = [&](const CUtensorMap& map, int x, uint8_t* d, uint64_t* bar) {
+      load_tile<L::kBoxes>(d, &map, bar, kv * group + x / per, row0 + (i0 + x % per) * kTile);
+    };
+    ok = copy_pairs<DP>(m, b, n, true, [&](int x) { return len - (i0 + x % per) * kTile; },
+                        [&](int x, uint8_t* d, uint64_t* bar) { load(mq, x, d, bar); },
+                        [&](int x, uint8_t* d, uint64_t* bar) { load(mdo, x, d, bar); });
+  } else if (warp == kStatistics) {
+    const float f = ex2(ds_exponent(a, kv) - kUp);           // P holds 2^kUp of dS's factor
     for (int x = 0; x < n && ok; ++x) {
-      const int stage = x % L::kStages, head = kv * group + x / per, i = i0 + x % per;
-      ok = wait(&b.stat_empty[stage], (x / L::kStages & 1) ^ 1);
+      const int head = kv * group + x / per, i = i0 + x % per;
+      ok = wait(&b.stat_empty[x % L::kStats], (x / L::kStats & 1) ^ 1);
       if (!ok) break;
-      float* dst = stats + stage * 2 * kTile;
+      float* dst = m.stats(x);
       const int64_t base = (int64_t)head * s.T + row0;
 #pragma unroll
       for (int e = 0; e < kTile; e += 32) {
         const int q = i * kTile + e + lane;
         const bool on = q < len;                  // a query that is not there weighs nothing
-        dst[e + lane] = on ? fmaf(a.lse[base + q], kLog2e, -kUp) : INFINITY;
-        dst[kTile + e + lane] = on ? a.delta[base + q] * f : 0.0f;
+        dst[e + lane] = on ? fmaf(a.lse[base + q], -kLog2e, kUp) : -INFINITY;
+        dst[kTile + e + lane] = on ? -a.delta[base + q] * f : 0.0f;
       }
-      arrive(&b.stat_full[stage]);
+      arrive(&b.stat_full[x % L::kStats]);
     }
-  } else if (warp == 8) {
+  } else if (warp == kProducts) {
     const int ksteps = (s.D + 15) / 16;
     const uint32_t idesc_s = ptx::idesc_f16_f32(kTile, kTile, false, false);
     const uint32_t idesc_o = ptx::idesc_f16_f32(kTile, ksteps * 16, false, true);
-    const uint32_t sk = ptx::smem_u32(smem), sv = sk + L::kTileBytes;
-    auto tile = [&](int x) { return ptx::smem_u32(ring + x % L::kStages * 2 * L::kTileBytes); };
+    const uint64_t dk = desc_k(ptx::smem_u32(m.fixed(0))), dv = desc_k(ptx::smem_u32(m.fixed(1)));
     auto scores = [&](int x) {
-      product_ss<DP / 16>(tmem + kS, desc_k(sk), desc_k(tile(x)), idesc_s, ksteps);
+      product_ss<DP / 16>(tmem + kS, dk, desc_k(ptx::smem_u32(m.a(x))), idesc_s, ksteps);
       ptx::mma_commit(&b.s_full[0]);
     };
     auto dprob = [&](int x) {
-      product_ss<DP / 16>(tmem + kDP, desc_k(sv), desc_k(tile(x) + L::kTileBytes), idesc_s, ksteps);
+      product_ss<DP / 16>(tmem + kDP, dv, desc_k(ptx::smem_u32(m.b(x))), idesc_s, ksteps);
       ptx::mma_commit(&b.dp_full);
     };
-    ok = wait(&b.fixed_full, 0) && wait(&b.full[0], 0);
+    ok = wait(&b.fixed_full, 0) && wait(&b.full_a[0], 0) && wait(&b.full_b[0], 0);
     ptx::tc_fence_after_sync();
     if (ok && ptx::elect_one()) {
       scores(0);
@@ -233,61 +272,57 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
     }
     __syncwarp();
     for (int x = 0; x < n && ok; ++x) {
-      ok = wait(&b.p_ready, x & 1);
-      if (ok && x + 1 < n) ok = wait(&b.full[(x + 1) % L::kStages], (x + 1) / L::kStages & 1);
+      if (x + 1 < n) ok = wait(&b.full_a[(x + 1) % L::kA], (x + 1) / L::kA & 1);
+      ok = ok && wait(&b.p_ready, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       if (ptx::elect_one()) {
-        product_ts<0, 8>(tmem + kDV, tmem + kS, desc_mn(tile(x) + L::kTileBytes), idesc_o, 8, x > 0);
+        product_ts<8, true>(tmem + kSums, tmem + kS, desc_mn(ptx::smem_u32(m.b(x))), idesc_o, 8, x > 0);
         if (x + 1 < n) scores(x + 1);             // in the place of that P
+        ptx::mma_commit(&b.empty_b[x % L::kB]);
       }
       __syncwarp();
-      ok = wait(&b.ds_ready, x & 1);
+      if (x + 1 < n) ok = wait(&b.full_b[(x + 1) % L::kB], (x + 1) / L::kB & 1);
+      ok = ok && wait(&b.ds_ready, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       if (ptx::elect_one()) {
-        product_ts<0, 8>(tmem + kDK, tmem + kDP, desc_mn(tile(x)), idesc_o, 8, x > 0);
-        ptx::mma_commit(&b.empty[x % L::kStages]);
+        product_ts<8, true>(tmem + kSums + DP, tmem + kDP, desc_mn(ptx::smem_u32(m.a(x))), idesc_o, 8, x > 0);
         if (x + 1 < n) dprob(x + 1);
         else ptx::mma_commit(&b.done);
+        ptx::mma_commit(&b.empty_a[x % L::kA]);
       }
       __syncwarp();
     }
   } else {
-    const int half = warp >> 2, key = k0 + (warp & 3) * 32 + lane;
+    const int quarter = warp >> 2, key = k0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + kS + lanes + half * 64, td = tmem + kDP + lanes + half * 64;
-    const float up = ds_exponent(a, kv), f = ex2(up - kUp), c = s.scale_log2;    // P holds 2^kUp of dS's factor
+    const uint32_t ts = tmem + kS + lanes + quarter * 32, td = tmem + kDP + lanes + quarter * 32;
+    const float up = ds_exponent(a, kv), f = ex2(up - kUp);  // P holds 2^kUp of dS's factor
+    const float2 c2 = make_float2(s.scale_log2, s.scale_log2), f2 = make_float2(f, f);
     for (int x = 0; x < n && ok; ++x) {
-      const int stage = x % L::kStages, q0 = (i0 + x % per) * kTile;
-      ok = wait(&b.stat_full[stage], x / L::kStages & 1) && wait(&b.s_full[0], x & 1);
+      const int q0 = (i0 + x % per) * kTile;
+      ok = wait(&b.stat_full[x % L::kStats], x / L::kStats & 1) && wait(&b.s_full[0], x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      uint32_t r0[32], r1[32];
-      load64(ts, r0, r1);
-      const float4* lse = reinterpret_cast<const float4*>(stats + stage * 2 * kTile + half * 64);
+      uint32_t r[32];
+      ptx::tmem_ld_32x32(ts, r);
+      ptx::tmem_ld_wait();
+      const float4* lse = reinterpret_cast<const float4*>(m.stats(x) + quarter * 32);
       const float4* delta = lse + kTile / 4;
       // queries that see this key: q - key in 0 .. window - 1
       const bool edge = s.causal && (q0 < k0 + kTile || (s.window > 0 && q0 + kTile > k0 + s.window));
-      const int q = q0 + half * 64;
-      const int begin = edge ? key - q : 0;
-      const int end = edge && s.window > 0 ? (int)min(key - q + s.window, (int64_t)64) : 64;
-      float p[64];
+      const int q = q0 + quarter * 32;
+      const int begin = key - q, end = s.window > 0 ? (int)min(key - q + s.window, (int64_t)32) : 32;
+      float2 p[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 8; ++i) {
         const float4 l = lse[i];
-        const float ls[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = 4 * i + e;
-          p[col] = ex2(fmaf(__uint_as_float(col < 32 ? r0[col % 32] : r1[col % 32]), c, -ls[e]));
-        }
+        const float2 u = fma2(pair_of(r, 2 * i), c2, make_float2(l.x, l.y)), v = fma2(pair_of(r, 2 * i + 1), c2, make_float2(l.z, l.w));
+        p[2 * i] = make_float2(ex2(u.x), ex2(u.y));
+        p[2 * i + 1] = make_float2(ex2(v.x), ex2(v.y));
       }
-      if (edge) {
-#pragma unroll
-        for (int col = 0; col < 64; ++col)
-          if (col < begin || col >= end) p[col] = 0.0f;
-      }
+      if (edge) mask32(p, begin, end);
       pack_store(ts, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
@@ -295,36 +330,33 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
       ok = wait(&b.dp_full, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      load64(td, r0, r1);
+      ptx::tmem_ld_32x32(td, r);
+      ptx::tmem_ld_wait();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float4 l = delta[i];
-        const float ds[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = 4 * i + e;
-          p[col] *= fmaf(__uint_as_float(col < 32 ? r0[col % 32] : r1[col % 32]), f, -ds[e]);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float4 d = delta[i];
+        p[2 * i] = mul2(p[2 * i], fma2(pair_of(r, 2 * i), f2, make_float2(d.x, d.y)));
+        p[2 * i + 1] = mul2(p[2 * i + 1], fma2(pair_of(r, 2 * i + 1), f2, make_float2(d.z, d.w)));
       }
-      if (edge) {                                 // 0 times what is not finite
-#pragma unroll
-        for (int col = 0; col < 64; ++col)
-          if (col < begin || col >= end) p[col] = 0.0f;
-      }
+      if (edge) mask32(p, begin, end);            // 0 times what is not finite
       pack_store(td, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
       arrive(&b.ds_ready);
-      arrive(&b.stat_empty[stage]);
+      arrive(&b.stat_empty[x % L::kStats]);
     }
     if (ok) ok = wait(&b.done, 0);
     if (ok) {
       ptx::tc_fence_after_sync();
       const bool on = key < len;
-      const int64_t row = at.start + key;
-      const int col0 = half * (DP / 2);
-      store_rows<DP / 2>(tmem + kDV + lanes + col0, ex2(-kUp), a.dv + row * a.lddv + (int64_t)kv * s.D, on, col0, s.D);
-      store_rows<DP / 2>(tmem + kDK + lanes + col0, s.scale * ex2(-up), a.dk + row * a.lddk + (int64_t)kv * s.D, on, col0, s.D);
+      const int64_t row = at.start + key, col = (int64_t)kv * s.D;
+#pragma unroll
+      for (int u = quarter * 32; u < 2 * DP; u += 128) {     // dV's columns, then dK's
+        const int col0 = u < DP ? u : u - DP;
+        if (col0 >= s.D) continue;                // warp-uniform
+        if (u < DP) store_rows(tmem + kSums + lanes + u, ex2(-kUp), a.dv + row * a.lddv + col, on, col0, s.D);
+        else store_rows(tmem + kSums + lanes + u, s.scale * ex2(-up), a.dk + row * a.lddk + col, on, col0, s.D);
+      }
     }
   }
   return ok;
@@ -332,63 +364,43 @@ __device__ __forceinline__ bool keys_block(const CUtensorMap& mq, const CUtensor
 
 template <int DP>
 __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
-                                              const CUtensorMap& mdo, const BwdArgs& a, const Place& at, int head,
-                                              uint8_t* smem, BwdBars<BwdLayout<DP>::kStages>& b) {
+                                              const CUtensorMap& mdo, const BwdArgs& a, const Place& at, int head, const BwdSmem<DP>& m) {
   using L = BwdLayout<DP>;
   const Shape& s = a.s;
+  BwdBars& b = m.bars();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kv = head / (s.heads / s.kv_heads);
   const int tile = (int)(at.tiles - 1 - at.tile), q0 = tile * kTile, len = (int)at.len, row0 = (int)at.start;
   const int last = min(q0 + kTile, len);
   const int j0 = s.window > 0 && q0 + 1 > s.window ? (int)(q0 + 1 - s.window) / kTile : 0;
   const int j1 = ((s.causal ? last : len) + kTile - 1) / kTile, n = j1 - j0;
-  uint8_t* ring = smem + 2 * L::kTileBytes;
   const uint32_t tmem = b.tmem;
   constexpr uint32_t kS = 0, kDP = 256, kDQ = 384;           // two places for S
   bool ok = true;
 
-  if (warp == 9) {
+  if (warp == kCopies) {
     if (lane == 0) {
       ptx::mbar_arrive_expect_tx(&b.fixed_full, 2 * L::kTileBytes);
-      load_tile<L::kBoxes>(smem, &mq, &b.fixed_full, head, row0 + q0);
-      load_tile<L::kBoxes>(smem + L::kTileBytes, &mdo, &b.fixed_full, head, row0 + q0);
+      load_tile<L::kBoxes>(m.fixed(0), &mq, &b.fixed_full, head, row0 + q0);
+      load_tile<L::kBoxes>(m.fixed(1), &mdo, &b.fixed_full, head, row0 + q0);
     }
-    int x = 0;
-    for (; x < n && ok; ++x) {
-      const int stage = x % L::kStages, j = j0 + x, valid = len - j * kTile;
-      ok = wait(&b.empty[stage], (x / L::kStages & 1) ^ 1);
-      if (!ok) break;
-      uint8_t* dst = ring + stage * 2 * L::kTileBytes;
-      const bool tail = valid < kTile;            // the last one alone
-      uint64_t* bar = tail ? &b.tail_full : &b.full[stage];
-      if (lane == 0) {
-        ptx::mbar_arrive_expect_tx(bar, 2 * L::kTileBytes);
-        load_tile<L::kBoxes>(dst, &mk, bar, kv, row0 + j * kTile);
-        load_tile<L::kBoxes>(dst + L::kTileBytes, &mv, bar, kv, row0 + j * kTile);
-      }
-      __syncwarp();
-      if (tail) {
-        ok = wait(&b.tail_full, 0);
-        clear_rows<L::kBoxes>(dst, valid);
-        if (lane == 0) ptx::mbar_arrive(&b.full[stage]);
-      }
-    }
-    wait(&b.fixed_full, 0);
-    for (int i = max(0, x - L::kStages); i < x; ++i) wait(&b.full[i % L::kStages], i / L::kStages & 1);
-  } else if (warp == 8) {
+    ok = copy_pairs<DP>(m, b, n, false, [&](int x) { return len - (j0 + x) * kTile; },
+                        [&](int x, uint8_t* d, uint64_t* bar) { load_tile<L::kBoxes>(d, &mk, bar, kv, row0 + (j0 + x) * kTile); },
+                        [&](int x, uint8_t* d, uint64_t* bar) { load_tile<L::kBoxes>(d, &mv, bar, kv, row0 + (j0 + x) * kTile); });
+  } else if (warp == kProducts) {
     const int ksteps = (s.D + 15) / 16;
     const uint32_t idesc_s = ptx::idesc_f16_f32(kTile, kTile, false, false);
     const uint32_t idesc_o = ptx::idesc_f16_f32(kTile, ksteps * 16, false, true);
-    const uint32_t sq = ptx::smem_u32(smem), sdo = sq + L::kTileBytes;
-    auto keys = [&](int x) { return ptx::smem_u32(ring + x % L::kStages * 2 * L::kTileBytes); };
+    const uint64_t dq = desc_k(ptx::smem_u32(m.fixed(0))), ddo = desc_k(ptx::smem_u32(m.fixed(1)));
     auto scores = [&](int x) {
-      product_ss<DP / 16>(tmem + kS + (x & 1) * kTile, desc_k(sq), desc_k(keys(x)), idesc_s, ksteps);
+      product_ss<DP / 16>(tmem + kS + (x & 1) * kTile, dq, desc_k(ptx::smem_u32(m.a(x))), idesc_s, ksteps);
       ptx::mma_commit(&b.s_full[x & 1]);
     };
     auto dprob = [&](int x) {
-      product_ss<DP / 16>(tmem + kDP, desc_k(sdo), desc_k(keys(x) + L::kTileBytes), idesc_s, ksteps);
+      product_ss<DP / 16>(tmem + kDP, ddo, desc_k(ptx::smem_u32(m.b(x))), idesc_s, ksteps);
       ptx::mma_commit(&b.dp_full);
+      ptx::mma_commit(&b.empty_b[x % L::kB]);
     };
-    ok = wait(&b.fixed_full, 0) && wait(&b.full[0], 0);
+    ok = wait(&b.fixed_full, 0) && wait(&b.full_a[0], 0) && wait(&b.full_b[0], 0);
     ptx::tc_fence_after_sync();
     if (ok && ptx::elect_one()) {
       scores(0);
@@ -397,31 +409,34 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
     __syncwarp();
     for (int x = 0; x < n && ok; ++x) {
       if (x + 1 < n) {                            // the next tile's scores while this one's are worked on
-        ok = wait(&b.full[(x + 1) % L::kStages], (x + 1) / L::kStages & 1) && wait(&b.s_free[(x + 1) & 1], ((x + 1) / 2 & 1) ^ 1);
+        ok = wait(&b.full_a[(x + 1) % L::kA], (x + 1) / L::kA & 1) && wait(&b.s_free[(x + 1) & 1], ((x + 1) / 2 & 1) ^ 1);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         if (ptx::elect_one()) scores(x + 1);
         __syncwarp();
+        ok = wait(&b.full_b[(x + 1) % L::kB], (x + 1) / L::kB & 1);
       }
-      ok = wait(&b.ds_ready, x & 1);
+      ok = ok && wait(&b.ds_ready, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
       if (ptx::elect_one()) {
-        product_ts<0, 8>(tmem + kDQ, tmem + kDP, desc_mn(keys(x)), idesc_o, 8, x > 0);
-        ptx::mma_commit(&b.empty[x % L::kStages]);
+        product_ts<8, true>(tmem + kDQ, tmem + kDP, desc_mn(ptx::smem_u32(m.a(x))), idesc_o, 8, x > 0);
         if (x + 1 < n) dprob(x + 1);
         else ptx::mma_commit(&b.done);
+        ptx::mma_commit(&b.empty_a[x % L::kA]);
       }
       __syncwarp();
     }
-  } else if (warp < 8) {
-    const int half = warp >> 2, row = q0 + (warp & 3) * 32 + lane;
+  } else if (warp < kCompute) {
+    const int quarter = warp >> 2, row = q0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t td = tmem + kDP + lanes + half * 64;
-    const float up = ds_exponent(a, kv), f = ex2(up - kUp), c = s.scale_log2;    // P holds 2^kUp of dS's factor
+    const uint32_t td = tmem + kDP + lanes + quarter * 32;
+    const float up = ds_exponent(a, kv), f = ex2(up - kUp);  // P holds 2^kUp of dS's factor
     const int64_t at_row = (int64_t)head * s.T + at.start + row;
     const bool on = row < len;
-    const float lse = on ? fmaf(a.lse[at_row], kLog2e, -kUp) : 0.0f, delta = on ? a.delta[at_row] * f : 0.0f;
+    const float lse = on ? fmaf(a.lse[at_row], -kLog2e, kUp) : 0.0f, delta = on ? -a.delta[at_row] * f : 0.0f;
+    const float2 c2 = make_float2(s.scale_log2, s.scale_log2), lse2 = make_float2(lse, lse);
+    const float2 f2 = make_float2(f, f), delta2 = make_float2(delta, delta);
     const int key1 = s.causal ? min(row + 1, len) : len;     // keys that this query sees
     const int key0 = s.window > 0 && row + 1 > s.window ? (int)(row + 1 - s.window) : 0;
     const int whole1 = s.causal ? min(q0 + 1, len) : len;
@@ -430,29 +445,27 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
       ok = wait(&b.s_full[x & 1], x / 2 & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      uint32_t r0[32], r1[32];
-      load64(tmem + kS + (x & 1) * kTile + lanes + half * 64, r0, r1);
+      uint32_t r[32];
+      ptx::tmem_ld_32x32(tmem + kS + (x & 1) * kTile + lanes + quarter * 32, r);
+      ptx::tmem_ld_wait();
       ptx::tc_fence_before_sync();
       arrive(&b.s_free[x & 1]);
       const int k0 = (j0 + x) * kTile;
       const bool edge = k0 + kTile > whole1 || k0 < whole0;
-      const int end = key1 - k0 - half * 64, begin = key0 - k0 - half * 64;
-      float p[64];
+      float2 p[16];
 #pragma unroll
-      for (int col = 0; col < 64; ++col)
-        p[col] = ex2(fmaf(__uint_as_float(col < 32 ? r0[col % 32] : r1[col % 32]), c, -lse));
+      for (int i = 0; i < 16; ++i) {
+        const float2 u = fma2(pair_of(r, i), c2, lse2);
+        p[i] = make_float2(ex2(u.x), ex2(u.y));
+      }
       ok = wait(&b.dp_full, x & 1);
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      load64(td, r0, r1);
+      ptx::tmem_ld_32x32(td, r);
+      ptx::tmem_ld_wait();
 #pragma unroll
-      for (int col = 0; col < 64; ++col)
-        p[col] *= fmaf(__uint_as_float(col < 32 ? r0[col % 32] : r1[col % 32]), f, -delta);
-      if (edge) {
-#pragma unroll
-        for (int col = 0; col < 64; ++col)
-          if (col < begin || col >= end) p[col] = 0.0f;
-      }
+      for (int i = 0; i < 16; ++i) p[i] = mul2(p[i], fma2(pair_of(r, i), f2, delta2));
+      if (edge) mask32(p, key0 - k0 - quarter * 32, key1 - k0 - quarter * 32);
       pack_store(td, p);
       tmem_st_wait();
       ptx::tc_fence_before_sync();
@@ -461,9 +474,9 @@ __device__ __forceinline__ bool queries_block(const CUtensorMap& mq, const CUten
     if (ok) ok = wait(&b.done, 0);
     if (ok) {
       ptx::tc_fence_after_sync();
-      const int col0 = half * (DP / 2);
-      store_rows<DP / 2>(tmem + kDQ + lanes + col0, s.scale * ex2(-up),
-                         a.dq + (at.start + row) * a.lddq + (int64_t)head * s.D, on, col0, s.D);
+      const int col0 = quarter * 32;
+      if (col0 < DP && col0 < s.D)
+        store_rows(tmem + kDQ + lanes + col0, s.scale * ex2(-up), a.dq + (at.start + row) * a.lddq + (int64_t)head * s.D, on, col0, s.D);
     }
   }
   return ok;
@@ -474,9 +487,9 @@ __global__ void __launch_bounds__(kBwdThreads, 1)
 mp_attention_bwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                         const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo, const BwdArgs a) {
   using L = BwdLayout<DP>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ BwdBars<L::kStages> b;
+  extern __shared__ __align__(1024) uint8_t smem[];          // (nothing else is in shared memory: it begins at a multiple of 1024)
+  const BwdSmem<DP> m{smem};
+  BwdBars& b = m.bars();
   const Shape& s = a.s;
   const int warp = threadIdx.x >> 5;
   ptx::launch_dependents();
@@ -489,35 +502,37 @@ mp_attention_bwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   if (threadIdx.x == 0) {
     ptx::mbar_init(&b.fixed_full, 1);
     ptx::mbar_init(&b.tail_full, 1);
-    for (int i = 0; i < L::kStages; ++i) {
-      ptx::mbar_init(&b.full[i], 1);
-      ptx::mbar_init(&b.empty[i], 1);
-      ptx::mbar_init(&b.stat_full[i], 1);
-      ptx::mbar_init(&b.stat_empty[i], 8);          // warps, as below
+    for (int i = 0; i < 4; ++i) {
+      ptx::mbar_init(&b.full_a[i], 1);
+      ptx::mbar_init(&b.empty_a[i], 1);
+      ptx::mbar_init(&b.full_b[i], 1);
+      ptx::mbar_init(&b.empty_b[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&b.stat_full[i], 1);
+      ptx::mbar_init(&b.stat_empty[i], kCompute);            // warps, as below
       ptx::mbar_init(&b.s_full[i], 1);
-      ptx::mbar_init(&b.s_free[i], 8);
+      ptx::mbar_init(&b.s_free[i], kCompute);
     }
     ptx::mbar_init(&b.dp_full, 1);
-    ptx::mbar_init(&b.p_ready, 8);
-    ptx::mbar_init(&b.ds_ready, 8);
+    ptx::mbar_init(&b.p_ready, kCompute);
+    ptx::mbar_init(&b.ds_ready, kCompute);
     ptx::mbar_init(&b.done, 1);
     ptx::fence_mbar_init();
   }
-  if (warp == 8) {
+  if (warp == kProducts) {
     ptx::tmem_alloc(&b.tmem, 512);
     ptx::tmem_relinquish();
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
-  const bool ok = keys ? keys_block<DP>(mq, mk, mv, mdo, a, at, item % heads, smem, b)
-                       : queries_block<DP>(mq, mk, mv, mdo, a, at, item % heads, smem, b);
+  const bool ok = keys ? keys_block<DP>(mq, mk, mv, mdo, a, at, item % heads, m)
+                       : queries_block<DP>(mq, mk, mv, mdo, a, at, item % heads, m);
   if (!ok && (threadIdx.x & 31) == 0) report_timeout(s);
   ptx::tc_fence_before_sync();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kProducts) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(b.tmem, 512);
   }
