@@ -4,7 +4,8 @@
 // gain (one for the queries, one for the keys) and rotated pair by pair by the token's position.  One read and one
 // write of the heads (backward: two reads and a write): HBM bounds it from some 10 MB on, launch latency below.
 // L lanes share a head, 8 elements each, so 32 / L heads are worked on by a warp at a time ("a round"); a warp keeps one
-// token's angles for all its rounds, since all heads of a token turn alike.
+// token's angles for all its rounds, since all heads of a token turn alike: each lane forms a few, through shared memory every
+// lane gets those of its columns.  Persistent blocks; the loads of a warp's next rounds are under way while it works on these.
 // Angles: a position times a frequency, in turns, is a 64-bit fixed-point product whose whole turns fall off the top: the
 // fraction stays exact to 2^-53 of a turn times the position, where an FP32 product has lost a whole radian at 2^24.
 
@@ -16,7 +17,7 @@
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxBlocks = 148 * 4;               // of the backward kernel: rows of its partial sums
+constexpr int kMaxBlocks = 148 * 2;               // as many as are resident; rows of the backward kernel's partial sums
 
 struct HeadArgs {
   const uint16_t *x, *dy, *gq, *gk;
@@ -37,15 +38,18 @@ template <bool PAIRS>
 struct Turn {
   static constexpr int N = PAIRS ? 4 : 8;
   float c[N], s[N];
-  // `back`: by the opposite angle.  Columns past `rot` keep their place.
-  __device__ __forceinline__ void set(const HeadArgs& a, const uint64_t (&f)[N], int64_t pos, bool back) {
+  // From the token's angles at `table`, of which this lane's begin at `first`.
+  __device__ __forceinline__ void load(const float2* table, int first) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float t = (float)(int32_t)((f[i] * (uint64_t)pos) >> 32) * 0x1p-31f;     // half turns, -1 .. 1
-      sincospif(back ? -t : t, &s[i], &c[i]);
+    for (int i = 0; i < N; i += 2) {
+      const float4 v = *reinterpret_cast<const float4*>(table + first + i);
+      c[i] = v.x;
+      s[i] = v.y;
+      c[i + 1] = v.z;
+      s[i + 1] = v.w;
     }
   }
-  // Rotates a lane's 8 columns.  `other`: lanes to the pair's other half (0: nothing turns here); `sign`: -1 in the first half.
+  // Rotates a lane's 8 columns; `partner`: the lane with the other halves of its pairs, `sign`: -1 in the first halves.
   __device__ __forceinline__ void apply(float (&v)[8], int partner, float sign) const {
     if constexpr (PAIRS) {
 #pragma unroll
@@ -63,21 +67,8 @@ struct Turn {
     }
   }
 };
+constexpr int kAngles = MP_HEAD_MAX_D / 2 + 8;    // of a token, and 8 zero angles for columns that do not turn
 
-template <bool PAIRS>
-__device__ __forceinline__ void load_freqs(const HeadArgs& a, int col, uint64_t (&f)[Turn<PAIRS>::N]) {
-#pragma unroll
-  for (int i = 0; i < Turn<PAIRS>::N; ++i) {
-    const int at = PAIRS ? col + 2 * i : col + i;
-    f[i] = 0;
-    if (at < a.rot) {
-      const int k = PAIRS ? at / 2 : at >= a.rot / 2 ? at - a.rot / 2 : at;
-      double t = a.freqs[k] * 0.15915494309189535;           // turns of one position
-      t -= floor(t);
-      f[i] = __double2ull_rn(t * 18446744073709551616.0);
-    }
-  }
-}
 __device__ __forceinline__ int64_t position(const HeadArgs& a, int64_t i) {
   if (a.rot == 0) return 0;
   return a.pos_bytes == 8 ? rows::load_id<int64_t>(a.pos, i) : rows::load_id<int32_t>(a.pos, i);
@@ -124,75 +115,134 @@ struct Rounds {
 template <int L, bool PAIRS, bool BACK>
 __global__ void __launch_bounds__(kThreads, 2) mp_head_norm_rope_kernel(const HeadArgs a) {
   constexpr int U = BACK ? 2 : 4;                 // rounds whose loads are in flight together
+  constexpr int kSlots = MP_HEAD_MAX_D / 64;      // angles of a lane
+  __shared__ __align__(16) float2 tables[kWarps][kAngles];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane % L, col = t * 8;
   const bool inside = col < a.D;
   ptx::launch_dependents();
   ptx::grid_dependency_wait();
   // the other member of a lane's pairs, where the halves of a head are rotated against one another
-  const int hop = a.rot / 16;
+  const int hop = a.rot / 16, angles = a.rot / 2;
   const int partner = col >= a.rot ? lane : t < hop ? lane + hop : lane - hop;
   const float sign = t < hop ? -1.0f : 1.0f;
-  uint64_t f[Turn<PAIRS>::N];
-  load_freqs<PAIRS>(a, col, f);
+  const int mine = col >= a.rot ? MP_HEAD_MAX_D / 2 : PAIRS ? col / 2 : col >= angles ? col - angles : col;
+  float2* table = tables[warp];
+  if (lane < 8) table[MP_HEAD_MAX_D / 2 + lane] = make_float2(1.0f, 0.0f);
+  // Turns of one position in 64-bit fixed point: times a position, whole turns fall off the top.
+  uint64_t f[kSlots];
+#pragma unroll
+  for (int i = 0; i < kSlots; ++i) {
+    f[i] = 0;
+    if (i * 32 + lane < angles) {
+      double x = a.freqs[i * 32 + lane] * 0.15915494309189535;
+      x -= floor(x);
+      f[i] = __double2ull_rn(x * 18446744073709551616.0);
+    }
+  }
   float gq[8], gk[8], sq[8], sk[8];
   gain8(a.gq, col, inside, gq);
   gain8(a.gk, col, inside, gk);
 #pragma unroll
   for (int i = 0; i < 8; ++i) sq[i] = sk[i] = 0.0f;
   const float inv_d = 1.0f / (float)a.D;
-  const int64_t items = a.T * a.parts;
-  for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < items; item += (int64_t)gridDim.x * kWarps) {
-    const int64_t i = item / a.parts;
-    const Rounds<L> rounds(a, (int)(item - i * a.parts));
-    rows::Raw8<uint16_t> rx[U], rd[U];
-    auto load = [&](int r) {
+  const int64_t items = a.T * a.parts, stride = (int64_t)gridDim.x * kWarps;
+  // Where a warp stands: the item (token, part), and its round.
+  struct At {
+    int64_t item, token;
+    int r, end;
+  };
+  auto enter = [&](At& p) {
+    p.r = p.end = 0;
+    if (p.item >= items) return;
+    p.token = p.item / a.parts;
+    const Rounds<L> x(a, (int)(p.item - p.token * a.parts));
+    p.r = x.first;
+    p.end = x.end;
+  };
+  const Rounds<L> rounds(a, 0);
+  auto load = [&](const At& p, rows::Raw8<uint16_t> (&rx)[U], rows::Raw8<uint16_t> (&rd)[BACK ? U : 1]) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = r + u < rounds.end ? rounds.head(r + u) : -1;
-        const int64_t c = (int64_t)h * a.D + col;
-        rx[u].load(a.x + i * a.ldx + c, h >= 0 && inside ? 8 : 0);
-        if constexpr (BACK) rd[u].load(a.dy + i * a.lddy + c, h >= 0 && inside ? 8 : 0);
-      }
-    };
-    load(rounds.first);
-    Turn<PAIRS> turn;
-    turn.set(a, f, position(a, i), BACK);
-    for (int r = rounds.first; r < rounds.end; r += U) {
-      if (r > rounds.first) load(r);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (r + u >= rounds.end) break;           // warp-uniform
-        const int h = rounds.head(r + u);
-        const bool query = r + u < rounds.rq;
-        float x[8], ss = 0.0f;
-        rx[u].floats(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-        const float root = rsqrtf(fmaf(head_sum<L>(ss), inv_d, a.eps));
-        if constexpr (!BACK) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= root * (query ? gq[e] : gk[e]);
-          turn.apply(x, partner, sign);
-        } else {
-          float d[8], dot = 0.0f;
-          rd[u].floats(d);
-          turn.apply(d, partner, sign);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] *= root;
-            const float w = d[e] * x[e];
-            if (query) sq[e] += w;
-            else sk[e] += w;
-            d[e] *= query ? gq[e] : gk[e];
-            dot = fmaf(d[e], x[e], dot);
-          }
-          dot = head_sum<L>(dot) * inv_d;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = root * fmaf(-x[e], dot, d[e]);
-        }
-        if (h >= 0 && inside) rows::store8(a.out + i * a.ldo + (int64_t)h * a.D + col, x, 8);
-      }
+    for (int u = 0; u < U; ++u) {
+      const int h = p.r + u < p.end ? rounds.head(p.r + u) : -1;
+      const int64_t c = (int64_t)h * a.D + col;
+      const int n = h >= 0 && inside ? 8 : 0;
+      rx[u].load(a.x + p.token * a.ldx + c, n);
+      if constexpr (BACK) rd[u].load(a.dy + p.token * a.lddy + c, n);
     }
+  };
+  auto after = [&](At p) {                        // the next rounds of the item, or the next item's first
+    p.r += U;
+    if (p.r >= p.end) {
+      p.item += stride;
+      enter(p);
+    }
+    return p;
+  };
+  At here{(int64_t)blockIdx.x * kWarps + warp, 0, 0, 0};
+  enter(here);
+  rows::Raw8<uint16_t> rx[U], rd[BACK ? U : 1];
+  load(here, rx, rd);
+  int64_t pos = here.item < items ? position(a, here.token) : 0, token = -1;
+  Turn<PAIRS> turn;
+  while (here.item < items) {
+    const At next = after(here);
+    rows::Raw8<uint16_t> nx[U], nd[BACK ? U : 1];
+    load(next, nx, nd);
+    const int64_t next_pos = next.item < items && next.token != here.token ? position(a, next.token) : pos;
+    if (here.token != token) {
+      token = here.token;
+      __syncwarp();                               // the angles before have been read
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i)
+        if (i * 32 + lane < angles) {
+          const float x = (float)(int32_t)((f[i] * (uint64_t)pos) >> 32) * 0x1p-31f;     // half turns, -1 .. 1
+          float2 cs;
+          sincospif(BACK ? -x : x, &cs.y, &cs.x);
+          table[i * 32 + lane] = cs;
+        }
+      __syncwarp();
+      turn.load(table, mine);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (here.r + u >= here.end) break;          // warp-uniform
+      const int h = rounds.head(here.r + u);
+      const bool query = here.r + u < rounds.rq;
+      float x[8], ss = 0.0f;
+      rx[u].floats(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+      const float root = rsqrtf(fmaf(head_sum<L>(ss), inv_d, a.eps));
+      if constexpr (!BACK) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= root * (query ? gq[e] : gk[e]);
+        turn.apply(x, partner, sign);
+      } else {
+        float d[8], dot = 0.0f;
+        rd[u].floats(d);
+        turn.apply(d, partner, sign);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] *= root;
+          const float w = d[e] * x[e];
+          if (query) sq[e] += w;
+          else sk[e] += w;
+          d[e] *= query ? gq[e] : gk[e];
+          dot = fmaf(d[e], x[e], dot);
+        }
+        dot = head_sum<L>(dot) * inv_d;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = root * fmaf(-x[e], dot, d[e]);
+      }
+      if (h >= 0 && inside) rows::store8(a.out + here.token * a.ldo + (int64_t)h * a.D + col, x, 8);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      rx[u] = nx[u];
+      if constexpr (BACK) rd[u] = nd[u];
+    }
+    here = next;
+    pos = next_pos;
   }
   if constexpr (BACK) {
     if (a.part == nullptr) return;
@@ -251,12 +301,11 @@ int launch(HeadArgs a, int* used, cudaStream_t st) {
   const int rounds = (a.hq + G - 1) / G + (a.hk + G - 1) / G;
   // Few tokens are cut into parts, down to one round a warp, so that the loads of all heads start at once; many keep a token's
   // angles for all its rounds.
-  const int64_t want = (int64_t)kMaxBlocks * kWarps * 2;
-  int64_t parts = (want + a.T - 1) / a.T;
-  if (a.T * 4 > want && parts > (rounds + 3) / 4) parts = (rounds + 3) / 4;
+  const int64_t want = (int64_t)kMaxBlocks * kWarps;
+  const int64_t parts = (want + a.T - 1) / a.T;
   a.parts = (int)(parts < 1 ? 1 : parts > rounds ? rounds : parts);
   int64_t blocks = (a.T * a.parts + kWarps - 1) / kWarps;
-  if (blocks > kMaxBlocks * (BACK ? 1 : 4)) blocks = kMaxBlocks * (BACK ? 1 : 4);
+  if (blocks > kMaxBlocks) blocks = kMaxBlocks;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
