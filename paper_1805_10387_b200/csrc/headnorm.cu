@@ -5,7 +5,7 @@
 // write of the heads (backward: two reads and a write): HBM bounds it from some 10 MB on, launch latency below.
 // L lanes share a head, 8 elements each, so 32 / L heads are worked on by a warp at a time ("a round"); a warp keeps one
 // token's angles for all its rounds, since all heads of a token turn alike: each lane forms a few, through shared memory every
-// lane gets those of its columns.  Persistent blocks; the loads of a warp's next rounds are under way while it works on these.
+// lane gets those of its columns.  Persistent blocks.
 // Angles: a position times a frequency, in turns, is a 64-bit fixed-point product whose whole turns fall off the top: the
 // fraction stays exact to 2^-53 of a turn times the position, where an FP32 product has lost a whole radian at 2^24.
 
@@ -17,6 +17,7 @@
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRounds = 4;                        // whose loads are in flight together
 constexpr int kMaxBlocks = 148 * 2;               // as many as are resident; rows of the backward kernel's partial sums
 
 struct HeadArgs {
@@ -79,15 +80,10 @@ __device__ __forceinline__ float head_sum(float v) {
   for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
-__device__ __forceinline__ void gain8(const uint16_t* g, int col, bool on, float (&f)[8]) {
-  rows::Raw8<uint16_t> r;
-  if (g == nullptr) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = 1.0f;
-    return;
-  }
-  r.load_cached(g + col, on ? 8 : 0);
-  r.floats(f);
+// A lane's 8 gains as stored (1 where there are none).
+__device__ __forceinline__ uint4 gain8(const uint16_t* g, int col, bool on) {
+  if (g == nullptr) return make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u);
+  return on ? __ldg(reinterpret_cast<const uint4*>(g + col)) : make_uint4(0, 0, 0, 0);
 }
 
 // Work items: (token, part of its rounds); rounds 0 .. rq-1 are the queries', the others the keys'.
@@ -113,10 +109,10 @@ struct Rounds {
 };
 
 template <int L, bool PAIRS, bool BACK>
-__global__ void __launch_bounds__(kThreads, 2) mp_head_norm_rope_kernel(const HeadArgs a) {
-  constexpr int U = BACK ? 2 : 4;                 // rounds whose loads are in flight together
-  constexpr int kSlots = MP_HEAD_MAX_D / 64;      // angles of a lane
+__global__ void __launch_bounds__(kThreads, BACK ? 2 : 4) mp_head_norm_rope_kernel(const HeadArgs a) {
+  constexpr int U = kRounds;
   __shared__ __align__(16) float2 tables[kWarps][kAngles];
+  __shared__ uint64_t turns[MP_HEAD_MAX_D / 2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane % L, col = t * 8;
   const bool inside = col < a.D;
   ptx::launch_dependents();
@@ -129,120 +125,83 @@ __global__ void __launch_bounds__(kThreads, 2) mp_head_norm_rope_kernel(const He
   float2* table = tables[warp];
   if (lane < 8) table[MP_HEAD_MAX_D / 2 + lane] = make_float2(1.0f, 0.0f);
   // Turns of one position in 64-bit fixed point: times a position, whole turns fall off the top.
-  uint64_t f[kSlots];
-#pragma unroll
-  for (int i = 0; i < kSlots; ++i) {
-    f[i] = 0;
-    if (i * 32 + lane < angles) {
-      double x = a.freqs[i * 32 + lane] * 0.15915494309189535;
-      x -= floor(x);
-      f[i] = __double2ull_rn(x * 18446744073709551616.0);
-    }
+  for (int i = threadIdx.x; i < angles; i += kThreads) {
+    double x = a.freqs[i] * 0.15915494309189535;
+    x -= floor(x);
+    turns[i] = __double2ull_rn(x * 18446744073709551616.0);
   }
-  float gq[8], gk[8], sq[8], sk[8];
-  gain8(a.gq, col, inside, gq);
-  gain8(a.gk, col, inside, gk);
+  __syncthreads();
+  const uint4 gain_q = gain8(a.gq, col, inside), gain_k = gain8(a.gk, col, inside);
+  float sq[8], sk[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) sq[i] = sk[i] = 0.0f;
   const float inv_d = 1.0f / (float)a.D;
   const int64_t items = a.T * a.parts, stride = (int64_t)gridDim.x * kWarps;
-  // Where a warp stands: the item (token, part), and its round.
-  struct At {
-    int64_t item, token;
-    int r, end;
-  };
-  auto enter = [&](At& p) {
-    p.r = p.end = 0;
-    if (p.item >= items) return;
-    p.token = p.item / a.parts;
-    const Rounds<L> x(a, (int)(p.item - p.token * a.parts));
-    p.r = x.first;
-    p.end = x.end;
-  };
-  const Rounds<L> rounds(a, 0);
-  auto load = [&](const At& p, rows::Raw8<uint16_t> (&rx)[U], rows::Raw8<uint16_t> (&rd)[BACK ? U : 1]) {
+  for (int64_t item = (int64_t)blockIdx.x * kWarps + warp; item < items; item += stride) {
+    const int64_t token = item / a.parts;
+    const Rounds<L> rounds(a, (int)(item - token * a.parts));
+    rows::Raw8<uint16_t> rx[U], rd[BACK ? U : 1];
+    auto load = [&](int r) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = p.r + u < p.end ? rounds.head(p.r + u) : -1;
-      const int64_t c = (int64_t)h * a.D + col;
-      const int n = h >= 0 && inside ? 8 : 0;
-      rx[u].load(a.x + p.token * a.ldx + c, n);
-      if constexpr (BACK) rd[u].load(a.dy + p.token * a.lddy + c, n);
-    }
-  };
-  auto after = [&](At p) {                        // the next rounds of the item, or the next item's first
-    p.r += U;
-    if (p.r >= p.end) {
-      p.item += stride;
-      enter(p);
-    }
-    return p;
-  };
-  At here{(int64_t)blockIdx.x * kWarps + warp, 0, 0, 0};
-  enter(here);
-  rows::Raw8<uint16_t> rx[U], rd[BACK ? U : 1];
-  load(here, rx, rd);
-  int64_t pos = here.item < items ? position(a, here.token) : 0, token = -1;
-  Turn<PAIRS> turn;
-  while (here.item < items) {
-    const At next = after(here);
-    rows::Raw8<uint16_t> nx[U], nd[BACK ? U : 1];
-    load(next, nx, nd);
-    const int64_t next_pos = next.item < items && next.token != here.token ? position(a, next.token) : pos;
-    if (here.token != token) {
-      token = here.token;
-      __syncwarp();                               // the angles before have been read
-#pragma unroll
-      for (int i = 0; i < kSlots; ++i)
-        if (i * 32 + lane < angles) {
-          const float x = (float)(int32_t)((f[i] * (uint64_t)pos) >> 32) * 0x1p-31f;     // half turns, -1 .. 1
-          float2 cs;
-          sincospif(BACK ? -x : x, &cs.y, &cs.x);
-          table[i * 32 + lane] = cs;
-        }
-      __syncwarp();
-      turn.load(table, mine);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (here.r + u >= here.end) break;          // warp-uniform
-      const int h = rounds.head(here.r + u);
-      const bool query = here.r + u < rounds.rq;
-      float x[8], ss = 0.0f;
-      rx[u].floats(x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-      const float root = rsqrtf(fmaf(head_sum<L>(ss), inv_d, a.eps));
-      if constexpr (!BACK) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= root * (query ? gq[e] : gk[e]);
-        turn.apply(x, partner, sign);
-      } else {
-        float d[8], dot = 0.0f;
-        rd[u].floats(d);
-        turn.apply(d, partner, sign);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] *= root;
-          const float w = d[e] * x[e];
-          if (query) sq[e] += w;
-          else sk[e] += w;
-          d[e] *= query ? gq[e] : gk[e];
-          dot = fmaf(d[e], x[e], dot);
-        }
-        dot = head_sum<L>(dot) * inv_d;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = root * fmaf(-x[e], dot, d[e]);
+      for (int u = 0; u < U; ++u) {
+        const int h = r + u < rounds.end ? rounds.head(r + u) : -1;
+        const int64_t c = (int64_t)h * a.D + col;
+        const int n = h >= 0 && inside ? 8 : 0;
+        rx[u].load(a.x + token * a.ldx + c, n);
+        if constexpr (BACK) rd[u].load(a.dy + token * a.lddy + c, n);
       }
-      if (h >= 0 && inside) rows::store8(a.out + here.token * a.ldo + (int64_t)h * a.D + col, x, 8);
+    };
+    load(rounds.first);
+    const uint64_t pos = (uint64_t)position(a, token);
+    __syncwarp();                                 // the angles before have been read
+    for (int i = lane; i < angles; i += 32) {
+      const float x = (float)(int32_t)((turns[i] * pos) >> 32) * 0x1p-31f;       // half turns, -1 .. 1
+      float2 cs;
+      sincospif(BACK ? -x : x, &cs.y, &cs.x);
+      table[i] = cs;
     }
+    __syncwarp();
+    Turn<PAIRS> turn;
+    turn.load(table, mine);
+    for (int r = rounds.first; r < rounds.end; r += U) {
+      if (r > rounds.first) load(r);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      rx[u] = nx[u];
-      if constexpr (BACK) rd[u] = nd[u];
+      for (int u = 0; u < U; ++u) {
+        if (r + u >= rounds.end) break;           // warp-uniform
+        const int h = rounds.head(r + u);
+        const bool query = r + u < rounds.rq;
+        float x[8], g[8], ss = 0.0f;
+        rx[u].floats(x);
+        rows::Raw8<uint16_t> gain;
+        gain.q = query ? gain_q : gain_k;
+        gain.floats(g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+        const float root = rsqrtf(fmaf(head_sum<L>(ss), inv_d, a.eps));
+        if constexpr (!BACK) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= root * g[e];
+          turn.apply(x, partner, sign);
+        } else {
+          float d[8], dot = 0.0f;
+          rd[u].floats(d);
+          turn.apply(d, partner, sign);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] *= root;
+            const float w = d[e] * x[e];
+            if (query) sq[e] += w;
+            else sk[e] += w;
+            d[e] *= g[e];
+            dot = fmaf(d[e], x[e], dot);
+          }
+          dot = head_sum<L>(dot) * inv_d;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = root * fmaf(-x[e], dot, d[e]);
+        }
+        if (h >= 0 && inside) rows::store8(a.out + token * a.ldo + (int64_t)h * a.D + col, x, 8);
+      }
     }
-    here = next;
-    pos = next_pos;
   }
   if constexpr (BACK) {
     if (a.part == nullptr) return;
@@ -299,13 +258,14 @@ template <int L, bool PAIRS, bool BACK>
 int launch(HeadArgs a, int* used, cudaStream_t st) {
   constexpr int G = 32 / L;
   const int rounds = (a.hq + G - 1) / G + (a.hk + G - 1) / G;
-  // Few tokens are cut into parts, down to one round a warp, so that the loads of all heads start at once; many keep a token's
-  // angles for all its rounds.
-  const int64_t want = (int64_t)kMaxBlocks * kWarps;
-  const int64_t parts = (want + a.T - 1) / a.T;
-  a.parts = (int)(parts < 1 ? 1 : parts > rounds ? rounds : parts);
+  // Tokens are cut into parts until every warp has some six of them, so that the last ones do not leave many idle, but not below the
+  // rounds whose loads are in flight together; few tokens down to one round a warp, so that the loads of all heads start at once.
+  const int64_t warps = (int64_t)148 * (BACK ? 2 : 4) * kWarps, whole = (rounds + kRounds - 1) / kRounds;
+  int64_t parts = (6 * warps + a.T - 1) / a.T;
+  if (parts > whole) parts = a.T * whole >= warps ? whole : (warps + a.T - 1) / a.T;
+  a.parts = (int)(parts > rounds ? rounds : parts);
   int64_t blocks = (a.T * a.parts + kWarps - 1) / kWarps;
-  if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+  if (blocks > 148 * (BACK ? 2 : 4)) blocks = 148 * (BACK ? 2 : 4);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
