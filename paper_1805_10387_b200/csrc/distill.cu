@@ -34,17 +34,16 @@ struct DistillArgs {
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kPartWords = 16 * kThreads * 8;     // words of a row that a block takes if a cluster of 8 can
 constexpr int kWarpWords = 2048;                  // rows of up to so many words go to single warps
-constexpr int kEach = MP_DISTILL_MAX_K / 32;      // entries of a lane
 
 // The entries of a row, lane l's are l, l + 32, ..: by the first warp of a row's threads.
+template <int E>
 struct Entries {
-  int id[kEach];                                  // -1: none; -2: not a token
-  float a[kEach], z[kEach];                       // the teacher's log-probability, the student's logit
+  int id[E];                                      // -1: none; -2: not a token
+  float a[E], z[E];                               // the teacher's log-probability, the student's logit
   __device__ __forceinline__ void load(const DistillArgs& g, int64_t i, bool on) {
-    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int k = e * 32 + lane;
+    for (int e = 0; e < E; ++e) {
+      const int k = e * 32 + (threadIdx.x & 31);
       id[e] = -1;
       a[e] = z[e] = -INFINITY;
       if (on && k < g.K) {
@@ -52,9 +51,13 @@ struct Entries {
         const int64_t t = g.id_bytes == 8 ? rows::load_id<int64_t>(g.ids, at) : rows::load_id<int32_t>(g.ids, at);
         a[e] = g.tlogp[at];
         id[e] = t == -1 ? -1 : t >= 0 && t < g.V ? (int)t : -2;
-        if (id[e] >= 0) z[e] = rows::h2f(g.z[i * g.ldl + id[e]]);
       }
     }
+  }
+  __device__ __forceinline__ void load_logits(const DistillArgs& g, int64_t i) {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (id[e] >= 0) z[e] = rows::h2f(g.z[i * g.ldl + id[e]]);
   }
 };
 
@@ -64,8 +67,9 @@ struct Grad {
   int check;
 };
 // What the first warp keeps until the gradients are written.
+template <int E>
 struct Listed {
-  float dz[kEach];
+  float dz[E];
 };
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -75,8 +79,9 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 
 // By a whole warp: the row's loss and the factors of its gradient, from the sum over the words that are not listed.
-__device__ __forceinline__ Grad finish(const DistillArgs& g, int64_t i, Entries& t, Sum2 rest, float w, float S, bool writer,
-                                       Listed& out) {
+template <int kEach>
+__device__ __forceinline__ Grad finish(const DistillArgs& g, int64_t i, Entries<kEach>& t, Sum2 rest, float w, float S,
+                                       bool writer, Listed<kEach>& out) {
   // the listed words' sum, their probabilities under the teacher
   float top = -INFINITY, most = -INFINITY;
   bool bad = false, any = false;
@@ -177,8 +182,8 @@ __device__ __forceinline__ bool strike(uint16_t* word, bool finite) {
 
 // TEAM threads a row: a warp each (short rows), or a block, or CL blocks of a cluster.  The layout of a row over its
 // threads and the refilling of its slots are the policy loss's.
-template <int CL, int TEAM>
-__global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillArgs g, int layers) {
+template <int CL, int TEAM, int kEach>
+__global__ void __launch_bounds__(kThreads, TEAM == 32 ? 8 : 7) mp_distill_kernel(const DistillArgs g, int layers) {
   static_assert(TEAM == kThreads || (TEAM == 32 && CL == 1), "a warp, a block or a cluster for a row");
   constexpr int TEAMS = kThreads / TEAM;
   extern __shared__ uint4 all_slots[];            // [team][vectors]
@@ -212,9 +217,15 @@ __global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillAr
   if constexpr (CL > 1) ptx::cluster_sync();
   float w = weight_of(first);
   if (w != 0.0f) fetch(first);
-  Entries e, ahead;
-  if (first_warp) ahead.load(g, first, w != 0.0f);
-  Listed listed;
+  // An entry's logit waits for its id: the ids are loaded two rows ahead, the logits one.
+  Entries<kEach> e, ahead, later;
+  float w_next = weight_of(first + step);
+  if (first_warp) {
+    ahead.load(g, first, w != 0.0f);
+    ahead.load_logits(g, first);
+    later.load(g, first + step, w_next != 0.0f);
+  }
+  Listed<kEach> listed;
   int64_t behind = -1;                            // the row whose listed words are still to be written
   int half = 0;
   bool bad = false;
@@ -230,8 +241,13 @@ __global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillAr
     behind = -1;
   };
   for (int64_t i = first; i < g.N; i += step) {
-    const float w_next = weight_of(i + step);
+    const float w_later = weight_of(i + 2 * step);
     const bool more = w_next != 0.0f;
+    auto advance = [&] {
+      ahead = later;
+      ahead.load_logits(g, i + step);
+      later.load(g, i + 2 * step, w_later != 0.0f);
+    };
     const uint16_t* from = g.z + (i + step) * g.ldl + mine * 8;
     uint16_t* dz = g.dz ? g.dz + i * g.lddl + mine * 8 : nullptr;
     if (w == 0.0f) {                              // a masked row is not read
@@ -240,11 +256,10 @@ __global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillAr
         for (int c = 0; c < whole; ++c) __stcs(reinterpret_cast<uint4*>(dz + c * kHop), make_uint4(0, 0, 0, 0));
         if (tail > 0) store_words(dz + whole * kHop, make_uint4(0, 0, 0, 0), tail);
       }
-      if (more) {
-        fetch(i + step);
-        if (first_warp) ahead.load(g, i + step, true);
-      }
+      if (more) fetch(i + step);
+      if (first_warp) advance();
       w = w_next;
+      w_next = w_later;
       continue;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -258,9 +273,9 @@ __global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillAr
           const int vec = e.id[k] >> 3, slot = vec / (CL * TEAM) * TEAM + vec % TEAM;
           if (strike(reinterpret_cast<uint16_t*>(slots + slot) + (e.id[k] & 7), e.z[k] != -INFINITY)) e.id[k] = -2;
         }
-      if (more) ahead.load(g, i + step, true);
     }
     sync();
+    if (first_warp) advance();
     Running r;
 #pragma unroll 4
     for (int c = 0; c < whole; ++c) r.add(z[c * TEAM], scale);
@@ -321,19 +336,20 @@ __global__ void __launch_bounds__(kThreads, 8) mp_distill_kernel(const DistillAr
     }
     half ^= 1;
     w = w_next;
+    w_next = w_later;
   }
   sync();
   if (first_warp && behind >= 0) write_listed();
   if (bad && g.st) atomicOr(&g.st->h.found_inf, 1);
 }
 
-template <int CL, int TEAM>
+template <int CL, int TEAM, int E>
 int launch(const DistillArgs& g, cudaStream_t st) {
   constexpr int TEAMS = kThreads / TEAM;
   static mp::PerDevice resident[MP_POLICY_MAX_V / 8 / (CL * TEAM) + 1];            // by layers
   const int64_t vecs = (g.V + 7) / 8;
   const int layers = (int)((vecs + CL * TEAM - 1) / (CL * TEAM));
-  auto kernel = mp_distill_kernel<CL, TEAM>;
+  auto kernel = mp_distill_kernel<CL, TEAM, E>;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = (size_t)layers * kThreads * 16;
@@ -360,6 +376,14 @@ int launch(const DistillArgs& g, cudaStream_t st) {
   MP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, g, layers));
   mp::count_launch();
   return MP_OK;
+}
+
+template <int E>                                  // entries of a lane
+int by_width(const DistillArgs& g, cudaStream_t st) {
+  return g.V <= kWarpWords ? launch<1, 32, E>(g, st)
+         : g.V <= kPartWords ? launch<1, kThreads, E>(g, st)
+         : g.V <= 2 * kPartWords ? launch<2, kThreads, E>(g, st)
+         : g.V <= 4 * kPartWords ? launch<4, kThreads, E>(g, st) : launch<8, kThreads, E>(g, st);
 }
 
 }  // namespace
@@ -391,10 +415,7 @@ extern "C" int mp_distill_loss(const void* logits16, int64_t ldl, const void* id
                       state ? state->dev : nullptr};
   cudaStream_t st = (cudaStream_t)stream;
   if (N > 0) {
-    const int rc = V <= kWarpWords ? launch<1, 32>(g, st)
-                   : V <= kPartWords ? launch<1, kThreads>(g, st)
-                   : V <= 2 * kPartWords ? launch<2, kThreads>(g, st)
-                   : V <= 4 * kPartWords ? launch<4, kThreads>(g, st) : launch<8, kThreads>(g, st);
+    const int rc = K <= 32 ? by_width<1>(g, st) : by_width<MP_DISTILL_MAX_K / 32>(g, st);
     if (rc) return rc;
   }
   return loss ? mp::sum_token_loss(token_loss, N, loss, st) : MP_OK;
