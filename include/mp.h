@@ -490,7 +490,8 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
  * p times 2^12 and ds times a power of two that fits the largest rows of do and v, so neither the loss scale nor
  * long rows cost bits.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
  * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs.  inf or NaN in a
- * row of do16 may reach all gradients of its sequence.  workspace: at least mp_attention_bwd_workspace_bytes(..)
+ * row of do16 or v16 may reach all gradients of its sequence, and the other sequences' ds then goes without that power
+ * of two.  workspace: at least mp_attention_bwd_workspace_bytes(..)
  * bytes of device scratch, 16-byte aligned. */
 int mp_attention_bwd(const void* do16, int64_t lddo, const void* q16, int64_t ldq, const void* k16, int64_t ldk,
                      const void* v16, int64_t ldv, const void* o16, int64_t ldo, const float* lse, void* dq16,

@@ -24,6 +24,8 @@ MP_ACT_NONE, MP_ACT_RELU, MP_ACT_CLIPPED_RELU = 0, 1, 2
 MP_NORM_RMS, MP_NORM_LAYER = 0, 1
 MP_NORM_MAX_D = 16384
 MP_ADAMW_BLOCK = 256
+MP_HEAD_MAX_D, MP_ATTENTION_MAX_D, MP_ATTENTION_MAX_ROWS = 256, 128, 1 << 30
+MP_TOP_MAX_K = MP_DISTILL_MAX_K = 128
 
 
 class MpError(RuntimeError):
