@@ -63,7 +63,6 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   __shared__ uint32_t s_tmem;
   const Shape& s = a.s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  ptx::launch_dependents();
   ptx::grid_dependency_wait();
   const int head = blockIdx.x % s.heads;
   const Place at = place_of<kTiles * kTile>(s, blockIdx.x / s.heads);
@@ -92,6 +91,9 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
+  // Only now may the next kernel's blocks come: one that takes tensor memory and then waits for this grid must not find an SM where
+  // a block of this grid has still to take its own.
+  ptx::launch_dependents();
   const uint32_t tmem = s_tmem;
   constexpr uint32_t kO = kTiles * kTile;
   // the long ones first: a causal query sees all keys before it

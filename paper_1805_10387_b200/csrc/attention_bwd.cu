@@ -492,7 +492,6 @@ mp_attention_bwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   BwdBars& b = m.bars();
   const Shape& s = a.s;
   const int warp = threadIdx.x >> 5;
-  ptx::launch_dependents();
   ptx::grid_dependency_wait();
   const bool keys = (int)blockIdx.x < a.key_blocks;
   const int item = keys ? blockIdx.x : blockIdx.x - a.key_blocks, heads = keys ? s.kv_heads : s.heads;
@@ -527,6 +526,7 @@ mp_attention_bwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
+  ptx::launch_dependents();                       // every block has its tensor memory, as in the forward pass
   const bool ok = keys ? keys_block<DP>(mq, mk, mv, mdo, a, at, item % heads, m)
                        : queries_block<DP>(mq, mk, mv, mdo, a, at, item % heads, m);
   if (!ok && (threadIdx.x & 31) == 0) report_timeout(s);

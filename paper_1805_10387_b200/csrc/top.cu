@@ -17,6 +17,8 @@
 namespace {
 
 using namespace softmax;
+using rows::add2;
+using rows::fma2;
 
 struct TopArgs {
   const uint16_t* z;
@@ -32,23 +34,6 @@ struct TopArgs {
   float* tlogp;
   mp_dev_state* st;
 };
-
-// Two FP32 operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<unsigned long long&>(d))
-      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)),
-        "l"(reinterpret_cast<const unsigned long long&>(c)));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("add.rn.f32x2 %0, %1, %2;"
-      : "=l"(reinterpret_cast<unsigned long long&>(d))
-      : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
-  return d;
-}
 
 // s 2^k = sum 2^(z scale), u = sum 2^y y with y = z scale - k.
 struct Sums {
