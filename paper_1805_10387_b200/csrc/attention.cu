@@ -1,13 +1,22 @@
 // Attention over packed sequences, forward: O = softmax(scale Q K^T) V for each head, with the rows' log-sums.
 //
-// One pass over the keys with a running maximum and sum.  A tile of 128 queries meets 64 keys at a time: S = Q K^T (64 columns of
-// tensor memory), the exponentials, O += P V with P in the place of its S as FP16 (rounded once, 2^-12 of the value; the
-// sum is taken from the unrounded FP32 values).  There are two places for S, so the tensor core forms the next scores while
-// these go through the exponential, and what a tile waits for is the special-function unit: 16 results a clock and SM, as long as
-// the products of a head of 128 elements take.  Scores of 128 keys at a time, whose next ones could not be formed before this
-// P was used up, took 1.6 times as long.  Keys and values pass through a ring in shared memory.
+// One pass over the keys with a running maximum and sum.  A tile of 128 queries meets 64 keys at a time: S = Q K^T in
+// tensor memory, the exponentials, O += P V with P in the place of its S as FP16 (rounded once, half a step of 2^-11 of
+// the value; the sum is taken from the unrounded FP32 values).  There are two places for S, so the tensor core forms the next
+// scores while these go through the exponential.  Keys and values pass through a ring in shared memory.
 // The running maximum may lag: it is raised, and O multiplied, only where a row's maximum has passed it by 2^8, so that
 // almost no step pays for it; P stays below 2^8 and its FP16 rounding is relative.
+//
+// What bounds it.  For a head of 128 elements the special-function unit (16 results a clock and SM) and the products take as long,
+// 16384 x 32 heads causal 1.0 and 1.3 ms; a step also waits for its scores and its P to change hands, 150 .. 200 clocks each
+// time, which the other tile's work covers in part: 2.0 .. 2.1 ms (1060 TFLOP/s), 2.4 when the card runs it for seconds
+// and meets its power limit.  Both units are busy just under half the time.  Sequences of 400 (64 of them, 25 heads of 64): a
+// block has seven steps of 64 keys, and of its 20000 clocks 9000 go to finding its place, the first copies and the last stores.
+// Taken back: one place for S and more blocks an SM (444 us against 263 there); 128 keys a step and two threads a row
+// (273 against 248, though 16384 x 32 heads of 128 took 1.98 ms against 2.07); 32 keys a step and three blocks an SM (242
+// against 265, but sequences of 16384 1080 against 963: a rule on the batch's lengths would make a row's bits depend on
+// what else is in the batch, and they do not); part of the exponentials as polynomials (2.25 ms); one lane polling a
+// barrier for its warp (1.51 ms against 1.30); the first copies issued ahead of the block's barrier (259 us against 255).
 
 #include <math.h>
 
@@ -28,8 +37,8 @@ struct FwdArgs {
   float* lse;
 };
 
-// TILES query tiles a block.  Heads of more than 64 elements: two tiles share the keys and values, which would else ask L2
-// for 64 bytes a clock and SM; below that one tile a block and two blocks an SM, whose beginnings and ends cover one another.
+// Heads of more than 64 elements: two tiles of queries a block share the keys and values, which would else ask L2 for 64 bytes a
+// clock and SM.  Below that one tile a block and two blocks an SM, whose beginnings and ends cover one another.
 template <int DP>
 struct FwdLayout {
   static constexpr int kTiles = DP == 64 ? 1 : 2, kBlocks = DP == 64 ? 2 : 1;      // tiles a block, blocks an SM

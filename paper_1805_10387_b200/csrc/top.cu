@@ -1,13 +1,17 @@
 // Scores of given tokens: log-probability, entropy of the distribution, and the top alternatives with theirs.
 //
-// One pass over the row, N V FP16 in and next to nothing out: HBM bounds it, the exponentials (one a word, 16 a clock and
+// One read of the row, N V FP16 in and next to nothing out: HBM bounds it, the exponentials (one a word, 16 a clock and
 // SM) come close.  The sums are those of the losses with one more, u = sum 2^y y for the entropy
-// log2 s - u / s.  The largest logits are found in the same pass: the vectors' maxima of the first few thousand words give a
-// value that at least k words reach, words that reach it are listed in shared memory as they stream by (a
-// few hundred of a random row), and a warp picks the k largest of the list at the end.  Where the list would
-// overflow, the bound is raised to its k-th entry; a row that defeats that too (rising order, thousands of equal
-// logits) is counted through again, bit by bit of the FP16 pattern, exactly.  Entries are one whole number, value
-// before id, so equal values go by the lower id whatever order they were listed in.
+// log2 s - u / s.  A row waits in shared memory (short ones: in a warp's registers) while three things are taken from it in
+// turn: each thread's two best vectors, the sums, and the words that reach a bound.  The bound: a value that each warp's share
+// of k lanes' maxima reach, and of these the lowest, so k words at least reach it; of a random row some dozens more do.  They are
+// listed, and an entry's place is the number of larger ones.  Where the list would overflow (rising order, thousands
+// of equal logits) the row is counted through bit by bit of the FP16 pattern, exactly.  Entries are one whole number,
+// value before id, so equal values go by the lower id whatever order they were listed in.
+//
+// 8192 x 32768, 20 alternatives: 170 us where the bytes alone take 74 (393 in one pass without the row kept, whose list grew
+// long before a good bound was known): a row's phases wait for one another, and the three blocks that fit an SM cover that in
+// part.  Entries of more than one k (128 of 32768: 336 us) take the time that comparing all with all does.
 
 #include <math.h>
 
@@ -246,7 +250,7 @@ __device__ __forceinline__ uint32_t key_reached(int quota, F count) {
   return t;
 }
 
-// ---- rows of up to 1024 words: a warp each, the row in registers ----
+// ---- rows of up to 1024 words: a warp each, the row in registers (40000 x 1000, 20 alternatives: 141 us, a block each 283) ----
 constexpr int kWarpThreads = 128, kWarpRows = kWarpThreads / 32, kWarpWords = 1024;
 template <int C>
 __global__ void __launch_bounds__(kWarpThreads) mp_token_top_warp_kernel(const TopArgs a) {
@@ -673,12 +677,14 @@ extern "C" int mp_token_top(const void* logits16, int64_t ldl, const void* targe
   else if (V <= 512) warp_launch<2>(a, st);
   else if (V <= kWarpWords) warp_launch<4>(a, st);
   else {
-    // A block takes up to kPartWords of a row; more blocks share one where there are fewer rows than SMs and each block has a layer
-    // of vectors still.
-    const bool few = N <= 148 && V > 8 * 256 * 8;
-    const int rc = few || V > 4 * kPartWords ? row_launch<8, 256>(a, st)
-                   : V <= 16384 ? row_launch<1, 128>(a, st) : V <= kPartWords ? row_launch<1, 256>(a, st)
-                   : V <= 2 * kPartWords ? row_launch<2, 256>(a, st) : row_launch<4, 256>(a, st);
+    // A block takes up to kPartWords of a row.  Up to 16384 words blocks of 128 threads, of which twice as many fit an SM, do more
+    // rows at once (16000 x 12000, 40 alternatives: 222 us against 323 with 256 threads; 8192 x 20000: 147 against 136).  Where the
+    // rows leave SMs idle, two or four blocks share one if every thread has a vector of it then (16 x 32768, 128 alternatives:
+    // four 10.3 us, two 12.4, one 16.5; 74 rows: 12.4, 12.4, 17.2; 148: 18.6, 14.5, 18.6; eight are slower than four at each).
+    const int rc = V > 4 * kPartWords ? row_launch<8, 256>(a, st)
+                   : V > 2 * kPartWords || (N <= 74 && V >= 4 * 256 * 8) ? row_launch<4, 256>(a, st)
+                   : V > kPartWords || (N <= 148 && V >= 2 * 256 * 8) ? row_launch<2, 256>(a, st)
+                   : V > 16384 ? row_launch<1, 256>(a, st) : row_launch<1, 128>(a, st);
     if (rc) return rc;
   }
   mp::count_launch();

@@ -185,3 +185,22 @@ def test_backward_of_sharp_and_flat_rows(mp, std, scale):
     c.forward(mp)
     c.backward(mp)
     c.check_backward()
+
+
+@pytest.mark.parametrize("window", [0, 1, 31, 33, 65, 129, 700])
+@pytest.mark.parametrize("lengths", [[512], [513], [1500], [1, 0, 1023], [0, 0, 0, 1300, 31, 33], [511, 513, 515], [97, 1700]])
+@pytest.mark.parametrize("D", [64, 40])
+def test_forward_windows_of_many_lengths(mp, D, lengths, window):
+    c = Case(lengths, 2, 1, D, window=window, seed=len(lengths) + window)
+    c.forward(mp)
+    c.check_forward()
+    c.check_untouched()
+
+
+@pytest.mark.parametrize("lengths", [[513], [1500], [129, 1, 31, 33, 65, 96], [1300, 97]])
+@pytest.mark.parametrize("D", [64, 8])
+def test_forward_of_all_keys_many_lengths(mp, D, lengths):
+    c = Case(lengths, 2, 2, D, causal=False, seed=D, before=3, after=5)
+    c.forward(mp)
+    c.check_forward()
+    c.check_untouched()

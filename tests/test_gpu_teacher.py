@@ -75,6 +75,15 @@ def test_top(mp, N, V, k):
     _check_top(z, k, temp, got, t)
 
 
+# Rows shared by several blocks begin at these widths and end at these numbers of rows.
+@pytest.mark.parametrize("N", [1, 74, 75, 148, 149])
+@pytest.mark.parametrize("V", [4095, 4096, 8191, 8192, 16384, 16385, 32768, 32769, 65537])
+def test_top_where_rows_are_shared(mp, N, V):
+    z = _rows(_gen(N + V), N, V)
+    for k in (1, 128):
+        _check_top(z, k, 1.0, _top(mp, z, k))
+
+
 @pytest.mark.parametrize("kind", ["equal", "steps", "rising", "falling", "minus_inf", "few", "zeros", "peak"])
 @pytest.mark.parametrize("N,V,k", [(6, 29, 29), (6, 900, 100), (6, 5000, 128), (6, 40000, 64), (200, 40000, 64), (3, 131071, 128)])
 def test_top_of_rows_that_defeat_a_bound(mp, kind, N, V, k):
