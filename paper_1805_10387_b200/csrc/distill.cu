@@ -185,9 +185,9 @@ __device__ __forceinline__ bool strike(uint16_t* word, bool finite) {
 // TEAM threads a row: a warp each (short rows), or a block, or CL blocks of a cluster.  The layout of a row over its
 // threads and the refilling of its slots are the policy loss's.
 // Blocks an SM: where several share a row six (1021 x 131071, 128 entries: 153 us, with seven 168), else seven, which 16384 words
-// each leave room for.
+// each leave room for; of warps eight, or five where a lane has four entries (20000 x 2000, 64 entries: 71 us, with eight 75).
 template <int CL, int TEAM, int kEach>
-__global__ void __launch_bounds__(kThreads, TEAM == 32 ? 8 : CL > 1 ? 6 : 7) mp_distill_kernel(const DistillArgs g, int layers) {
+__global__ void __launch_bounds__(kThreads, TEAM == 32 ? kEach > 1 ? 5 : 8 : CL > 1 ? 6 : 7) mp_distill_kernel(const DistillArgs g, int layers) {
   static_assert(TEAM == kThreads || (TEAM == 32 && CL == 1), "a warp, a block or a cluster for a row");
   constexpr int TEAMS = kThreads / TEAM;
   extern __shared__ uint4 all_slots[];            // [team][vectors]

@@ -3,8 +3,8 @@
 // A row of the projection's output is heads of D elements; each is divided by its root mean square, multiplied by a
 // gain (one for the queries, one for the keys) and rotated pair by pair by the token's position.  One read and one
 // write of the heads (backward: two reads and a write).  6387 tokens x 30 heads of 128: 28 us, where the bytes alone take
-// 15; 8192 x 32 heads of 64 backward, with the gains' gradients: 37 us, the bytes 15.  What bounds it is issue: seven of ten
-// slots are used forward, 5.7 backward, where two blocks an SM are all that the gains' sums leave registers for.
+// 15; 8192 x 32 heads of 64 backward, with the gains' gradients: 37 us, the bytes 15.  What bounds it is issue: 6.7 of ten
+// slots are used forward, 5.6 backward, where two blocks an SM are all that the gains' sums leave registers for.
 // Angles formed by each lane for itself, in blocks of a few tokens each, took 35 us and 46; loads of the next round ahead of this
 // one's work were no faster: other warps cover them.
 // L lanes share a head, 8 elements each, so 32 / L heads are worked on by a warp at a time ("a round"); a warp keeps one
@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kRounds = 4;                        // whose loads are in flight together
-constexpr int kMaxBlocks = 148 * 2;               // as many as are resident; rows of the backward kernel's partial sums
+constexpr int kMaxBlocks = 148 * 2;               // of the backward kernel: as many as are resident; rows of its partial sums
 
 struct HeadArgs {
   const uint16_t *x, *dy, *gq, *gk;
@@ -112,8 +112,12 @@ struct Rounds {
   }
 };
 
+// Blocks an SM: three forward (16384 x 40 heads of 128: 84 us; with four, which spill at 64 registers,
+// 87), two backward.
+template <bool BACK>
+constexpr int kResident = BACK ? 2 : 3;
 template <int L, bool PAIRS, bool BACK>
-__global__ void __launch_bounds__(kThreads, BACK ? 2 : 4) mp_head_norm_rope_kernel(const HeadArgs a) {
+__global__ void __launch_bounds__(kThreads, kResident<BACK>) mp_head_norm_rope_kernel(const HeadArgs a) {
   constexpr int U = kRounds;
   __shared__ __align__(16) float2 tables[kWarps][kAngles];
   __shared__ uint64_t turns[MP_HEAD_MAX_D / 2];
@@ -264,12 +268,12 @@ int launch(HeadArgs a, int* used, cudaStream_t st) {
   const int rounds = (a.hq + G - 1) / G + (a.hk + G - 1) / G;
   // Tokens are cut into parts until every warp has some six of them, so that the last ones do not leave many idle, but not below the
   // rounds whose loads are in flight together; few tokens down to one round a warp, so that the loads of all heads start at once.
-  const int64_t warps = (int64_t)148 * (BACK ? 2 : 4) * kWarps, whole = (rounds + kRounds - 1) / kRounds;
+  const int64_t warps = (int64_t)148 * kResident<BACK> * kWarps, whole = (rounds + kRounds - 1) / kRounds;
   int64_t parts = (6 * warps + a.T - 1) / a.T;
   if (parts > whole) parts = a.T * whole >= warps ? whole : (warps + a.T - 1) / a.T;
   a.parts = (int)(parts > rounds ? rounds : parts);
   int64_t blocks = (a.T * a.parts + kWarps - 1) / kWarps;
-  if (blocks > 148 * (BACK ? 2 : 4)) blocks = 148 * (BACK ? 2 : 4);
+  if (blocks > 148 * kResident<BACK>) blocks = 148 * kResident<BACK>;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
