@@ -475,7 +475,7 @@ size_t mp_head_norm_rope_bwd_workspace_bytes(int64_t T, int64_t q_heads, int64_t
  * on is then not specified (nothing outside the matrices is touched).  Scores, sums and outputs
  * are FP32 until one rounding; the weights p enter their product in FP16.  Values of other sequences never matter;
  * inf or NaN in a key or value may reach all queries of its own sequence, those that do not see it
- * too.  o16 may not be an input.  T = 0 or n_seq = 0 is legal.  scale > 0. */
+ * too.  o16 may not be an input (refused where their addresses are equal).  T = 0 or n_seq = 0 is legal.  scale > 0. */
 #define MP_ATTENTION_MAX_D 128
 #define MP_ATTENTION_MAX_ROWS (1 << 30)
 int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk, const void* v16, int64_t ldv,
@@ -489,7 +489,7 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
  * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16,
  * p times 2^12 and ds times a power of two that fits the largest rows of do and v, so neither the loss scale nor
  * long rows cost bits.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
- * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs.  inf or NaN in a
+ * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs or one another.  inf or NaN in a
  * row of do16 or v16 may reach all gradients of its sequence, and the other sequences' ds then goes without that power
  * of two.  workspace: at least mp_attention_bwd_workspace_bytes(..)
  * bytes of device scratch, 16-byte aligned. */

@@ -424,6 +424,8 @@ extern "C" int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, i
   if ((uintptr_t)lse & 3) return mp::set_error(MP_ERR_ALIGNMENT, "%s: FP32 values must be aligned", name);
   if (T > 0 && n_seq > 0 && (!q16 || !k16 || !v16 || !o16 || !lse))
     return mp::set_error(MP_ERR_INVALID_ARG, "%s: null pointer", name);
+  if (T > 0 && n_seq > 0 && (o16 == q16 || o16 == k16 || o16 == v16))
+    return mp::set_error(MP_ERR_INVALID_ARG, "%s: the result may not be an input", name);
   if (int rc = mp::check_device()) return rc;
   if (T == 0 || n_seq == 0) return MP_OK;
   if (int rc = mp::gemm_status_device_ptr(&a.s.status)) return rc;

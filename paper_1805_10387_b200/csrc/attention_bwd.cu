@@ -623,6 +623,11 @@ int mp_attention_bwd(const void* do16, int64_t lddo, const void* q16, int64_t ld
   if (need > 0 && T > 0 && n_seq > 0 && (!workspace || workspace_bytes < need))
     return mp::set_error(MP_ERR_NOMEM, "%s: workspace of %zu bytes needed, %zu given", name, need,
                          workspace ? workspace_bytes : (size_t)0);
+  if (T > 0 && n_seq > 0)
+    for (int i = 0; i < 8; ++i)                   // five inputs, three results
+      for (int j = i < 5 ? 5 : i + 1; j < 8; ++j)
+        if (all[i].p == all[j].p)
+          return mp::set_error(MP_ERR_INVALID_ARG, "%s: a result may be neither an input nor another result", name);
   if (int rc = mp::check_device()) return rc;
   if (T == 0 || n_seq == 0) return MP_OK;
   if (int rc = mp::gemm_status_device_ptr(&a.s.status)) return rc;

@@ -642,7 +642,7 @@ def mp_head_norm_rope_bwd(dy16, x16, gq16, gk16, positions, freqs, dx16, dgq16, 
 def _attention_sizes(q16, k16, v16, heads, kv_heads):
     """Rows and head size of an attention call."""
     T, width = q16.shape
-    if heads <= 0 or kv_heads <= 0 or width % heads:
+    if heads <= 0 or kv_heads <= 0 or width % heads or width == 0:
         raise ValueError(f"{width} columns are not {heads} heads")
     return T, width // heads
 

@@ -92,6 +92,18 @@ def test_attention_refusals(p16):
     assert mp.mp_attention_bwd_workspace_bytes(64, 4, 3, 32) == 0
 
 
+def test_attention_refuses_results_in_an_inputs_place(p16):
+    L, at = mp.lib(), {x: p16 + 1024 * i for i, x in enumerate(("do", "q", "k", "v", "o", "dq", "dk", "dv"))}
+    for x in ("q", "k", "v"):
+        assert _attn(L, p16, **{**at, "o": at[x]}) == INV
+    for x in ("dq", "dk", "dv"):
+        for y in at:
+            assert x == y or _attn(L, p16, True, **{**at, x: at[y]}) == INV, (x, y)
+    q = torch.zeros(4, 0, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        mp.mp_attention_fwd(q, q, q, q, torch.zeros(1, 4), torch.zeros(2, dtype=torch.int32), 1, 1)
+
+
 def _top(L, p, **k):
     a = dict(z=p, ldl=64, t=p, tb=8, w=p, N=4, V=60, k=5, temp=1.0, lp=p, ent=p, ids=p, tlp=p)
     a.update(k)
