@@ -474,7 +474,8 @@ size_t mp_head_norm_rope_bwd_workspace_bytes(int64_t T, int64_t q_heads, int64_t
  * (none when they are equal); rows of no sequence are not read, and their outputs stay as they were.
  * Offsets out of order or range give status MP_ERR_INVALID_ARG in the state, and which sequences are worked
  * on is then not specified (nothing outside the matrices is touched).  Scores, sums and outputs
- * are FP32 until one rounding; the weights p enter their product in FP16.  Values of other sequences never matter;
+ * are FP32 until one rounding; the weights p enter their product in FP16 times a power of two: those down to 2^-21 of their row's
+ * largest keep all its bits, smaller ones are off by at most 2^-32 of the largest.  Values of other sequences never matter;
  * inf or NaN in a key or value may reach all queries of its own sequence, those that do not see it
  * too.  o16 may not be an input (refused where their addresses are equal).  T = 0 or n_seq = 0 is legal.  scale > 0. */
 #define MP_ATTENTION_MAX_D 128
@@ -488,8 +489,8 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
  * delta_i = do_i . o_i and ds_ij = p_ij (do_i . v_j - delta_i):
  *   dv_j = sum_i p_ij do_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i
  * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16,
- * p times 2^12 and ds times a power of two that fits the largest rows of do and v, so neither the loss scale nor
- * long rows cost bits.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
+ * p times 2^12, so weights down to 2^-26 keep all its bits, and ds times a power of two that fits the largest rows of do and v, so
+ * the loss scale costs none.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
  * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs or one another.  inf or NaN in a
  * row of do16 or v16 may reach all gradients of its sequence, and the other sequences' ds then goes without that power
  * of two.  workspace: at least mp_attention_bwd_workspace_bytes(..)

@@ -1,11 +1,13 @@
 // Attention over packed sequences, forward: O = softmax(scale Q K^T) V for each head, with the rows' log-sums.
 //
 // One pass over the keys with a running maximum and sum.  A tile of 128 queries meets 64 keys at a time: S = Q K^T in
-// tensor memory, the exponentials, O += P V with P in the place of its S as FP16 (rounded once, half a step of 2^-11 of
-// the value; the sum is taken from the unrounded FP32 values).  There are two places for S, so the tensor core forms the next
+// tensor memory, the exponentials, O += P V with P in the place of its S as FP16 (rounded once; the sum is taken from the
+// unrounded FP32 values).  There are two places for S, so the tensor core forms the next
 // scores while these go through the exponential.  Keys and values pass through a ring in shared memory.
 // The running maximum may lag: it is raised, and O multiplied, only where a row's maximum has passed it by 2^8, so that
-// almost no step pays for it; P stays below 2^8 and its FP16 rounding is relative.
+// almost no step pays for it.  P is held times 2^7, so it stays below 2^15 and fits FP16, and a weight down to 2^-21 of its row's
+// largest is rounded to half a step, 2^-11 of it; smaller ones are off by at most 2^-32 of the largest.  (Without the factor thousands of
+// keys 18 nats below one other weighed nothing, while the sum counted them.)
 //
 // What bounds it.  For a head of 128 elements the special-function unit (16 results a clock and SM) and the products take as long,
 // 16384 x 32 heads causal 1.0 and 1.3 ms; a step also waits for its scores and its P to change hands, 150 .. 200 clocks each
@@ -51,7 +53,7 @@ struct FwdLayout {
   static constexpr int kColumns = DP == 64 ? 256 : 512;      // of tensor memory: S, with P in its place, then O, for each tile
 };
 constexpr int kStep = 64;                         // keys that a tile meets at once
-constexpr float kLag = 8.0f;
+constexpr float kLag = 8.0f, kUp = 7.0f;          // powers of two: see above
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -260,7 +262,7 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
           }
         }
       }
-      const float shift = m == -INFINITY ? 0.0f : -m;
+      const float shift = m == -INFINITY ? 0.0f : kUp - m;
       const float2 c2 = make_float2(c, c), shift2 = make_float2(shift, shift);
       float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
@@ -305,7 +307,7 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
           }
         }
       }
-      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (m + log2f(sum)) * kLn2;
+      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (m + (log2f(sum) - kUp)) * kLn2;
     }
   }
   if (!ok && lane == 0) report_timeout(s);
