@@ -444,7 +444,8 @@ int mp_adamw_update(mp_adamw_plan* plan, mp_state* state, const mp_adamw_config*
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t)
  * pairs are elements (i, i + rot / 2) with pairs 0, (2 i, 2 i + 1) with pairs 1.  positions: T integers of
  * pos_bytes (4 or 8) bytes, of any size; freqs: rot / 2 FP64 values in radians, finite.  The angle is formed in 64-bit fixed
- * point turns, so far positions keep their precision.  y16 may be x16 itself (same pitch).  T = 0 is legal. */
+ * point turns, so far positions keep their precision.  eps >= 0; with 0 a head of zeros has no norm and gives NaN.  y16 may be x16
+ * itself (same pitch).  T = 0 is legal. */
 #define MP_HEAD_MAX_D 256
 int mp_head_norm_rope_fwd(const void* x16, int64_t ldx, const void* gq16, const void* gk16, const void* positions,
                           int pos_bytes, const double* freqs, int64_t rot, int pairs, float eps, void* y16,

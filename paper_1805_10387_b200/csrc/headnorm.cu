@@ -185,7 +185,9 @@ __global__ void __launch_bounds__(kThreads, kResident<BACK>) mp_head_norm_rope_k
         gain.floats(g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-        const float root = rsqrtf(fmaf(head_sum<L>(ss), inv_d, a.eps));
+        ss = head_sum<L>(ss);                     // every lane takes part
+        float root = rsqrtf(fmaf(ss, inv_d, a.eps));
+        if constexpr (BACK) root = h >= 0 ? root : 0.0f;     // zeros must stay so in the gains' sums, without an eps too
         if constexpr (!BACK) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] *= root * g[e];
