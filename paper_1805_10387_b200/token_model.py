@@ -33,8 +33,16 @@ class TokenModel:
                  kl_coef=0.0, init_scale=65536.0, growth_interval=1000, seed=0, device="cuda", heads=0, kv_heads=None,
                  head_dim=64, window=0, rope_base=10000.0, sequences=1):
         """tokens: rows of a step (fixed, as the buffers are).  state_bits: 32, or 8 for E4M3 moments.  heads: query heads of
-        head_dim elements, kv_heads of keys and values (None: as many; 0 heads: no attention), of which a query sees
-        the last `window` (0: all) of its sequence; sequences: how many a step's rows are packed from at most (set_sequences)."""
+        head_dim elements (a multiple of 8, at most mp.MP_ATTENTION_MAX_D), kv_heads of keys and values (None: as many; 0 heads: no
+        attention), of which a query sees the last `window` (0: all) of its sequence; sequences: how many a step's rows are packed
+        from at most (set_sequences)."""
+        if heads:
+            kv = heads if kv_heads is None else kv_heads
+            if heads < 0 or kv <= 0 or heads % kv or window < 0 or sequences < 1:
+                raise ValueError(f"expected key heads that divide the query heads, a window of at least 0 and at least one sequence, got "
+                                 f"{heads} and {kv} heads, a window of {window}, {sequences} sequences")
+            if head_dim <= 0 or head_dim % 8 or head_dim > mp.MP_ATTENTION_MAX_D:
+                raise ValueError(f"expected heads of a multiple of 8 elements, at most {mp.MP_ATTENTION_MAX_D}, got {head_dim}")
         self.V, self.D, self.F, self.L, self.n = vocab, width, inner, blocks, tokens
         self.kind, self.eps, self.res, self.pad_id = kind, eps, res_scale, pad_id
         self.loss_args = dict(clip_lo=clip_lo, clip_hi=clip_hi, kl_coef=kl_coef)
