@@ -377,7 +377,7 @@ int mp_token_logp(const void* logits16, int64_t ldl, const void* targets, int id
  *   top_ids[i, 0 .. k-1], top_logp[i, ..] = the k largest logits' ids and lp, largest first; of equal logits the
  *   lower id comes first.  The same call gives the same bits; the last bits of a row's values may differ with
  *   N, by how many blocks share a row.
- * targets: N integers of id_bytes (4 or 8) bytes, or NULL (then logp must be NULL).  logp, entropy and weight may be
+ * targets: N integers of id_bytes (4 or 8) bytes; targets and logp are both given or both NULL.  entropy and weight may be
  * NULL.  top_ids (int32) and top_logp [N, k] dense, 1 <= k <= min(V, MP_TOP_MAX_K).  A row of weight 0 is not
  * read: its ids become -1, its values 0.  A target out of range gives NaN and a status, as in mp_policy_loss.
  * A row with +inf or NaN among its logits has NaN for its values; its ids are then not specified (-1 or a

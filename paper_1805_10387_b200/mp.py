@@ -566,7 +566,7 @@ def mp_token_logp(logits16, targets, logp, weight=None, state=None):
 
 def mp_token_top(logits16, top_ids, top_logp, targets=None, logp=None, entropy=None, weight=None, temperature=1.0, state=None):
     """top_ids (int32), top_logp [N, k]: the k likeliest tokens of each row and their log-probabilities at the temperature;
-    logp, entropy [N] (FP32, may be None): of targets[i], and of the row.  Rows of weight 0: ids -1, values 0."""
+    logp [N] (FP32): of targets[i] (both or neither); entropy [N] (may be None): of the row.  Rows of weight 0: ids -1, values 0."""
     N, V = logits16.shape
     z, ldl = _rows(logits16, (N, V), _F16)
     if top_ids.dim() != 2 or top_ids.shape[0] != N or not top_ids.is_contiguous():
