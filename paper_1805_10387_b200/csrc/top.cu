@@ -430,9 +430,9 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 8) mp_token_to
   const uint32_t base = ptx::smem_u32(slots) + threadIdx.x * 16;
   uint4* z = slots + threadIdx.x;
   // Each warp's share of k: when every warp has a value that so many of its words reach, k words of the row reach the lowest
-  // of these values.  Warps without a whole layer of vectors (in a row of one block) have none.
-  const int taking = CL > 1 ? CL * kWarps : vecs >= kThreads ? kWarps : vecs / 32;
-  const int share = (a.k + taking - 1) / taking;
+  // of these values.  Every thread has a vector at least: a row has more than 128 vectors for 128 threads, and for 256 in CL blocks
+  // CL * 256 of them.
+  const int share = (a.k + CL * kWarps - 1) / (CL * kWarps);
   auto weight_of = [&](int64_t i) { return i >= a.N ? 0.0f : a.weight ? __ldg(a.weight + i) : 1.0f; };
   auto fetch = [&](int64_t i) {
     const uint16_t* from = a.z + i * a.ldl + (int64_t)mine * 8;
@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 8) mp_token_to
       if (lane == 0) bounds[warp] = mine_reaches;
       __syncthreads();
       bound = bounds[0];
-      for (int x = 1; x < taking; ++x) bound = fminf(bound, bounds[x]);
+      for (int x = 1; x < kWarps; ++x) bound = fminf(bound, bounds[x]);
     }
     // The few threads whose largest word reaches the bound list what does so in its vector; fewer have another such vector, and
     // hardly one a third.
