@@ -491,7 +491,8 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
  *   dv_j = sum_i p_ij do_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i
  * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16,
  * p times 2^12, so weights down to 2^-26 keep all its bits, and ds times a power of two that fits the largest rows of do and v, so
- * the loss scale costs none.  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
+ * the loss scale costs none.  p is formed again from s - lse in FP32: with scores of about 2^k it is off by some 2^(k - 22) of itself, and
+ * from 2^23 on it may pass FP16's range (inf or NaN in the gradients of those rows' sequences).  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
  * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs or one another.  inf or NaN in a
  * row of do16 or v16 may reach all gradients of its sequence, and the other sequences' ds then goes without that power
  * of two.  workspace: at least mp_attention_bwd_workspace_bytes(..)

@@ -4,10 +4,13 @@
 // tensor memory, the exponentials, O += P V with P in the place of its S as FP16 (rounded once; the sum is taken from the
 // unrounded FP32 values).  There are two places for S, so the tensor core forms the next
 // scores while these go through the exponential.  Keys and values pass through a ring in shared memory.
-// The running maximum may lag: it is raised, and O multiplied, only where a row's maximum has passed it by 2^8, so that
-// almost no step pays for it.  P is held times 2^7, so it stays below 2^15 and fits FP16, and a weight down to 2^-21 of its row's
-// largest is rounded to half a step, 2^-11 of it; smaller ones are off by at most 2^-32 of the largest.  (Without the factor thousands of
-// keys 18 nats below one other weighed nothing, while the sum counted them.)
+// P = 2^(score - ref), with ref 7 below a maximum of the row that may lag: it is raised, and O multiplied, only where a score has passed
+// that maximum by 8, so that almost no step pays for it.  So P stays below 2^15 and fits FP16, and a weight down to 2^-21 of its row's
+// largest is rounded to half a step, 2^-11 of it; smaller ones are off by at most 2^-32 of the largest.  (With ref the maximum itself
+// thousands of keys 18 nats below one other weighed nothing, while the sum counted them.)
+// Scores of 2^22 and more (in powers of two), which FP32 holds in steps that count here, are rounded before ref is taken from them: the
+// fused operation keeps what ref has lost in rounding, and P could pass FP16's range.  They have a copy of the steps apart (64 x 400:
+// 236.7 us; a branch in the steps took 242).
 //
 // What bounds it.  For a head of 128 elements the special-function unit (16 results a clock and SM) and the products take as long,
 // 16384 x 32 heads causal 1.0 and 1.3 ms; a step also waits for its scores and its P to change hands, 150 .. 200 clocks each
@@ -53,12 +56,111 @@ struct FwdLayout {
   static constexpr int kColumns = DP == 64 ? 256 : 512;      // of tensor memory: S, with P in its place, then O, for each tile
 };
 constexpr int kStep = 64;                         // keys that a tile meets at once
-constexpr float kLag = 8.0f, kUp = 7.0f;          // powers of two: see above
+constexpr float kLag = 8.0f, kUp = 7.0f, kLarge = 4194304.0f;         // in powers of two: see above
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+
+// The rows of a warp, one a thread: what they see, their tile's barriers, and how far they have come.
+struct Rows {
+  uint32_t ts, to_o;                              // S and O
+  int lo, hi;                                     // steps
+  int key0, key1, whole0, whole1, end;            // keys: of the thread's query, and of the warp's
+  float c;
+  uint64_t *s_full, *p_ready, *o_done;
+  float ref, sum;
+  bool ok;
+};
+// From step u on; returns the first step that is left, where the usual kind has met large scores before anything was made of them.
+template <int DP, bool kAnySize>
+__device__ __forceinline__ int row_steps(Rows& w, int u) {
+  const float c = w.c;
+  for (; u < w.hi && w.ok; ++u) {
+    const int n = u - w.lo, k0 = u * kStep;
+    const uint32_t at_s = w.ts + (n & 1) * kStep;
+    w.ok = wait(&w.s_full[n & 1], n >> 1 & 1);
+    if (!w.ok) break;
+    ptx::tc_fence_after_sync();
+    // pieces of 32 columns with keys that are seen
+    const int pieces = max(0, min(2, (w.end - k0 + 31) / 32));
+    uint32_t r[2][32];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i < pieces) ptx::tmem_ld_32x32(at_s + i * 32, r[i]);
+    ptx::tmem_ld_wait();
+    if (k0 + kStep > w.whole1 || k0 < w.whole0) {
+      const int stop = w.key1 - k0, begin = w.key0 - k0;
+#pragma unroll
+      for (int e = 0; e < kStep; ++e)
+        if (e >= stop || e < begin) r[e / 32][e % 32] = 0xFF800000u;
+    }
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i < pieces)
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          top[2 * i] = max3(top[2 * i], __uint_as_float(r[i][e]), __uint_as_float(r[i][e + 1]));
+          top[2 * i + 1] = max3(top[2 * i + 1], __uint_as_float(r[i][e + 2]), __uint_as_float(r[i][e + 3]));
+        }
+    const float most = max3(fmaxf(top[0], top[1]), top[2], top[3]);
+    // from -inf on: at the first step with a key that is seen
+    const bool raise = (kAnySize ? __fmul_rn(most, c) - w.ref : fmaf(most, c, -w.ref)) > kUp + kLag;
+    if (__any_sync(0xFFFFFFFFu, raise)) {
+      const float next = raise ? (kAnySize ? __fmul_rn(most, c) - kUp : fmaf(most, c, -kUp)) : w.ref, f = raise ? ex2(w.ref - next) : 1.0f;
+      if (!kAnySize && __any_sync(0xFFFFFFFFu, fabsf(next) >= kLarge && next > -INFINITY)) break;
+      w.ref = next;
+      w.sum *= f;
+      if (n > 0) {                                // the products so far have this maximum's factor
+        w.ok = wait(&w.o_done[(n - 1) & 1], n - 1 >> 1 & 1);
+        ptx::tc_fence_after_sync();
+#pragma unroll 1
+        for (int i = 0; i < DP; i += 32) {
+          uint32_t v[32];
+          ptx::tmem_ld_32x32(w.to_o + i, v);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
+          tmem_st_32x32(w.to_o + i, v);
+        }
+      }
+    }
+    const float shift = w.ref == -INFINITY ? 0.0f : -w.ref;
+    const float2 c2 = make_float2(c, c), shift2 = make_float2(shift, shift);
+    float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t p[16];
+      if (i < pieces) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float2 z = make_float2(__uint_as_float(r[i][2 * e]), __uint_as_float(r[i][2 * e + 1]));
+          // (packed, the product and the sum would be fused)
+          const float2 x = kAnySize ? make_float2(__fadd_rn(__fmul_rn(z.x, c), shift), __fadd_rn(__fmul_rn(z.y, c), shift)) : fma2(z, c2, shift2);
+          const float2 y = make_float2(ex2(x.x), ex2(x.y));
+          part[e & 1] = add2(part[e & 1], y);
+          p[e] = rows::pack2(y.x, y.y);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = 0;
+      }
+      tmem_st_32x16(at_s + i * 16, p);
+    }
+    tmem_st_wait();
+    ptx::tc_fence_before_sync();
+    arrive(&w.p_ready[n & 1]);
+    w.sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+  }
+  return u;
+}
+template <int DP>
+__device__ __noinline__ Rows large_row_steps(Rows w, int u) {
+  row_steps<DP, true>(w, u);
+  return w;
 }
 template <int DP>
 __global__ void __launch_bounds__(FwdLayout<DP>::kThreads, FwdLayout<DP>::kBlocks)
@@ -200,7 +302,6 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + t * kTile + lanes, to_o = tmem + kO + t * DP + lanes;
     const int lo = t ? u0[kTiles - 1] : u0[0], hi = t ? u1[kTiles - 1] : u1[0];
-    const float c = s.scale_log2;
     const bool some = row - lane < len;           // the warp has rows that exist
     // the keys that this query sees
     const int key1 = s.causal ? min(row + 1, len) : len;
@@ -209,84 +310,18 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     const int first = row - lane;
     const int whole1 = s.causal ? min(first + 1, len) : len, end = s.causal ? min(first + 32, len) : len;
     const int whole0 = s.window > 0 && first + 32 > s.window ? (int)(first + 32 - s.window) : 0;
-    float m = -INFINITY, sum = 0.0f;
-    for (int u = lo; u < hi && ok; ++u) {
-      const int n = u - lo, k0 = u * kStep;
-      const uint32_t at_s = ts + (n & 1) * kStep;
-      ok = wait(&s_full[t][n & 1], n >> 1 & 1);
-      if (!ok) break;
-      if (!some) {                                // rows of what comes behind the sequence: whatever P holds stays in them
-        arrive(&p_ready[t][n & 1]);
-        continue;
+    Rows w{ts, to_o, lo, hi, key0, key1, whole0, whole1, end, s.scale_log2, s_full[t], p_ready[t], o_done[t], -INFINITY, 0.0f, true};
+    if (some) {
+      const int left = row_steps<DP, false>(w, lo);
+      if (left < hi && w.ok) w = large_row_steps<DP>(w, left);
+      ok = w.ok;
+    } else {                                      // rows of what comes behind the sequence: whatever P holds stays in them
+      for (int n = 0; n < hi - lo && ok; ++n) {
+        ok = wait(&s_full[t][n & 1], n >> 1 & 1);
+        if (ok) arrive(&p_ready[t][n & 1]);
       }
-      ptx::tc_fence_after_sync();
-      // pieces of 32 columns with keys that are seen
-      const int pieces = max(0, min(2, (end - k0 + 31) / 32));
-      uint32_t r[2][32];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (i < pieces) ptx::tmem_ld_32x32(at_s + i * 32, r[i]);
-      ptx::tmem_ld_wait();
-      if (k0 + kStep > whole1 || k0 < whole0) {
-        const int stop = key1 - k0, begin = key0 - k0;
-#pragma unroll
-        for (int e = 0; e < kStep; ++e)
-          if (e >= stop || e < begin) r[e / 32][e % 32] = 0xFF800000u;
-      }
-      float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if (i < pieces)
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            top[2 * i] = max3(top[2 * i], __uint_as_float(r[i][e]), __uint_as_float(r[i][e + 1]));
-            top[2 * i + 1] = max3(top[2 * i + 1], __uint_as_float(r[i][e + 2]), __uint_as_float(r[i][e + 3]));
-          }
-      const float now = max3(fmaxf(top[0], top[1]), top[2], top[3]) * c;
-      const bool raise = now > m + kLag;          // from -inf on: at the first step with a key that is seen
-      if (__any_sync(0xFFFFFFFFu, raise)) {
-        const float f = raise ? ex2(m - now) : 1.0f;
-        m = raise ? now : m;
-        sum *= f;
-        if (n > 0) {                              // the products so far have this maximum's factor
-          ok = wait(&o_done[t][(n - 1) & 1], n - 1 >> 1 & 1);
-          ptx::tc_fence_after_sync();
-#pragma unroll 1
-          for (int i = 0; i < DP; i += 32) {
-            uint32_t v[32];
-            ptx::tmem_ld_32x32(to_o + i, v);
-            ptx::tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-            tmem_st_32x32(to_o + i, v);
-          }
-        }
-      }
-      const float shift = m == -INFINITY ? 0.0f : kUp - m;
-      const float2 c2 = make_float2(c, c), shift2 = make_float2(shift, shift);
-      float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t p[16];
-        if (i < pieces) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float2 x = fma2(make_float2(__uint_as_float(r[i][2 * e]), __uint_as_float(r[i][2 * e + 1])), c2, shift2);
-            const float2 y = make_float2(ex2(x.x), ex2(x.y));
-            part[e & 1] = add2(part[e & 1], y);
-            p[e] = rows::pack2(y.x, y.y);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) p[e] = 0;
-        }
-        tmem_st_32x16(at_s + i * 16, p);
-      }
-      tmem_st_wait();
-      ptx::tc_fence_before_sync();
-      arrive(&p_ready[t][n & 1]);
-      sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
     }
+    const float ref = w.ref, sum = w.sum;
     if (ok && some && hi > lo) {
       ok = wait(&o_done[t][(hi - 1 - lo) & 1], hi - 1 - lo >> 1 & 1);
       ptx::tc_fence_after_sync();
@@ -307,7 +342,7 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
           }
         }
       }
-      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (m + (log2f(sum) - kUp)) * kLn2;
+      if (ok && row < len) a.lse[(int64_t)head * s.T + at.start + row] = (ref + log2f(sum)) * kLn2;
     }
   }
   if (!ok && lane == 0) report_timeout(s);
