@@ -72,7 +72,7 @@ struct Rows {
   float c;
   uint64_t *s_full, *p_ready, *o_done;
   float ref, sum;
-  bool ok;
+  bool on, ok;                                    // the query exists; no wait has run out
 };
 // From step u on; returns the first step that is left, where the usual kind has met large scores before anything was made of them.
 template <int DP, bool kAnySize>
@@ -111,7 +111,7 @@ __device__ __forceinline__ int row_steps(Rows& w, int u) {
     const bool raise = (kAnySize ? __fmul_rn(most, c) - w.ref : fmaf(most, c, -w.ref)) > kUp + kLag;
     if (__any_sync(0xFFFFFFFFu, raise)) {
       const float next = raise ? (kAnySize ? __fmul_rn(most, c) - kUp : fmaf(most, c, -kUp)) : w.ref, f = raise ? ex2(w.ref - next) : 1.0f;
-      if (!kAnySize && __any_sync(0xFFFFFFFFu, fabsf(next) >= kLarge && next > -INFINITY)) break;
+      if (!kAnySize && __any_sync(0xFFFFFFFFu, fabsf(next) >= kLarge && next > -INFINITY && w.on)) break;
       w.ref = next;
       w.sum *= f;
       if (n > 0) {                                // the products so far have this maximum's factor
@@ -310,7 +310,7 @@ mp_attention_fwd_kernel(const __grid_constant__ CUtensorMap mq, const __grid_con
     const int first = row - lane;
     const int whole1 = s.causal ? min(first + 1, len) : len, end = s.causal ? min(first + 32, len) : len;
     const int whole0 = s.window > 0 && first + 32 > s.window ? (int)(first + 32 - s.window) : 0;
-    Rows w{ts, to_o, lo, hi, key0, key1, whole0, whole1, end, s.scale_log2, s_full[t], p_ready[t], o_done[t], -INFINITY, 0.0f, true};
+    Rows w{ts, to_o, lo, hi, key0, key1, whole0, whole1, end, s.scale_log2, s_full[t], p_ready[t], o_done[t], -INFINITY, 0.0f, row < len, true};
     if (some) {
       const int left = row_steps<DP, false>(w, lo);
       if (left < hi && w.ok) w = large_row_steps<DP>(w, left);

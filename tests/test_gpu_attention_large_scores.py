@@ -37,3 +37,19 @@ def test_weights_sum_to_one(mp, power, D, sign):
         x = (c.q.double() @ c.k.double().T).amax(1)
         # what FP32 keeps of the sum of products, in any order of its additions: 2 ^-23 of the magnitude for each of three roundings
         assert bool(((c.lse[0].double() - x).abs() <= 3 * 2.0 ** -23 * x.abs() + math.log(n) + 2.0 ** -18).all()), (step, (c.lse[0].double() - x).abs().max().item())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_queries_of_the_next_sequence_change_no_bits(mp, D, causal):
+    for lengths in ([40, 300], [130, 70], [257, 5]):
+        c = Case(lengths, 2, 1, D, causal, std=3.0, scale=8.0)
+        c.forward(mp)
+        n = lengths[0]
+        o, lse = c.o[:n].clone(), c.lse[:, :n].clone()
+        own = (c.q[:n].float().abs().max() * c.k[:n].float().abs().max() * D * 8).item()
+        assert own < 2.0 ** 21                              # not large themselves
+        for value in (60000.0, math.inf):
+            c.q[n:] = value * c.k[0].sign().repeat(2)
+            c.forward(mp)
+            assert torch.equal(c.o[:n], o) and torch.equal(c.lse[:, :n], lse), (lengths, value)
