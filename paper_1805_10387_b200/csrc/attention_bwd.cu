@@ -14,8 +14,9 @@
 // runs it for seconds); the tensor core is busy 52 %, the rest goes to what the two kinds of product wait for, P and dS on
 // their way through registers and shared memory.  Sixteen warps compute (eight, with two tiles of A, took 1.07 ms), and the next scores are formed
 // while these are worked on, into a second place, from a third tile of A.  Two warps that issue products, which helped the
-// forward pass, took 5 % longer here.  Heads of 64, 16 sequences of 512 on average, 16 heads: 150 .. 190 us; a block
-// has four steps, and about half of its time goes to its beginning and its end, 13 us to the kernel ahead.
+// forward pass, took 5 % longer here.  Heads of 64, 16 sequences of 512 on average, 16 heads: 185 .. 190 us, of which 15 go to the
+// kernel ahead; a block has some four steps and an SM to itself, so nothing covers its place, first copies and last stores, and the last tile of
+// a sequence costs a whole one (64 x 400, 25 heads: 980 us, ten times its operations).
 //
 // FP16 operands P and dS.  P, at most 1, is multiplied by 2^12, so that weights down to 2^-26 keep all their bits.
 // |dS| is at most B = 2 max |dO_i| max |v_j| (row norms, Cauchy and Schwarz), so dS is formed times the power of two
