@@ -489,14 +489,14 @@ int mp_attention_fwd(const void* q16, int64_t ldq, const void* k16, int64_t ldk,
 /* Backward of the call above, from its inputs, o16 and lse; do16 [T, heads D]: gradient at o.  With
  * delta_i = do_i . o_i and ds_ij = p_ij (do_i . v_j - delta_i):
  *   dv_j = sum_i p_ij do_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i
- * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16,
- * p times 2^12, so weights down to 2^-26 keep all its bits, and ds times a power of two that fits the largest rows of do and v, so
- * the loss scale costs none.  p is formed again from s - lse in FP32: with scores of about 2^k it is off by some 2^(k - 22) of itself, and
- * from 2^23 on it may pass FP16's range (inf or NaN in the gradients of those rows' sequences).  Every sum runs in a fixed order.  Rows of no sequence are not read, and their
- * gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be inputs or one another.  inf or NaN in a
- * row of do16 or v16 may reach all gradients of its sequence, and the other sequences' ds then goes without that power
- * of two.  workspace: at least mp_attention_bwd_workspace_bytes(..)
- * bytes of device scratch, 16-byte aligned. */
+ * (for a key head summed over the query heads that share it).  p and ds enter their products in FP16: p times 2^12, so weights
+ * down to 2^-26 keep all its bits, and ds times a power of two that fits the largest rows of do and v, so the loss scale costs
+ * none.  p is formed again from s - lse in FP32: with scores of about 2^k it is off by some 2^(k - 22) of itself, and from 2^23
+ * on it may pass FP16's range (inf or NaN in the gradients of those rows' sequences).  Every sum runs in a fixed order.  Rows of
+ * no sequence are not read, and their gradients stay as they were.  dq16 [T, heads D], dk16, dv16 [T, kv_heads D] may not be
+ * inputs or one another.  inf or NaN in a row of do16 or v16 may reach all gradients of its sequence, and the other sequences'
+ * ds then goes without that power of two.  workspace: at least mp_attention_bwd_workspace_bytes(..) bytes of device scratch,
+ * 16-byte aligned. */
 int mp_attention_bwd(const void* do16, int64_t lddo, const void* q16, int64_t ldq, const void* k16, int64_t ldk,
                      const void* v16, int64_t ldv, const void* o16, int64_t ldo, const float* lse, void* dq16,
                      int64_t lddq, void* dk16, int64_t lddk, void* dv16, int64_t lddv, const void* offsets,
